@@ -483,6 +483,89 @@ int sq_squeezenet_forward_bf16(const void *in, sq_dtype in_dtype, const void *co
                                size_t workspace_bytes, float *const *taps);
 
 /*
+ * Channels-last maps: [N][H][W][C], the C layers of one pixel adjacent, so that a pixel is a row of
+ * a matrix of N*H*W rows.  The layout of the layers that networks put where SqueezeNet has fire
+ * layers: normalise, project every pixel (a 1x1 convolution = a matrix product of rows), add.
+ *   ld (ld_in, ld_out, ld_res): values from one row to the next, at least the row's own length
+ *     (else SQ_ERR_SHAPE).  A larger one makes the operand a slice of a wider map: pass the address
+ *     of its first layer; the other layers of the rows are neither read nor written.
+ *   dtype: SQ_F32 or SQ_BF16 (2 bytes a value); anything else SQ_ERR_UNSUPPORTED.  Sums, statistics
+ *     and activations are fp32 in both, a bfloat16 result is rounded once, to nearest even.
+ *   act: one of the codes below; anything else SQ_ERR_UNSUPPORTED.
+ *   Every pointer must be aligned to the size of its values (else SQ_ERR_UNSUPPORTED); rows whose
+ *     address and ld are multiples of 16 bytes are read and written fastest.
+ *   Sizes: offsets are 64-bit; there is no limit but memory.
+ *   The arithmetic mode of sq_set_dtype() does not matter to these calls.
+ */
+enum {
+    SQ_ACT_NONE = 0,
+    SQ_ACT_RELU = 1,  /* x < 0 ? 0 : x (a NaN stays one)                          */
+    SQ_ACT_SILU = 2,  /* x / (1 + exp(-x))                                        */
+    SQ_ACT_GELU = 3   /* x/2 erfc(-x / sqrt 2), the form with the error function  */
+};
+
+/*
+ * NCHW map to channels-last map and back, with a conversion between the two types on the way
+ * (fp32 to bfloat16 rounds to nearest even, the other direction is exact).
+ *   sq_nhwc_pack():   in [N][C][H][W] of in_dtype, out [N][H][W] rows of ld_out values, of out_dtype.
+ *   sq_nhwc_unpack(): in [N][H][W] rows of ld_in values, of in_dtype; the C layers go to layers
+ *     [c_offset, c_offset + C) of out [N][out_channels][H][W], of out_dtype (0 <= c_offset and
+ *     c_offset + C <= out_channels, else SQ_ERR_SHAPE).
+ * in and out must not overlap.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_HIP.
+ */
+int sq_nhwc_pack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dtype, int N, int C,
+                 int H, int W, int ld_out);
+int sq_nhwc_unpack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dtype, int N, int C,
+                   int H, int W, int ld_in, int out_channels, int c_offset);
+
+/*
+ * Group norm with an activation on a channels-last map.  The C layers form G groups of C/G
+ * neighbouring layers; over the m = H*W*C/G values of one image and group
+ *   mean = sum x / m,  var = sum (x - mean)^2 / m,
+ *   out[n][h][w][c] = act( (x - mean) / sqrt(var + eps) * gamma[c] + beta[c] ).
+ * G = 1 normalises over all layers of an image, G = C each layer by itself.
+ *   in, out: rows of ld_in / ld_out values of dtype.  out may be in itself with the same ld
+ *     (otherwise they must not overlap).
+ *   gamma, beta [C] fp32, each may be NULL (= 1, = 0).
+ *   eps >= 0 (else, or NaN, SQ_ERR_SHAPE).  With eps = 0 a group of equal values gives 0/0.
+ *   workspace: sq_nhwc_group_norm_workspace_bytes(N, C, H, W, G) bytes of device scratch, 256-byte
+ *     aligned (else SQ_ERR_WORKSPACE; 0 = none is needed, workspace may be NULL).  Contents on
+ *     return are unspecified; two calls in flight at once need two.
+ *   An infinity or NaN makes its own image and group NaN and no other.  The squares of the values'
+ *   deviations have to stay within fp32.  The same call gives the same bits every time.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE (incl. C not a multiple of G), SQ_ERR_UNSUPPORTED,
+ * SQ_ERR_WORKSPACE, SQ_ERR_HIP.
+ */
+size_t sq_nhwc_group_norm_workspace_bytes(int N, int C, int H, int W, int G);
+int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *gamma,
+                       const float *beta, int N, int C, int H, int W, int G, float eps, int act,
+                       int ld_in, int ld_out, void *workspace, size_t workspace_bytes);
+
+/*
+ * Matrix product of rows with bias, activation and residual: the fully connected layer, and the
+ * 1x1 convolution of a channels-last map (rows = N*H*W):
+ *   out[r][j] = act( b[j] + sum_k in[r][k] * w[j][k] ) + residual[r][j]
+ *   in [rows] rows of ld_in values, the first Cin of them read; w [Cout][Cin] dense (the kernels of a
+ *     1x1 convolution as they lie); both of in_dtype.
+ *   b [Cout] fp32 or NULL (= zero).
+ *   residual: rows of ld_res values, or NULL (= none; ld_res is then not looked at); out: rows of
+ *     ld_out values; both of out_dtype: SQ_F32 with SQ_F32 inputs, either with SQ_BF16 inputs
+ *     (otherwise SQ_ERR_UNSUPPORTED).  residual may be out itself with the same ld; apart from that
+ *     out must not overlap any input.
+ *   workspace: device scratch, 256-byte aligned (else SQ_ERR_WORKSPACE), or NULL.  With at least
+ *     sq_linear_workspace_bytes(in_dtype, rows, Cin, Cout) bytes a long sum with few results is split
+ *     over more of the chip; less only rules that out (the result is the same up to rounding).
+ *     Contents on return are unspecified; two calls in flight at once need two.
+ *   The same call gives the same bits every time.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP.
+ */
+size_t sq_linear_workspace_bytes(sq_dtype in_dtype, int rows, int Cin, int Cout);
+int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out,
+                      sq_dtype in_dtype, sq_dtype out_dtype, int rows, int Cin, int Cout, int act,
+                      int ld_in, int ld_res, int ld_out, void *workspace, size_t workspace_bytes);
+
+/*
  * Per-launch timing, off by default.  Between sq_profile_begin() and sq_profile_end()
  * every kernel the library launches from this host thread is bracketed by a pair of
  * HIP events on the library's stream.  These two calls are the only ones in the

@@ -18,6 +18,7 @@ lib = ctypes.CDLL(_LIB_PATH)
 
 SQ_F32, SQ_BF16 = 0, 1
 SQ_ALGO_AUTO, SQ_ALGO_DIRECT, SQ_ALGO_VARIANT0 = 0, 1, 2
+SQ_ACT_NONE, SQ_ACT_RELU, SQ_ACT_SILU, SQ_ACT_GELU = 0, 1, 2, 3
 SQ_SQUEEZENET_MAX_BATCH, SQ_SQUEEZENET_BF16_MAX_BATCH = 453, 907   # as in include/sq.h
 
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
@@ -87,6 +88,15 @@ lib.sq_squeezenet_bf16_pack_params.argtypes = [ctypes.POINTER(_vp), _vp, _sz]
 lib.sq_squeezenet_bf16_workspace_bytes.restype = _sz
 lib.sq_squeezenet_bf16_workspace_bytes.argtypes = [_i]
 lib.sq_squeezenet_forward_bf16.argtypes = [_vp, _i, ctypes.POINTER(_vp), _vp, _vp, _i, _vp, _sz, ctypes.POINTER(_vp)]
+
+lib.sq_nhwc_pack.argtypes = [_vp, _i, _vp, _i] + [_i] * 5
+lib.sq_nhwc_unpack.argtypes = [_vp, _i, _vp, _i] + [_i] * 7
+lib.sq_nhwc_group_norm_workspace_bytes.restype = _sz
+lib.sq_nhwc_group_norm_workspace_bytes.argtypes = [_i] * 5
+lib.sq_nhwc_group_norm.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 5 + [ctypes.c_float] + [_i] * 3 + [_vp, _sz]
+lib.sq_linear_workspace_bytes.restype = _sz
+lib.sq_linear_workspace_bytes.argtypes = [_i] * 4
+lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9 + [_vp, _sz]
 
 lib.sq_profile_begin.argtypes = [_i]
 lib.sq_profile_get_mfma_flops.argtypes = [_i, ctypes.POINTER(ctypes.c_double)]
@@ -697,6 +707,156 @@ def sq_squeezenet_forward_bf16(x, params, packed, workspace=None, probs=None, wa
                                         workspace.numel() * workspace.element_size(), tarr)
     _check(rc, "sq_squeezenet_forward_bf16")
     return (probs, taps) if want_taps else probs
+
+
+# ---- channels-last maps -----------------------------------------------------------------------------------------
+# An operand here is a tensor whose last dimension is dense and whose other dimensions count rows at one stride:
+# a contiguous tensor, or a slice of the last dimension of one.  All tensors of a call live on one GPU, which need
+# not be the current one; the call runs on that GPU's current stream.
+_MAX_INT = 2**31 - 1
+
+
+def _rows_of(t, name):
+    """Values from one row to the next."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    shape = t.shape
+    if len(shape) < 2:
+        raise ValueError(f"{name} must have at least two dimensions")
+    length = shape[-1]
+    if t.is_contiguous():
+        ld = length
+    else:
+        stride, ld, span = t.stride(), None, 0
+        for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+            if size == 1:
+                continue
+            if ld is None:
+                ld, span = step, step * size
+            elif step == span:
+                span *= size
+            else:
+                ld = -1
+                break
+        ld = length if ld is None else ld
+        if (stride[-1] != 1 and length > 1) or ld < length:
+            raise ValueError(f"{name} must be contiguous or a slice of the last dimension of a contiguous tensor")
+    if ld > _MAX_INT or max(shape) > _MAX_INT:
+        _check(-3, name)
+    return ld
+
+
+def _same_device(x, *others):
+    for t, name in others:
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name} must live on {x.device}")
+
+
+def _run(x, what, fn, *args):
+    index = x.device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            _use_current_stream()
+            rc = fn(*args)
+    else:
+        _use_current_stream()
+        rc = fn(*args)
+    _check(rc, what)
+
+
+def _scratch(workspace, need, x):
+    if workspace is None:
+        return (None, 0) if need == 0 else _scratch(torch.empty(need, device=x.device, dtype=torch.uint8), need, x)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def sq_nhwc_pack(x, dtype=None, out=None):
+    """NCHW float32 / bfloat16 -> channels-last map [N][H][W][C] of `dtype` (default: that of x or of out)."""
+    N, C, H, W = x.shape
+    if out is None:
+        out = torch.empty((N, H, W, C), device=x.device, dtype=dtype or x.dtype)
+    elif tuple(out.shape) != (N, H, W, C) or dtype not in (None, out.dtype):
+        raise ValueError("out has the wrong shape or type")
+    _same_device(x, (out, "out"))
+    ld = _rows_of(out, "out")
+    _run(x, "sq_nhwc_pack", lib.sq_nhwc_pack, _dev(x, None, "x"), _dtype_code(x, "x"), out.data_ptr(), _dtype_code(out, "out"),
+         N, C, H, W, ld)
+    return out
+
+
+def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
+    """Channels-last map [N][H][W][C] -> NCHW of `dtype`.  `out` may be a larger [N][C'][H][W] tensor; the result lands in
+    layers [c_offset, c_offset + C) and its type is that of out."""
+    N, H, W, C = m.shape
+    if out is None:
+        out = torch.empty((N, C + c_offset, H, W), device=m.device, dtype=dtype)
+    if out.dim() != 4 or (out.shape[0], out.shape[2], out.shape[3]) != (N, H, W):
+        raise ValueError("out has the wrong shape")
+    _same_device(m, (out, "out"))
+    _run(m, "sq_nhwc_unpack", lib.sq_nhwc_unpack, m.data_ptr(), _dtype_code(m, "m"), _dev(out, None, "out"),
+         _dtype_code(out, "out"), N, C, H, W, _rows_of(m, "m"), out.shape[1], int(c_offset))
+    return out
+
+
+def sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups) -> int:
+    return int(lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups))
+
+
+def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NONE, out=None, workspace=None):
+    """Group norm with an activation on a channels-last map [N][H][W][C] (float32 or bfloat16); gamma, beta [C] float32 or
+    None.  `out` may be m itself."""
+    N, H, W, C = m.shape
+    if out is None:
+        out = torch.empty((N, H, W, C), device=m.device, dtype=m.dtype)
+    elif out.shape != m.shape or out.dtype != m.dtype:
+        raise ValueError("out has the wrong shape or type")
+    for t, name in ((gamma, "gamma"), (beta, "beta")):
+        if t is not None and t.numel() != C:
+            raise ValueError(f"{name} must have one value per layer")
+    _same_device(m, (out, "out"), (gamma, "gamma"), (beta, "beta"), (workspace, "workspace"))
+    ld_in, ld_out = _rows_of(m, "m"), _rows_of(out, "out")
+    workspace, nbytes = _scratch(workspace, lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, int(groups)), m)
+    _run(m, "sq_nhwc_group_norm", lib.sq_nhwc_group_norm, m.data_ptr(), out.data_ptr(), _dtype_code(m, "m"),
+         _dev(gamma, torch.float32, "gamma"), _dev(beta, torch.float32, "beta"), N, C, H, W, int(groups), float(eps), int(act),
+         ld_in, ld_out, _dev(workspace), nbytes)
+    return out
+
+
+def sq_linear_workspace_bytes(dtype, rows, Cin, Cout) -> int:
+    """dtype: SQ_F32 or SQ_BF16, the type of the inputs."""
+    return int(lib.sq_linear_workspace_bytes(dtype, rows, Cin, Cout))
+
+
+def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None, workspace=None):
+    """act(x @ w.T + b) + residual.  x [..., Cin] and w [Cout][Cin] (a 1x1 convolution's [Cout][Cin][1][1] too), float32 or
+    both bfloat16; b [Cout] float32 or None; out and residual [..., Cout] of out_dtype (default: that of x, residual or
+    out).  `residual` may be `out` itself."""
+    if w.dim() not in (2, 4) or w.dim() == 4 and tuple(w.shape[2:]) != (1, 1) or x.shape[-1] != w.shape[1]:
+        raise ValueError("kernel shape does not match the input")
+    if x.dtype != w.dtype:
+        raise ValueError("x and w must both be float32 or both bfloat16")
+    Cout, Cin = w.shape[0], w.shape[1]
+    shape = x.shape[:-1] + (Cout,)
+    if out is None:
+        out = torch.empty(shape, device=x.device, dtype=out_dtype or (x.dtype if residual is None else residual.dtype))
+    elif out.shape != shape or out_dtype not in (None, out.dtype):
+        raise ValueError("out has the wrong shape or type")
+    if residual is not None and (residual.shape != shape or residual.dtype != out.dtype):
+        raise ValueError("residual must have the shape and type of the result")
+    if b is not None and b.numel() != Cout:
+        raise ValueError("b must have one value per output layer")
+    _same_device(x, (w, "w"), (b, "b"), (residual, "residual"), (out, "out"), (workspace, "workspace"))
+    ld_in, ld_out = _rows_of(x, "x"), _rows_of(out, "out")
+    ld_res = 0 if residual is None else _rows_of(residual, "residual")
+    rows = x.numel() // Cin if Cin else 0
+    if rows > _MAX_INT or max(Cin, Cout) > _MAX_INT:
+        _check(-3, "sq_linear_forward")
+    code = _dtype_code(x, "x")
+    workspace, nbytes = _scratch(workspace, lib.sq_linear_workspace_bytes(code, rows, Cin, Cout), x)
+    _run(x, "sq_linear_forward", lib.sq_linear_forward, x.data_ptr(), _dev(w, None, "w"), _dev(b, torch.float32, "b"),
+         None if residual is None else residual.data_ptr(), out.data_ptr(), code, _dtype_code(out, "out"), rows, Cin, Cout,
+         int(act), ld_in, ld_res, ld_out, _dev(workspace), nbytes)
+    return out
 
 
 def sq_profile_begin(max_launches: int = 4096) -> None:

@@ -1347,4 +1347,78 @@ int sq_squeezenet_forward_bf16(const void *in, sq_dtype in_dtype, const void *co
     return copy_tap(taps, 14, probs, n * 1000);
 }
 
+namespace {
+bool known_dtype(int d) { return d == SQ_F32 || d == SQ_BF16; }
+bool aligned_to(const void *p, int dtype) { return ((uintptr_t)p & (dtype == SQ_BF16 ? 1 : 3)) == 0; }
+bool known_act(int act) { return act >= SQ_ACT_NONE && act <= SQ_ACT_GELU; }
+}  // namespace
+
+int sq_nhwc_pack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dtype, int N, int C, int H, int W, int ld_out)
+{
+    if (!in || !out) return SQ_ERR_NULL;
+    if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || ld_out < C) return SQ_ERR_SHAPE;
+    if (!known_dtype(in_dtype) || !known_dtype(out_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (!aligned_to(in, in_dtype) || !aligned_to(out, out_dtype)) return SQ_ERR_UNSUPPORTED;
+    return nhwc_pack(in, in_dtype, out, out_dtype, N, C, (long long)H * W, ld_out);
+}
+
+int sq_nhwc_unpack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dtype, int N, int C, int H, int W, int ld_in,
+                   int out_channels, int c_offset)
+{
+    if (!in || !out) return SQ_ERR_NULL;
+    if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || ld_in < C) return SQ_ERR_SHAPE;
+    if (c_offset < 0 || out_channels < C || c_offset > out_channels - C) return SQ_ERR_SHAPE;
+    if (!known_dtype(in_dtype) || !known_dtype(out_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (!aligned_to(in, in_dtype) || !aligned_to(out, out_dtype)) return SQ_ERR_UNSUPPORTED;
+    char *first = (char *)out + (size_t)c_offset * H * W * (out_dtype == SQ_BF16 ? 2 : 4);
+    return nhwc_unpack(in, in_dtype, first, out_dtype, N, C, (long long)H * W, ld_in, out_channels);
+}
+
+size_t sq_nhwc_group_norm_workspace_bytes(int N, int C, int H, int W, int G)
+{
+    if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || G <= 0 || C % G) return 0;
+    return nhwc_group_norm_workspace_bytes(N, C, (long long)H * W, G);
+}
+
+int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *gamma, const float *beta, int N, int C, int H, int W,
+                       int G, float eps, int act, int ld_in, int ld_out, void *workspace, size_t workspace_bytes)
+{
+    if (!in || !out) return SQ_ERR_NULL;
+    if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || G <= 0 || C % G || ld_in < C || ld_out < C) return SQ_ERR_SHAPE;
+    if (!(eps >= 0.f)) return SQ_ERR_SHAPE;
+    if (!known_dtype(dtype) || !known_act(act)) return SQ_ERR_UNSUPPORTED;
+    if (!aligned_to(in, dtype) || !aligned_to(out, dtype) || !aligned_to(gamma, SQ_F32) || !aligned_to(beta, SQ_F32))
+        return SQ_ERR_UNSUPPORTED;
+    const size_t need = sq_nhwc_group_norm_workspace_bytes(N, C, H, W, G);
+    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+    return nhwc_group_norm(in, out, dtype, gamma, beta, N, C, (long long)H * W, G, eps, act, ld_in, ld_out, workspace, workspace_bytes);
+}
+
+size_t sq_linear_workspace_bytes(sq_dtype in_dtype, int rows, int Cin, int Cout)
+{
+    if (!known_dtype(in_dtype) || rows <= 0 || Cin <= 0 || Cout <= 0) return 0;
+    return linear_workspace_bytes(in_dtype, rows, Cin, Cout);
+}
+
+int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out, sq_dtype in_dtype,
+                      sq_dtype out_dtype, int rows, int Cin, int Cout, int act, int ld_in, int ld_res, int ld_out, void *workspace,
+                      size_t workspace_bytes)
+{
+    if (!in || !w || !out) return SQ_ERR_NULL;
+    if (rows <= 0 || Cin <= 0 || Cout <= 0 || ld_in < Cin || ld_out < Cout || (residual && ld_res < Cout)) return SQ_ERR_SHAPE;
+    if (!known_dtype(in_dtype) || !known_dtype(out_dtype) || !known_act(act)) return SQ_ERR_UNSUPPORTED;
+    if (in_dtype == SQ_F32 && out_dtype != SQ_F32) return SQ_ERR_UNSUPPORTED;
+    if (!aligned_to(in, in_dtype) || !aligned_to(w, in_dtype) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype) ||
+        !aligned_to(b, SQ_F32))
+        return SQ_ERR_UNSUPPORTED;
+    if ((uintptr_t)workspace & 255) return SQ_ERR_WORKSPACE;
+    LinearArgs a;
+    a.in = in; a.w = w; a.b = b; a.residual = residual; a.out = out;
+    a.in_dtype = in_dtype; a.out_dtype = out_dtype;
+    a.rows = rows; a.Cin = Cin; a.Cout = Cout; a.act = act;
+    a.ld_in = ld_in; a.ld_res = ld_res; a.ld_out = ld_out;
+    a.ws = workspace; a.ws_bytes = workspace ? workspace_bytes : 0;
+    return linear(a);
+}
+
 }  // extern "C"

@@ -202,6 +202,33 @@ int maxpool(const float *in, float *out, int N, int C, int H, int W, int K, int 
 int avgpool_global(const float *in, float *out, int N, int C, int H, int W);
 int softmax(const float *in, float *out, int N, int C);
 
+// Channels-last maps: [N][HW] rows of ld values, the first C of them the operator's (nhwc_layout.hip, nhwc_norm.hip).
+int nhwc_pack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld);
+int nhwc_unpack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld, int out_channels);
+size_t nhwc_group_norm_workspace_bytes(int N, int C, long long HW, int G);
+int nhwc_group_norm(const void *in, void *out, int dtype, const float *gamma, const float *beta, int N, int C, long long HW, int G,
+                    float eps, int act, long long ld_in, long long ld_out, void *workspace, size_t workspace_bytes);
+// Matrix product of rows (linear.hip), after validation.
+struct LinearArgs {
+    const void *in, *w;
+    const float *b;
+    const void *residual;
+    void *out;
+    int in_dtype, out_dtype;      // of in and w; of residual and out
+    int rows, Cin, Cout, act;
+    long long ld_in, ld_res, ld_out;
+    void *ws;
+    size_t ws_bytes;
+};
+inline double linear_flops(const LinearArgs &a) { return 2.0 * a.rows * a.Cin * a.Cout; }
+inline double linear_bytes(const LinearArgs &a)
+{
+    const double si = a.in_dtype == SQ_BF16 ? 2.0 : 4.0, so = a.out_dtype == SQ_BF16 ? 2.0 : 4.0;
+    return si * ((double)a.rows * a.Cin + (double)a.Cout * a.Cin) + so * (double)a.rows * a.Cout * (a.residual ? 2 : 1) + 4.0 * a.Cout;
+}
+size_t linear_workspace_bytes(int in_dtype, int rows, int Cin, int Cout);
+int linear(const LinearArgs &a);
+
 // Optional per-launch timing (sq_profile_begin/end).  A LaunchScope brackets one kernel
 // launch with a pair of HIP events on the library's stream when profiling is on and
 // costs one thread-local load when it is off.  flops and bytes are the algorithmic
