@@ -237,6 +237,18 @@ def test_linear_shapes(sq, rows, cin, cout, ti, to):
     linear_case(sq, rows, cin, cout, (rows + cin) % 4, ti, to, rows + cin, residual=(rows + cout) % 2 == 0)
 
 
+# enough work for the tiles through LDS: whole and part steps of k, ragged edges both ways, one tile row or column
+LINEAR_LARGE = [(1024, 2048, 1024), (2100, 1032, 1000), (3601, 328, 3584), (13000, 200, 1000), (129, 4096, 4104), (9000, 2056, 130),
+                (2187, 1000, 1001), (4100, 777, 1030)]
+
+
+@pytest.mark.parametrize("ti,to", TYPES)
+@pytest.mark.parametrize("rows,cin,cout", LINEAR_LARGE)
+def test_linear_large(sq, rows, cin, cout, ti, to):
+    linear_case(sq, rows, cin, cout, (rows + cin) % 4, ti, to, rows + cin, residual=(rows + cout) % 2 == 0)
+    linear_case(sq, rows, cin, cout, 0, ti, to, rows + cin, residual=(rows + cout) % 2 == 1, pads=(8, 3, 8))
+
+
 @pytest.mark.parametrize("ti,to", TYPES)
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("rows,cin,cout", [(3, 64, 40), (70, 128, 72), (600, 64, 264)])
