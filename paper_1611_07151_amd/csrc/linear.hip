@@ -84,21 +84,35 @@ template <typename TI> __device__ __forceinline__ u32x4_t load16(const TI *p)
     return __builtin_bit_cast(u32x4_t, load_n<16 / (int)sizeof(TI)>(p));
 }
 
+// Rows and layers of the b-th tile: neighbouring workgroups of one XCD take a band of eight row tiles, row tile fastest,
+// so that what one of its L2 holds is eight row tiles and a few layer tiles.
+__device__ __forceinline__ void tile_at(int b, int tiles, int tiles_r, int tiles_j, int &tr, int &tj)
+{
+    const int q = tiles >> 3, rest = tiles & 7, xcd = b & 7;
+    b = (xcd < rest ? xcd * (q + 1) : rest * (q + 1) + (xcd - rest) * q) + (b >> 3);
+    const int band = b / (8 * tiles_j), in_band = b - band * 8 * tiles_j;
+    const int high = min(8, tiles_r - band * 8);
+    tj = in_band / high;
+    tr = band * 8 + in_band - tj * high;
+}
+
 // ---- few results: wavefronts that share out the sum ---------------------------------------------------------------
 // A workgroup makes CT layers of RT rows; its wavefronts share out k in pieces of 64 bytes of a row ("steps"), each
 // holding the whole RT x CT block of sums in registers, and add up through LDS, in order of wavefronts.  Operands go
 // from memory straight into the lanes of v_mfma_f32_16x16x32_bf16 / _16x16x4_f32: lane l takes 16 bytes of row l % 16 at
 // piece l / 16 of the step (fp32: value i of every lane's four is one instruction; both operands number k alike).
 template <typename TI, typename TO, int RT, int CT, int MAXW>
-__global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, int tiles_j, long long tiles)
+__global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
     constexpr int RB = RT / 16, CB = CT / 16, kStep = 64 / (int)sizeof(TI), kPiece = 16 / (int)sizeof(TI), kRow = CT + 4;
     constexpr int kMost = 16 / (RB + CB) ? 16 / (RB + CB) : 1;       // steps whose loads fly together
     __shared__ float red[MAXW * RT * kRow];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
     const int l16 = lane & 15, piece = lane >> 4;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int r0 = (int)(tile / tiles_j) * RT, j0 = (int)(tile % tiles_j) * CT;
+    {
+        int tr, tj;
+        tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
+        const int r0 = tr * RT, j0 = tj * CT;
         const TI *xr[RB], *wr[CB];
 #pragma unroll
         for (int i = 0; i < RB; ++i) xr[i] = (const TI *)p.in + row_at(r0, 16 * i + l16, p.rows) * p.ld_in + piece * kPiece;
@@ -168,168 +182,480 @@ __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, in
 }
 
 // ---- many results: tiles through LDS ------------------------------------------------------------------------------
-// Rows and layers of the b-th tile: neighbouring workgroups of one XCD take a band of eight row tiles, row tile fastest,
-// so that what one of its L2 holds is eight row tiles and a few layer tiles.
-__device__ __forceinline__ void tile_at(int b, int tiles, int tiles_r, int tiles_j, int &tr, int &tj)
+// The results of a wavefront, 32 * XB rows from r0 on and 32 * JB layers from j0 on, out through its own part of LDS, 32 rows at
+// a time: the accumulators hold a row's layers spread over registers and lanes, LDS gives them back row by row, so that
+// the residual is read and the result written in whole lines.  A lane's layers are the same in every row: its bias is loaded
+// once, and the residual one block of 32 rows ahead.
+template <typename TO, int XB, int JB> __device__ __forceinline__ void write_rows(const LinearArgs &p, float *buf, const f32x16_t (&acc)[XB][JB], int r0, int j0, int lane)
 {
-    const int q = tiles >> 3, rest = tiles & 7, xcd = b & 7;
-    b = (xcd < rest ? xcd * (q + 1) : rest * (q + 1) + (xcd - rest) * q) + (b >> 3);
-    const int band = b / (8 * tiles_j), in_band = b - band * 8 * tiles_j;
-    const int high = min(8, tiles_r - band * 8);
-    tj = in_band / high;
-    tr = band * 8 + in_band - tj * high;
-}
-
-// A wavefront's 32 rows x 32*NJ layers (in order j-block, then the accumulator's registers), through its own part of
-// LDS, out row by row.
-template <typename TO, int NJ> __device__ __forceinline__ void write_rows(const LinearArgs &p, float *buf, const f32x16_t (&acc)[NJ], int r0, int j0, int lane)
-{
-    constexpr int kRow = 32 * NJ + 4, n = 16 / (int)sizeof(TO), kLanes = 32 * NJ / n, kPer = 64 / kLanes;
+    constexpr int kRow = 32 * JB + 4, n = 16 / (int)sizeof(TO), kLanes = 32 * JB / n, kPer = 64 / kLanes, kTurns = 32 / kPer;
+    const int j = lane % kLanes * n, row = lane / kLanes;
+    auto stage = [&](int x) {
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int c = 0; c < NJ; ++c)
+        for (int c = 0; c < JB; ++c)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4_t v = {acc[c][4 * q], acc[c][4 * q + 1], acc[c][4 * q + 2], acc[c][4 * q + 3]};
-            *(f32x4_t *)&buf[(lane & 31) * kRow + c * 32 + q * 8 + (lane >> 5) * 4] = v;
+            for (int q = 0; q < 4; ++q) {
+                const f32x4_t v = {acc[x][c][4 * q], acc[x][c][4 * q + 1], acc[x][c][4 * q + 2], acc[x][c][4 * q + 3]};
+                *(f32x4_t *)&buf[(lane & 31) * kRow + c * 32 + q * 8 + (lane >> 5) * 4] = v;
+            }
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto staged = [&](int t, float (&v)[n]) {
+#pragma unroll
+        for (int e = 0; e < n; e += 4) *(f32x4_t *)&v[e] = *(const f32x4_t *)&buf[(row + t * kPer) * kRow + j + e];
+    };
+    if (!row_in(r0, 32 * XB - 1, p.rows) || !row_in(j0, 32 * JB - 1, p.Cout)) {     // the edge of the output
+#pragma unroll
+        for (int x = 0; x < XB; ++x) {
+            stage(x);
+#pragma unroll 1
+            for (int t = 0; t < kTurns; ++t) {
+                float v[n];
+                staged(t, v);
+                const int i = 32 * x + row + t * kPer;
+                if (row_in(r0, i, p.rows)) finish<TO>(p, (long long)r0 + i, j0 + j, p.Cout - j0 - j, v);
+            }
         }
-    __builtin_amdgcn_wave_barrier();
-    const int j = lane % kLanes * n;
-    for (int i = lane / kLanes; i < 32; i += kPer) {
-        float v[n];
-#pragma unroll
-        for (int e = 0; e < n; e += 4) *(f32x4_t *)&v[e] = *(const f32x4_t *)&buf[i * kRow + j + e];
-        if (row_in(r0, i, p.rows)) finish<TO>(p, (long long)r0 + i, j0 + j, p.Cout - j0 - j, v);
+        return;
     }
-    __builtin_amdgcn_wave_barrier();
+    float bias[n];
+#pragma unroll
+    for (int e = 0; e < n; ++e) bias[e] = 0.f;
+    if (p.b) {
+        const Vec<float, n> b = load_n<n>(p.b + j0 + j);
+#pragma unroll
+        for (int e = 0; e < n; ++e) bias[e] = b.v[e];
+    }
+    const TO *res = (const TO *)p.residual + (r0 + row) * p.ld_res + j0 + j;
+    TO *out = (TO *)p.out + (r0 + row) * p.ld_out + j0 + j;
+    Vec<TO, n> ahead[kTurns];
+    auto load = [&](int x) {
+        if (p.residual)
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t) ahead[t] = load_n<n>(res + (32 * x + t * kPer) * p.ld_res);
+    };
+    auto blocks = [&](auto act) {
+        load(0);
+#pragma unroll
+        for (int x = 0; x < XB; ++x) {
+            stage(x);
+            float v[kTurns][n];
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t) {
+                staged(t, v[t]);
+#pragma unroll
+                for (int e = 0; e < n; ++e) v[t][e] = activate<decltype(act)::value>(v[t][e] + bias[e]);
+                if (p.residual)
+#pragma unroll
+                    for (int e = 0; e < n; ++e) v[t][e] += to_f32(ahead[t].v[e]);
+            }
+            if (x + 1 < XB) load(x + 1);
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t) {
+                Vec<TO, n> o;
+#pragma unroll
+                for (int e = 0; e < n; ++e) o.v[e] = from_f32<TO>(v[t][e]);
+                __builtin_memcpy(out + (32 * x + t * kPer) * p.ld_out, &o, sizeof(o));
+            }
+        }
+    };
+    switch (p.act) {
+        case SQ_ACT_RELU: blocks(std::integral_constant<int, SQ_ACT_RELU>{}); break;
+        case SQ_ACT_SILU: blocks(std::integral_constant<int, SQ_ACT_SILU>{}); break;
+        case SQ_ACT_GELU: blocks(std::integral_constant<int, SQ_ACT_GELU>{}); break;
+        default: blocks(std::integral_constant<int, SQ_ACT_NONE>{});
+    }
 }
 
 // bfloat16: BM rows x BN layers per workgroup of WR x WC wavefronts, v_mfma_f32_32x32x16_bf16 with the kernels as the
 // first operand.  64 values of k per step; a row's 128 bytes lie as eight 16-byte pieces, piece q of row r at place
-// q ^ (r & 7), so that the 32 rows a read takes at one k spread over all banks.  Two images of the step in LDS: the
+// q ^ (r / 2 % 8), so that any 16 neighbouring rows a read takes at one k cover the 64 banks once.  Two images of the step in LDS: the
 // next one is loaded (memory to LDS directly) while this one is multiplied.
-template <typename TO, int BM, int BN, int WR, int WC> __device__ __forceinline__ void linear_tile_bf16(const LinearArgs &p, int tiles_r, int tiles_j)
+template <typename TO, int BM, int BN, int WR, int WC, int NS>
+__global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 : 1) void linear_tile_bf16_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
-    constexpr int NW = WR * WC, XB = BM / WR / 32, JB = BN / WC / 32;
-    constexpr int XI = BM / 8 / NW, JI = BN / 8 / NW;       // loads of 8 rows per wavefront
-    __shared__ u32x4_t lds0[(BM + BN) * 8];
-    __shared__ u32x4_t lds1[(BM + BN) * 8];
+    constexpr int NW = WR * WC, XB = BM / WR / 32, JB = BN / WC / 32, kImage = (BM + BN) * 8;
+    constexpr int XI = BM / 8 / NW, JI = BN / 8 / NW, NI = XI + JI;       // loads of 8 rows per wavefront
+    __shared__ u32x4_t lds[NS * kImage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
     const int r0 = tr * BM, j0 = tj * BN;
-    const int piece = (lane & 7) ^ (lane >> 3);
-    // per load the lane's row and piece as a 32-bit offset from the tile's first row; k moves in the uniform offset
-    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void *)((const bf16_t *)p.in + r0 * p.ld_in), 0, 0xffffffffu, 0x00020000);
-    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)((const bf16_t *)p.w + (long long)j0 * p.Cin), 0, 0xffffffffu, 0x00020000);
-    uint32_t xo[XI], wo[JI];
+    // Loads 0 to XI - 1 of a wavefront are rows of the input, the others of the kernels; load i takes rows 8 g to 8 g + 7, the
+    // lane's row is lane / 8 and its place lane % 8.  Per load the lane's row and piece are a 32-bit offset from the
+    // tile's first row; k moves in the uniform offset.
+    auto piece = [&](int i) { return (lane & 7) ^ (((wave * (i < XI ? XI : JI) + (i < XI ? i : i - XI)) & 1) * 4 + (lane >> 4)); };
+    const bf16_t *const x0 = (const bf16_t *)p.in + r0 * p.ld_in, *const w0 = (const bf16_t *)p.w + (long long)j0 * p.Cin;
+    const u32x4_t xr = {(uint32_t)(uintptr_t)x0, (uint32_t)((uintptr_t)x0 >> 32), 0xffffffffu, 0x00020000u};
+    const u32x4_t wr = {(uint32_t)(uintptr_t)w0, (uint32_t)((uintptr_t)w0 >> 32), 0xffffffffu, 0x00020000u};
+    uint32_t off[NI];
 #pragma unroll
-    for (int i = 0; i < XI; ++i) xo[i] = (uint32_t)(row_at(r0, (wave * XI + i) * 8 + (lane >> 3), p.rows) - r0) * (uint32_t)(2 * p.ld_in) + piece * 16;
-#pragma unroll
-    for (int i = 0; i < JI; ++i) wo[i] = (uint32_t)(row_at(j0, (wave * JI + i) * 8 + (lane >> 3), p.Cout) - j0) * (uint32_t)(2 * p.Cin) + piece * 16;
-    auto fetch = [&](u32x4_t *to, int k) {
-        u32x4_t *xto = to + wave * XI * 64, *wto = to + BM * 8 + wave * JI * 64;
-#pragma unroll
-        for (int i = 0; i < XI; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void *)(xto + i * 64), 16, xo[i], 2 * k, 0, 0);
-#pragma unroll
-        for (int i = 0; i < JI; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void *)(wto + i * 64), 16, wo[i], 2 * k, 0, 0);
+    for (int i = 0; i < NI; ++i)
+        off[i] = i < XI ? (uint32_t)(row_at(r0, (wave * XI + i) * 8 + (lane >> 3), p.rows) - r0) * (uint32_t)(2 * p.ld_in) + piece(i) * 16
+                        : (uint32_t)(row_at(j0, (wave * JI + i - XI) * 8 + (lane >> 3), p.Cout) - j0) * (uint32_t)(2 * p.Cin) + piece(i) * 16;
+    auto place_of = [&](int i) { return i < XI ? (wave * XI + i) * 64 : BM * 8 + (wave * JI + i - XI) * 64; };
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4_t *)lds);
+    // Load i of the step at k into an image.  As an instruction of its own, because the compiler would let every later read of
+    // LDS wait for it; `arrive` is what orders them.  m0 is set before each: nothing else in this kernel reads it (gfx950's
+    // LDS instructions do not).
+    auto fetch = [&](int img, int k, int i) {
+        __asm__ volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+                         :: "v"(off[i]), "s"(i < XI ? xr : wr), "s"(2 * k), "s"(lds0 + 16 * (uint32_t)(img * kImage + place_of(i))));
     };
     const int xrow = wave / WC * (XB * 32) + (lane & 31), wrow = BM + wave % WC * (JB * 32) + (lane & 31);
     f32x16_t acc[XB][JB] = {};
-    auto multiply = [&](const u32x4_t *from) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int place = (2 * s + (lane >> 5)) ^ (lane & 7);
-            bf16x8 x[XB], w[JB];
-#pragma unroll
-            for (int i = 0; i < JB; ++i) w[i] = __builtin_bit_cast(bf16x8, from[(wrow + 32 * i) * 8 + place]);
-#pragma unroll
-            for (int i = 0; i < XB; ++i) x[i] = __builtin_bit_cast(bf16x8, from[(xrow + 32 * i) * 8 + place]);
-#pragma unroll
-            for (int i = 0; i < XB; ++i)
-#pragma unroll
-                for (int c = 0; c < JB; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[c], x[i], acc[i][c], 0, 0, 0);
-        }
+    // Until all but the loads of the `younger` youngest steps have landed, and every wavefront is here: a wavefront waits for
+    // its own loads and for its reads of LDS, the barrier for those of the others.
+    auto arrive = [&](auto younger, bool all) {
+        if (decltype(younger)::value > 0 && !all) __asm__ volatile("s_waitcnt vmcnt(%0)" :: "n"(decltype(younger)::value * NI) : "memory");
+        else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
-    auto arrive = [&]() {
-        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    // the part of k behind the last whole step goes first, through registers, with zeros behind its end
-    const int whole = p.Cin & ~63;
-    if (whole < p.Cin) {
-        const int have = p.Cin - whole - piece * 8;
-        const bf16_t *x = (const bf16_t *)p.in + r0 * p.ld_in + whole, *w = (const bf16_t *)p.w + (long long)j0 * p.Cin + whole;
+    // Step s lies in image s % NS.  The part of k behind the last whole step goes first, through registers, with zeros behind
+    // its end, as step -1 in the last image.
+    const int whole = p.Cin / 64, tail = p.Cin - 64 * whole;
+    if (tail) {
 #pragma unroll 1
-        for (int i = 0; i < XI; ++i) lds1[(wave * XI + i) * 64 + lane] = load16_tail((const bf16_t *)((const char *)x + xo[i]), have);
-#pragma unroll 1
-        for (int i = 0; i < JI; ++i) lds1[BM * 8 + (wave * JI + i) * 64 + lane] = load16_tail((const bf16_t *)((const char *)w + wo[i]), have);
-    } else {
-        fetch(lds0, 0);
+        for (int i = 0; i < NI; ++i)
+            lds[(NS - 1) * kImage + place_of(i) + lane] = load16_tail((const bf16_t *)((const char *)((i < XI ? x0 : w0) + 64 * whole) + off[i]), tail - piece(i) * 8);
     }
-    for (int k = whole < p.Cin ? -128 : 0;; k += 128) {
-        if (k >= 0) {
-            arrive();
-            if (k + 64 < whole) fetch(lds1, k + 64);
-            multiply(lds0);
-            if (k + 64 >= whole) break;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+        if (s < (tail ? min(whole, NS - 1) : whole)) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) fetch(s, 64 * s, i);
         }
-        arrive();
-        if (k + 128 < whole) fetch(lds0, k + 128);
-        multiply(lds1);
-        if (k + 128 >= whole) break;
+    // Four parts of 16 k per step; the operands of a part are read while the part before is multiplied.  Before the last part,
+    // whose operands are in registers by then, every wavefront is done with the image: it takes step s + NS, and the
+    // first operands of step s + 1 are read under the last part's products.
+    bf16x8 x[2][XB], w[2][JB];
+    auto read = [&](const u32x4_t *from, int q) {
+        const int place = (2 * q + (lane >> 5)) ^ ((lane >> 1) & 7);
+#pragma unroll
+        for (int i = 0; i < JB; ++i) w[q & 1][i] = __builtin_bit_cast(bf16x8, from[(wrow + 32 * i) * 8 + place]);
+#pragma unroll
+        for (int i = 0; i < XB; ++i) x[q & 1][i] = __builtin_bit_cast(bf16x8, from[(xrow + 32 * i) * 8 + place]);
+    };
+    // with half of the loads of a step spread over the products: issued at once they hold the wavefront up while the unit
+    // that takes them works through 64 bytes a cycle
+    auto multiply = [&](int q, bool load, int to, int k, int half) {
+#pragma unroll
+        for (int m = 0; m < XB * JB; ++m) {
+            if (half >= 0) {
+                if (load) {
+#pragma unroll
+                    for (int i = 0; i < NI / 2; ++i)
+                        if (i * XB * JB / (NI / 2) == m) fetch(to, k, half * (NI / 2) + i);
+                }
+            }
+            if (m == 0) __builtin_amdgcn_s_setprio(1);
+            acc[m / JB][m % JB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[q & 1][m % JB], x[q & 1][m / JB], acc[m / JB][m % JB], 0, 0, 0);
+            if (half >= 0) __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    int img = tail ? NS - 1 : 0;
+    arrive(std::integral_constant<int, NS - 1>{}, tail || whole < NS);
+    read(lds + img * kImage, 0);
+    const int first = tail ? -1 : 0;
+    for (int s = first; s < whole; ++s) {
+        const u32x4_t *const from = lds + img * kImage;
+        const int next = img == NS - 1 ? 0 : img + 1, last = img == 0 ? NS - 1 : img - 1;
+        read(from, 1);
+        multiply(0, s > first && s - 1 + NS < whole, last, 64 * (s - 1 + NS), 1);
+        read(from, 2);
+        multiply(1, false, 0, 0, -1);
+        read(from, 3);
+        multiply(2, false, 0, 0, -1);
+        if (s + 1 < whole) {
+            arrive(std::integral_constant<int, NS - 2>{}, s + NS > whole);
+            read(lds + next * kImage, 0);
+        }
+        multiply(3, s + NS < whole, img, 64 * (s + NS), 0);
+        img = next;
     }
     __syncthreads();
     constexpr int kBuf = 32 * (32 * JB + 4);
-    static_assert(kBuf * 4 * (NW / 2) <= (BM + BN) * 128, "the exchange areas of half of the wavefronts fit an image");
-    float *buf = wave < NW / 2 ? (float *)lds0 + wave * kBuf : (float *)lds1 + (wave - NW / 2) * kBuf;
-#pragma unroll
-    for (int i = 0; i < XB; ++i)
-        write_rows<TO, JB>(p, buf, acc[i], r0 + wave / WC * (XB * 32) + 32 * i, j0 + wave % WC * (JB * 32), lane);
+    static_assert(kBuf * 4 * NW <= NS * kImage * 16, "the wavefronts' exchange areas fit the images");
+    write_rows<TO, XB, JB>(p, (float *)lds + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
 }
 
-template <typename TO, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(64 * WR *WC) void linear_tile_bf16_kernel(LinearArgs p, int tiles_r, int tiles_j)
+// The same tiles through registers: operands that memory-to-LDS loads cannot take (rows at any address, any number of
+// layers) and fp32.  A step is 128 bytes of a row, PF of them on their way in registers, two images in LDS.
+//
+// fp32 products run on the bf16 instructions: every operand is the sum of three bfloat16 values, x = h + m + l with h its
+// upper half, m = round(x - h) and l = x - h - m, all three exact (24 bits in pieces of at most 8), and of the nine products the
+// six down to 2^-16 of the largest are summed: m l, l m and l l are together below 2^-22 of the term, with the sign of
+// chance, where each addition in fp32 loses up to 2^-24 of a whole sum.  Six instructions of 16 k cost 192 cycles of the
+// matrix unit where fp32 ones take 512.  Every term keeps its own accuracy whatever lies beside it; only operands below
+// 2^-110 lose bits (their l falls below what a bfloat16 can hold).
+// An infinity has no such form (inf - inf).  It, a NaN, or sums that overflow leave a sum that is not finite; the tile is then
+// made once more from the rounded upper parts alone, whose products have the right infinities and NaN, and those results
+// that were not finite take its values.
+template <typename TI> struct Image;
+template <> struct Image<bf16_t> {
+    static constexpr int kStep = 64, kPlanes = 1;
+    // 16-byte piece q of row r
+    static __device__ __forceinline__ int at(int r, int q) { return r * 8 + (q ^ ((r >> 1) & 7)); }
+};
+template <> struct Image<float> {
+    static constexpr int kStep = 32, kPlanes = 3;
+    // 16-byte piece q of row r in one of the planes: two rows share 128 bytes
+    static __device__ __forceinline__ int at(int r, int q) { return (r >> 1) * 8 + (((r & 1) * 4 + q) ^ ((r >> 2) & 3)); }
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
 {
-    linear_tile_bf16<TO, BM, BN, WR, WC>(p, tiles_r, tiles_j);
+    uint32_t v;     // written out: the compiler would round `a` a second time where it is wanted as fp32 again
+    __asm__("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(v) : "v"(a), "v"(b));
+    return v;
+}
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l)
+{
+    const uint32_t ua = __builtin_bit_cast(uint32_t, a), ub = __builtin_bit_cast(uint32_t, b);
+    h = __builtin_amdgcn_perm(ub, ua, 0x07060302);
+    a -= __builtin_bit_cast(float, ua & 0xffff0000u);
+    b -= __builtin_bit_cast(float, ub & 0xffff0000u);
+    m = bf16_pair(a, b);
+    l = bf16_pair(a - __builtin_bit_cast(float, m << 16), b - __builtin_bit_cast(float, m & 0xffff0000u));
+}
+
+template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF>
+__global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, int tiles_r, int tiles_j)
+{
+    using I = Image<TI>;
+    constexpr int NW = WR * WC, XB = BM / WR / 32, JB = BN / WC / 32, kRows = BM + BN, kStep = I::kStep;
+    constexpr int kPlane = kRows * 8 / (sizeof(TI) == 4 ? 2 : 1), kImage = kPlane * I::kPlanes;       // in 16-byte pieces
+    constexpr int NP = kRows * 8 / (64 * NW), kPiece = 16 / (int)sizeof(TI), kSub = kStep / 16;
+    static_assert(NP * 64 * NW == kRows * 8 && BM * 8 % (64 * NW) == 0, "whole pieces per thread");
+    constexpr int kBuf = 32 * (32 * JB + 4);
+    static_assert(kBuf * 4 * NW <= kImage * 32, "the wavefronts' exchange areas fit the images");
+    __shared__ u32x4_t lds[2 * kImage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int tr, tj;
+    tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
+    const int r0 = tr * BM, j0 = tj * BN;
+    // thread t takes piece t % 8 of rows t / 8 + i * (threads / 8): BM rows of the input, then BN of the kernels
+    const int q = threadIdx.x & 7, row = threadIdx.x >> 3;
+    const TI *src[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int r = row + i * 8 * NW;
+        src[i] = (i * 8 * NW < BM ? (const TI *)p.in + row_at(r0, r, p.rows) * p.ld_in : (const TI *)p.w + row_at(j0, r - BM, p.Cout) * p.Cin) + q * kPiece;
+    }
+    auto fetch = [&](u32x4_t (&to)[NP], int k) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) to[i] = load16(src[i] + k);
+    };
+    const int xrow = wave / WC * (XB * 32) + (lane & 31), wrow = BM + wave % WC * (JB * 32) + (lane & 31);
+    f32x16_t acc[XB][JB];
+    // the sums of all of k; rough: from rounded upper parts only (fp32)
+    auto sums = [&](auto rough) {
+        constexpr bool kRough = decltype(rough)::value;
+        auto store = [&](const u32x4_t (&from)[NP], u32x4_t *to) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int r = row + i * 8 * NW;
+                if constexpr (sizeof(TI) == 2) {
+                    to[I::at(r, q)] = from[i];
+                } else {
+                    const f32x4_t v = __builtin_bit_cast(f32x4_t, from[i]);
+                    uint2 *at = (uint2 *)(to + I::at(r, q >> 1)) + (q & 1);
+                    if constexpr (kRough) {
+                        at[0] = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+                    } else {
+                        uint2 h, m, l;
+                        split_pair(v[0], v[1], h.x, m.x, l.x);
+                        split_pair(v[2], v[3], h.y, m.y, l.y);
+                        at[0] = h;
+                        at[2 * kPlane] = m;
+                        at[4 * kPlane] = l;
+                    }
+                }
+            }
+        };
+        auto multiply = [&](const u32x4_t *from) {
+            constexpr int NPL = kRough ? 1 : I::kPlanes;
+#pragma unroll
+            for (int s = 0; s < kSub; ++s) {
+                bf16x8 x[NPL][XB], w[NPL][JB];
+#pragma unroll
+                for (int n = 0; n < NPL; ++n) {
+#pragma unroll
+                    for (int i = 0; i < JB; ++i) w[n][i] = __builtin_bit_cast(bf16x8, from[n * kPlane + I::at(wrow + 32 * i, 2 * s + (lane >> 5))]);
+#pragma unroll
+                    for (int i = 0; i < XB; ++i) x[n][i] = __builtin_bit_cast(bf16x8, from[n * kPlane + I::at(xrow + 32 * i, 2 * s + (lane >> 5))]);
+                }
+                // the smallest products first
+#pragma unroll
+                for (int n = NPL - 1; n >= 0; --n)
+#pragma unroll
+                    for (int a = 0; a <= n; ++a)
+#pragma unroll
+                        for (int i = 0; i < XB; ++i)
+#pragma unroll
+                            for (int c = 0; c < JB; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[a][c], x[n - a][i], acc[i][c], 0, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < XB; ++i)
+#pragma unroll
+            for (int c = 0; c < JB; ++c) acc[i][c] = f32x16_t{};
+        // Image s % 2 holds step s, ring entry s % PF what is to become step s; loads behind the last step take it again.
+        const int whole = p.Cin / kStep, tail = p.Cin - whole * kStep;
+        u32x4_t ring[PF][NP];
+#pragma unroll
+        for (int i = 0; i < PF; ++i)
+            if (whole) fetch(ring[i], min(i, whole - 1) * kStep);
+        __syncthreads();
+        if (tail) {     // the part of k behind the last whole step goes first, with zeros behind its end
+            u32x4_t rest[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) rest[i] = load16_tail(src[i] + whole * kStep, tail - q * kPiece);
+            store(rest, lds);
+            __syncthreads();
+            multiply(lds);
+            __syncthreads();
+        }
+        if (whole) {
+            auto step = [&](int s, u32x4_t (&next)[NP]) {
+                store(next, lds + (s + 1) % 2 * kImage);
+                fetch(next, min(s + 1 + PF, whole - 1) * kStep);
+                multiply(lds + s % 2 * kImage);
+                if constexpr (XB * JB > 1) {    // larger tiles: the loads go out between the products, not before them (3 to 6 %)
+                    constexpr int M = XB * JB * kSub * (kRough || sizeof(TI) == 2 ? 1 : 6);
+                    __builtin_amdgcn_sched_group_barrier(0x008, M / 4, 0);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x008, (M / 2 + NP - 1) / NP, 0);
+                    }
+                }
+                __syncthreads();
+            };
+            store(ring[0], lds);
+            fetch(ring[0], min(PF, whole - 1) * kStep);
+            __syncthreads();
+            int s = 0;
+            for (; s + PF < whole; s += PF)
+#pragma unroll
+                for (int u = 0; u < PF; ++u) step(s + u, ring[(u + 1) % PF]);
+#pragma unroll
+            for (int u = 0; u < PF - 1; ++u)
+                if (s + 1 < whole) step(s++, ring[(u + 1) % PF]);
+            multiply(lds + s % 2 * kImage);
+            __syncthreads();
+        }
+    };
+    sums(std::false_type{});
+    if constexpr (sizeof(TI) == 4) {
+        int odd = 0;
+#pragma unroll
+        for (int i = 0; i < XB; ++i)
+#pragma unroll
+            for (int c = 0; c < JB; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) odd |= !__builtin_isfinite(acc[i][c][e]);
+        if (__syncthreads_or(odd)) {
+            f32x16_t fine[XB][JB];
+#pragma unroll
+            for (int i = 0; i < XB; ++i)
+#pragma unroll
+                for (int c = 0; c < JB; ++c) fine[i][c] = acc[i][c];
+            sums(std::true_type{});
+#pragma unroll
+            for (int i = 0; i < XB; ++i)
+#pragma unroll
+                for (int c = 0; c < JB; ++c)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][c][e] = __builtin_isfinite(fine[i][c][e]) ? fine[i][c][e] : acc[i][c][e];
+        }
+    }
+    write_rows<TO, XB, JB>(p, (float *)lds + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
 template <typename TI, typename TO, int RT, int CT, int MAXW> int launch_wave(const LinearArgs &p, int waves)
 {
-    const int tj = (p.Cout - 1) / CT + 1;
-    const long long tiles = (long long)tj * ((p.rows - 1) / RT + 1);
+    const int tr = (p.rows - 1) / RT + 1, tj = (p.Cout - 1) / CT + 1;
     const LaunchScope prof("linear_wave", linear_flops(p), linear_bytes(p));
-    hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW>), dim3((unsigned)std::min<long long>(tiles, 1 << 20)), dim3(64 * std::min(waves, MAXW)), 0,
-                       current_stream(), p, tj, tiles);
+    hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW>), dim3((unsigned)tr * tj), dim3(64 * std::max(1, std::min(waves, MAXW))), 0,
+                       current_stream(), p, tr, tj);
     return check_launch();
 }
 
-template <typename TO, int BM, int BN, int WR, int WC> int launch_tile_bf16(const LinearArgs &p)
+template <typename TO, int BM, int BN, int WR, int WC, int NS> int launch_tile_bf16(const LinearArgs &p)
 {
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
-    const LaunchScope prof("linear_tile", linear_flops(p), linear_bytes(p));
-    hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC>), dim3((unsigned)(tr * tj)), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
+    const LaunchScope prof("linear_tile_bf16", linear_flops(p), linear_bytes(p));
+    hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC, NS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
     return check_launch();
 }
 
+template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF> int launch_tile(const LinearArgs &p)
+{
+    const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
+    const LaunchScope prof("linear_tile", linear_flops(p), linear_bytes(p), (sizeof(TI) == 4 ? 6.0 : 1.0) * linear_flops(p));
+    hipLaunchKernelGGL((linear_tile_kernel<TI, TO, BM, BN, WR, WC, PF>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
+    return check_launch();
+}
+
+// Microseconds of a tiling, from what it measured (products of 128 to 8192 rows, layers and results): `fixed` for filling the
+// pipeline and writing the results, `step` for 128 bytes of k when `slots` workgroups share the chip, `alone` when each
+// has a compute unit to itself.
+struct Tiling { int BM, BN, slots; double fixed, step, alone; };
+double tiling_us(const Tiling &t, const LinearArgs &p, int steps)
+{
+    const long long tiles = (long long)((p.rows - 1) / t.BM + 1) * ((p.Cout - 1) / t.BN + 1);
+    if (tiles <= 256) return t.fixed + t.alone * steps;
+    return (double)((tiles + t.slots - 1) / t.slots) * (t.fixed + t.step * steps);
+}
+template <int n> int cheapest(const Tiling (&t)[n], const LinearArgs &p, int steps)
+{
+    int best = 0;
+    for (int i = 1; i < n; ++i)
+        if (tiling_us(t[i], p, steps) < tiling_us(t[best], p, steps)) best = i;
+    return best;
+}
+
+// Few results: the wavefronts, in blocks of 16 x 16 up to 2^16 results, a short sum or 16 rows, else 32 x 32 (us, 16 / 32: 586 x
+// 1952 x 64 bf16 5.4 / 7.8, 99 x 3088 x 80 7.0 / 10.9; 45 x 1792 x 3520 12.9 / 9.5, 3458 x 2016 x 56 13.1 / 8.2).  Tiles through LDS
+// from as many results on as they need to fill the chip: 2^18 bf16 (us, wavefronts / tiles: 461 x 64 x 2752 7.8 / 3.8, 729 x 1536
+// x 384 14.2 / 10.4; 1959 x 3224 x 72 11.9 / 17.8), 2^17 where rows lie at any address (905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
+// 16.1 / 18.1), 2^20 fp32 (461 x 64 x 2752 8.9 / 6.3, 3506 x 416 x 1096 58 / 27; 409 x 576 x 1184 12.2 / 14.1, 729 x 1536 x 384 26 / 29).
 template <typename TI, typename TO> int by_size(const LinearArgs &p)
 {
-    if constexpr (sizeof(TI) == 2) {
-        const bool direct = p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
-                            p.ld_in < (1 << 22) && p.Cin < (1 << 22);      // a tile's rows within 32-bit offsets
-        if (direct && linear_flops(p) > 4e9) {
-            const long long big = (long long)((p.rows - 1) / 256 + 1) * ((p.Cout - 1) / 256 + 1);
-            if (big >= 200) return launch_tile_bf16<TO, 256, 256, 2, 4>(p);
-            return launch_tile_bf16<TO, 128, 128, 2, 2>(p);
-        }
+    const double results = (double)p.rows * p.Cout;
+    const int steps = (int)(((long long)p.Cin * sizeof(TI) + 127) / 128);
+    // memory-to-LDS loads: whole 16-byte pieces, a tile's rows within 32-bit offsets
+    const bool direct = sizeof(TI) == 2 && p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
+                        p.ld_in < (1 << 22) && p.Cin < (1 << 22);
+    if (p.rows <= 16 || results <= 65536 || steps <= 2) {
+        if (p.rows <= 16 || results < (direct ? 1 << 18 : sizeof(TI) == 2 ? 1 << 17 : 1 << 20)) return launch_wave<TI, TO, 16, 16, 16>(p, 2 * steps);
+    } else if (results < (direct ? 1 << 18 : sizeof(TI) == 2 ? 1 << 17 : 1 << 20)) {
+        return launch_wave<TI, TO, 32, 32, 8>(p, steps);
     }
-    const int steps = (int)(p.Cin * sizeof(TI) / 64) + 1;
-    if (p.rows <= 16) return launch_wave<TI, TO, 16, 16, 16>(p, std::max(1, steps));
-    const long long t64 = (long long)((p.rows - 1) / 64 + 1) * ((p.Cout - 1) / 64 + 1);
-    if (t64 >= 200) return launch_wave<TI, TO, 64, 64, 8>(p, std::max(1, steps / 4));
-    return launch_wave<TI, TO, 32, 32, 8>(p, std::max(1, steps / 2));
+    if constexpr (sizeof(TI) == 4) {
+        static const Tiling kF32[] = {{64, 64, 768, 2.0, 1.25, 0.6}, {128, 128, 256, 3.0, 1.36, 1.2}, {256, 128, 256, 5.0, 2.45, 2.1}};
+        switch (cheapest(kF32, p, steps)) {
+            case 0: return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
+            case 1: return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
+            default: return launch_tile<TI, TO, 256, 128, 4, 2, 1>(p);
+        }
+    } else if (direct) {
+        static const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29}, {128, 128, 256, 2.5, 0.57, 0.5}, {128, 128, 512, 4.4, 1.0, 0.75}, {256, 256, 256, 9.0, 1.5, 1.25}};
+        switch (cheapest(kDirect, p, steps)) {
+            case 0: return launch_tile_bf16<TO, 64, 64, 2, 2, 4>(p);
+            case 1: return launch_tile_bf16<TO, 128, 128, 2, 4, 4>(p);
+            case 2: return launch_tile_bf16<TO, 128, 128, 2, 2, 2>(p);
+            default: return launch_tile_bf16<TO, 256, 256, 2, 4, 2>(p);
+        }
+    } else {
+        static const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45}, {128, 128, 512, 4.0, 1.8, 0.85}};
+        if (cheapest(kAny, p, steps) == 0) return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
+        return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
+    }
 }
 
 }  // namespace

@@ -239,7 +239,9 @@ def test_linear_shapes(sq, rows, cin, cout, ti, to):
 
 # enough work for the tiles through LDS: whole and part steps of k, ragged edges both ways, one tile row or column
 LINEAR_LARGE = [(1024, 2048, 1024), (2100, 1032, 1000), (3601, 328, 3584), (13000, 200, 1000), (129, 4096, 4104), (9000, 2056, 130),
-                (2187, 1000, 1001), (4100, 777, 1030)]
+                (2187, 1000, 1001), (4100, 777, 1030), (5400, 520, 2048), (6100, 72, 1801), (905, 193, 704), (1100, 33, 520), (905, 200, 704),
+                (700, 72, 600), (300, 1536, 200), (150, 2048, 500), (257, 1000, 333), (600, 40, 520), (600, 8, 520), (2100, 31, 600),
+                (1500, 64, 700), (1500, 128, 700), (1500, 96, 1032), (1200, 256, 1024)]
 
 
 @pytest.mark.parametrize("ti,to", TYPES)
