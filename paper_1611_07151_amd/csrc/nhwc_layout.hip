@@ -1,4 +1,5 @@
-// NCHW maps to channels-last rows and back: a transposition of each image's [C][HW] matrix with a conversion on the way.
+// NCHW maps to channels-last rows and back: a transposition of each image's [layers][pixels] matrix with a conversion on the
+// way.  Bound by memory.
 #include "nhwc_common.h"
 
 #include <algorithm>
@@ -6,57 +7,114 @@
 namespace sq {
 namespace {
 
-constexpr int kTile = 64;
+// Per image a matrix of `rows` rows of `cols` values (dense within a row, ld_in from row to row) becomes one of `cols` rows.
+struct TransposeArgs {
+    const void *in;
+    void *out;
+    long long rows, cols, ld_in, img_in, ld_out, img_out;
+    long long tiles_r, tiles_c;     // per image
+};
 
-// n matrices [rows][cols] (row stride ld_in, matrix stride img_in) -> [cols][rows] (ld_out, img_out).
-template <typename TI, typename TO>
-__global__ __launch_bounds__(256) void transpose_kernel(const TI *in, TO *out, long long rows, long long cols, long long ld_in,
-                                                        long long img_in, long long ld_out, long long img_out,
-                                                        long long tiles_r, long long tiles_c, long long tiles)
+template <typename T> constexpr int kPer = 16 / (int)sizeof(T);
+
+// 16 bytes of a row at any address, of which `have` values exist
+template <typename T> __device__ __forceinline__ void load_piece(const T *p, long long have, float (&v)[kPer<T>])
 {
-    __shared__ float tile[kTile][kTile + 1];
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const long long c0 = t % tiles_c * kTile, q = t / tiles_c;
-        const long long r0 = q % tiles_r * kTile, n = q / tiles_r;
-        const TI *src = in + n * img_in;
-        TO *dst = out + n * img_out;
-        for (int i = ty; i < kTile; i += 4)
-            if (r0 + i < rows && c0 + tx < cols) tile[i][tx] = to_f32(src[(r0 + i) * ld_in + c0 + tx]);
-        __syncthreads();
-        for (int i = ty; i < kTile; i += 4)
-            if (c0 + i < cols && r0 + tx < rows) dst[(c0 + i) * ld_out + r0 + tx] = from_f32<TO>(tile[tx][i]);
-        __syncthreads();
+    T raw[kPer<T>];
+    if (have >= kPer<T>) {
+        __builtin_memcpy(raw, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer<T>; ++i) raw[i] = i < have ? p[i] : T(0);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer<T>; ++i) v[i] = to_f32(raw[i]);
+}
+template <typename T> __device__ __forceinline__ void store_piece(T *p, long long have, const float (&v)[kPer<T>])
+{
+    T raw[kPer<T>];
+#pragma unroll
+    for (int i = 0; i < kPer<T>; ++i) raw[i] = from_f32<T>(v[i]);
+    if (have >= kPer<T>) {
+        __builtin_memcpy(p, raw, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer<T>; ++i)
+            if (i < have) p[i] = raw[i];
     }
 }
 
-template <typename TI, typename TO>
-int transpose(const char *name, const void *in, void *out, int N, long long rows, long long cols, long long ld_in, long long img_in,
-              long long ld_out, long long img_out)
+// R x C values per workgroup of 256 threads through LDS as fp32.  Both sides move 16 bytes a lane, along the rows of the input
+// and along the rows of the output.
+template <typename TI, typename TO, int R, int C> __global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs p)
 {
-    const long long tr = (rows + kTile - 1) / kTile, tc = (cols + kTile - 1) / kTile, tiles = tr * tc * N;
-    const LaunchScope prof(name, 0.0, (double)N * rows * cols * (sizeof(TI) + sizeof(TO)), 0.0);
-    hipLaunchKernelGGL((transpose_kernel<TI, TO>), dim3((unsigned)std::min<long long>(tiles, 1 << 20)), dim3(256), 0, current_stream(),
-                       (const TI *)in, (TO *)out, rows, cols, ld_in, img_in, ld_out, img_out, tr, tc, tiles);
+    constexpr int ni = kPer<TI>, no = kPer<TO>, kPitch = C + 1;
+    constexpr int LI = C / ni, LO = R / no;      // lanes along a row
+    constexpr int KI = R * LI / 256, KO = C * LO / 256;
+    static_assert(KI * 256 == R * LI && KO * 256 == C * LO, "whole turns");
+    __shared__ float tile[R * kPitch];
+    const unsigned t = blockIdx.x, per = (unsigned)(p.tiles_r * p.tiles_c), in_image = t % per;
+    const long long n = t / per, c0 = (long long)(in_image % (unsigned)p.tiles_c) * C, r0 = (long long)(in_image / (unsigned)p.tiles_c) * R;
+    const TI *in = (const TI *)p.in + n * p.img_in;
+    TO *out = (TO *)p.out + n * p.img_out;
+    {
+        const int c = threadIdx.x % LI * ni, r = threadIdx.x / LI;
+        float v[KI][ni];
+#pragma unroll
+        for (int k = 0; k < KI; ++k) {
+            const long long row = r0 + r + k * (256 / LI);
+            if (row < p.rows && c0 + c < p.cols) load_piece(in + row * p.ld_in + c0 + c, p.cols - c0 - c, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < KI; ++k)
+#pragma unroll
+            for (int i = 0; i < ni; ++i) tile[(r + k * (256 / LI)) * kPitch + c + i] = v[k][i];
+    }
+    __syncthreads();
+    const int r = threadIdx.x % LO * no, c = threadIdx.x / LO;
+#pragma unroll
+    for (int k = 0; k < KO; ++k) {
+        const long long row = c0 + c + k * (256 / LO);
+        if (row >= p.cols || r0 + r >= p.rows) continue;
+        float v[no];
+#pragma unroll
+        for (int i = 0; i < no; ++i) v[i] = tile[(r + i) * kPitch + c + k * (256 / LO)];
+        store_piece(out + row * p.ld_out + r0 + r, p.rows - r0 - r, v);
+    }
+}
+
+template <typename TI, typename TO, int R, int C> int launch(const char *name, TransposeArgs p, int N)
+{
+    p.tiles_r = (p.rows + R - 1) / R;
+    p.tiles_c = (p.cols + C - 1) / C;
+    const long long tiles = p.tiles_r * p.tiles_c * N;
+    if (tiles > 0xffffffffll / 256) return SQ_ERR_UNSUPPORTED;
+    const LaunchScope prof(name, 0.0, (double)N * p.rows * p.cols * (sizeof(TI) + sizeof(TO)), 0.0);
+    hipLaunchKernelGGL((transpose_kernel<TI, TO, R, C>), dim3((unsigned)tiles), dim3(256), 0, current_stream(), p);
     return check_launch();
 }
 
-template <typename... A> int by_types(int ti, int to, A... a)
+template <typename TI, typename TO> int transpose(const char *name, const TransposeArgs &p, int N)
 {
-    if (ti == SQ_F32) return to == SQ_F32 ? transpose<float, float>(a...) : transpose<float, bf16_t>(a...);
-    return to == SQ_F32 ? transpose<bf16_t, float>(a...) : transpose<bf16_t, bf16_t>(a...);
+    return launch<TI, TO, 64, 64>(name, p, N);
+}
+
+int by_types(int ti, int to, const char *name, const TransposeArgs &p, int N)
+{
+    if (ti == SQ_F32) return to == SQ_F32 ? transpose<float, float>(name, p, N) : transpose<float, bf16_t>(name, p, N);
+    return to == SQ_F32 ? transpose<bf16_t, float>(name, p, N) : transpose<bf16_t, bf16_t>(name, p, N);
 }
 
 }  // namespace
 
 int nhwc_pack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld)
 {
-    return by_types(in_dtype, out_dtype, "nhwc_pack", in, out, N, (long long)C, HW, HW, C * HW, ld, HW * ld);
+    return by_types(in_dtype, out_dtype, "nhwc_pack", TransposeArgs{in, out, C, HW, HW, C * HW, ld, HW * ld, 0, 0}, N);
 }
 
 int nhwc_unpack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld, int out_channels)
 {
-    return by_types(in_dtype, out_dtype, "nhwc_unpack", in, out, N, HW, (long long)C, ld, HW * ld, HW, out_channels * HW);
+    return by_types(in_dtype, out_dtype, "nhwc_unpack", TransposeArgs{in, out, HW, C, ld, HW * ld, HW, out_channels * HW, 0, 0}, N);
 }
 
 }  // namespace sq

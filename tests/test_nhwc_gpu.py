@@ -143,7 +143,10 @@ def norm_case(sq, n, h, w, c, groups, act, dt, seed, left=0, right=0, affine=Tru
 
 NORM_SHAPES = [(1, 1, 1, 8, 2), (2, 1, 1, 1, 1), (1, 1, 3, 6, 3), (3, 5, 7, 12, 4), (1, 13, 13, 512, 32), (2, 13, 13, 96, 8),
                (2, 27, 27, 64, 16), (1, 27, 27, 96, 1), (4, 9, 11, 40, 40), (1, 55, 55, 32, 2), (2, 31, 33, 150, 6), (1, 111, 111, 16, 8),
-               (3, 7, 7, 1000, 8), (1, 64, 64, 320, 32), (65, 3, 3, 24, 3), (1, 1, 1, 4096, 1), (1, 200, 130, 8, 1), (2, 16, 16, 7, 7)]
+               (3, 7, 7, 1000, 8), (1, 64, 64, 320, 32), (65, 3, 3, 24, 3), (1, 1, 1, 4096, 1), (1, 200, 130, 8, 1), (2, 16, 16, 7, 7),
+               # more than a workgroup keeps: chunks; groups wider than a workgroup; widths that leave vectors of every size
+               (1, 40, 40, 4096, 1), (2, 300, 300, 24, 2), (1, 500, 501, 8, 2), (1, 150, 150, 6, 2), (3, 64, 64, 999, 3), (1, 9, 9, 5000, 2),
+               (1, 260, 260, 12, 1), (2, 170, 170, 30, 1), (1, 130, 130, 320, 32), (5, 53, 57, 150, 6), (2, 111, 111, 96, 8), (1, 20, 20, 9999, 1)]
 
 
 @pytest.mark.parametrize("dt", (F32, BF16))
