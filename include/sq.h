@@ -494,7 +494,8 @@ int sq_squeezenet_forward_bf16(const void *in, sq_dtype in_dtype, const void *co
  *   act: one of the codes below; anything else SQ_ERR_UNSUPPORTED.
  *   Every pointer must be aligned to the size of its values (else SQ_ERR_UNSUPPORTED); rows whose
  *     address and ld are multiples of 16 bytes are read and written fastest.
- *   Sizes: offsets are 64-bit; there is no limit but memory.
+ *   Sizes: offsets are 64-bit.  A call that would need 2^32 threads or more in one launch (tens of
+ *     billions of values) returns SQ_ERR_UNSUPPORTED.
  *   The arithmetic mode of sq_set_dtype() does not matter to these calls.
  */
 enum {
@@ -553,17 +554,16 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
  *     ld_out values; both of out_dtype: SQ_F32 with SQ_F32 inputs, either with SQ_BF16 inputs
  *     (otherwise SQ_ERR_UNSUPPORTED).  residual may be out itself with the same ld; apart from that
  *     out must not overlap any input.
- *   workspace: device scratch, 256-byte aligned (else SQ_ERR_WORKSPACE), or NULL.  With at least
- *     sq_linear_workspace_bytes(in_dtype, rows, Cin, Cout) bytes a long sum with few results is split
- *     over more of the chip; less only rules that out (the result is the same up to rounding).
- *     Contents on return are unspecified; two calls in flight at once need two.
- *   The same call gives the same bits every time.
- * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP.
+ *   fp32: from about a million results on, the products run on the bfloat16 matrix instructions with
+ *     each operand as the exact sum of three bfloat16 values and fp32 sums: the error stays that of fp32
+ *     sums of the same terms, except that operands below 2^-110 in magnitude keep fewer bits.  An
+ *     infinity or NaN reaches the results of its row or kernel and no others.
+ *   The call needs no scratch.  The same call gives the same bits every time.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_HIP.
  */
-size_t sq_linear_workspace_bytes(sq_dtype in_dtype, int rows, int Cin, int Cout);
 int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out,
                       sq_dtype in_dtype, sq_dtype out_dtype, int rows, int Cin, int Cout, int act,
-                      int ld_in, int ld_res, int ld_out, void *workspace, size_t workspace_bytes);
+                      int ld_in, int ld_res, int ld_out);
 
 /*
  * Per-launch timing, off by default.  Between sq_profile_begin() and sq_profile_end()

@@ -94,9 +94,7 @@ lib.sq_nhwc_unpack.argtypes = [_vp, _i, _vp, _i] + [_i] * 7
 lib.sq_nhwc_group_norm_workspace_bytes.restype = _sz
 lib.sq_nhwc_group_norm_workspace_bytes.argtypes = [_i] * 5
 lib.sq_nhwc_group_norm.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 5 + [ctypes.c_float] + [_i] * 3 + [_vp, _sz]
-lib.sq_linear_workspace_bytes.restype = _sz
-lib.sq_linear_workspace_bytes.argtypes = [_i] * 4
-lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9 + [_vp, _sz]
+lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9
 
 lib.sq_profile_begin.argtypes = [_i]
 lib.sq_profile_get_mfma_flops.argtypes = [_i, ctypes.POINTER(ctypes.c_double)]
@@ -714,12 +712,20 @@ def sq_squeezenet_forward_bf16(x, params, packed, workspace=None, probs=None, wa
 # a contiguous tensor, or a slice of the last dimension of one.  All tensors of a call live on one GPU, which need
 # not be the current one; the call runs on that GPU's current stream.
 _MAX_INT = 2**31 - 1
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _rows_of(t, name):
-    """Values from one row to the next."""
-    if not t.is_cuda:
+def _gpu_of(x, name):
+    index = x.get_device()
+    if index < 0:
         raise ValueError(f"{name} must live on the GPU")
+    return index
+
+
+def _rows_of(t, name, index):
+    """Values from one row to the next of a tensor on GPU `index`."""
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on GPU {index}")
     shape = t.shape
     if len(shape) < 2:
         raise ValueError(f"{name} must have at least two dimensions")
@@ -746,41 +752,50 @@ def _rows_of(t, name):
     return ld
 
 
-def _same_device(x, *others):
-    for t, name in others:
-        if t is not None and t.device != x.device:
-            raise ValueError(f"{name} must live on {x.device}")
+def _dense(t, name, index, dtype):
+    """Address of a contiguous tensor on GPU `index`, or None."""
+    if t is None:
+        return None
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on GPU {index}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _run(x, what, fn, *args):
-    index = x.device.index
+def _run(index, what, fn, *args):
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
-            _use_current_stream()
+            lib.sq_set_stream(_raw_stream(index))
             rc = fn(*args)
     else:
-        _use_current_stream()
+        lib.sq_set_stream(_raw_stream(index))
         rc = fn(*args)
-    _check(rc, what)
+    if rc:
+        _check(rc, what)
 
 
-def _scratch(workspace, need, x):
+def _scratch(workspace, need, x, index):
+    """The workspace (held by the caller until the launch is made), its address and size."""
     if workspace is None:
-        return (None, 0) if need == 0 else _scratch(torch.empty(need, device=x.device, dtype=torch.uint8), need, x)
-    return workspace, workspace.numel() * workspace.element_size()
+        if not need:
+            return None, None, 0
+        workspace = torch.empty(need, device=x.device, dtype=torch.uint8)
+    return workspace, _dense(workspace, "workspace", index, workspace.dtype), workspace.numel() * workspace.element_size()
 
 
 def sq_nhwc_pack(x, dtype=None, out=None):
     """NCHW float32 / bfloat16 -> channels-last map [N][H][W][C] of `dtype` (default: that of x or of out)."""
     N, C, H, W = x.shape
+    index = _gpu_of(x, "x")
     if out is None:
         out = torch.empty((N, H, W, C), device=x.device, dtype=dtype or x.dtype)
     elif tuple(out.shape) != (N, H, W, C) or dtype not in (None, out.dtype):
         raise ValueError("out has the wrong shape or type")
-    _same_device(x, (out, "out"))
-    ld = _rows_of(out, "out")
-    _run(x, "sq_nhwc_pack", lib.sq_nhwc_pack, _dev(x, None, "x"), _dtype_code(x, "x"), out.data_ptr(), _dtype_code(out, "out"),
-         N, C, H, W, ld)
+    _run(index, "sq_nhwc_pack", lib.sq_nhwc_pack, _dense(x, "x", index, x.dtype), _dtype_code(x, "x"), out.data_ptr(),
+         _dtype_code(out, "out"), N, C, H, W, _rows_of(out, "out", index))
     return out
 
 
@@ -788,13 +803,13 @@ def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
     """Channels-last map [N][H][W][C] -> NCHW of `dtype`.  `out` may be a larger [N][C'][H][W] tensor; the result lands in
     layers [c_offset, c_offset + C) and its type is that of out."""
     N, H, W, C = m.shape
+    index = _gpu_of(m, "m")
     if out is None:
         out = torch.empty((N, C + c_offset, H, W), device=m.device, dtype=dtype)
     if out.dim() != 4 or (out.shape[0], out.shape[2], out.shape[3]) != (N, H, W):
         raise ValueError("out has the wrong shape")
-    _same_device(m, (out, "out"))
-    _run(m, "sq_nhwc_unpack", lib.sq_nhwc_unpack, m.data_ptr(), _dtype_code(m, "m"), _dev(out, None, "out"),
-         _dtype_code(out, "out"), N, C, H, W, _rows_of(m, "m"), out.shape[1], int(c_offset))
+    _run(index, "sq_nhwc_unpack", lib.sq_nhwc_unpack, m.data_ptr(), _dtype_code(m, "m"), _dense(out, "out", index, out.dtype),
+         _dtype_code(out, "out"), N, C, H, W, _rows_of(m, "m", index), out.shape[1], int(c_offset))
     return out
 
 
@@ -806,6 +821,7 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
     """Group norm with an activation on a channels-last map [N][H][W][C] (float32 or bfloat16); gamma, beta [C] float32 or
     None.  `out` may be m itself."""
     N, H, W, C = m.shape
+    index = _gpu_of(m, "m")
     if out is None:
         out = torch.empty((N, H, W, C), device=m.device, dtype=m.dtype)
     elif out.shape != m.shape or out.dtype != m.dtype:
@@ -813,49 +829,42 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
     for t, name in ((gamma, "gamma"), (beta, "beta")):
         if t is not None and t.numel() != C:
             raise ValueError(f"{name} must have one value per layer")
-    _same_device(m, (out, "out"), (gamma, "gamma"), (beta, "beta"), (workspace, "workspace"))
-    ld_in, ld_out = _rows_of(m, "m"), _rows_of(out, "out")
-    workspace, nbytes = _scratch(workspace, lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, int(groups)), m)
-    _run(m, "sq_nhwc_group_norm", lib.sq_nhwc_group_norm, m.data_ptr(), out.data_ptr(), _dtype_code(m, "m"),
-         _dev(gamma, torch.float32, "gamma"), _dev(beta, torch.float32, "beta"), N, C, H, W, int(groups), float(eps), int(act),
-         ld_in, ld_out, _dev(workspace), nbytes)
+    ld_in, ld_out, groups = _rows_of(m, "m", index), _rows_of(out, "out", index), int(groups)
+    workspace, address, nbytes = _scratch(workspace, lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups), m, index)
+    _run(index, "sq_nhwc_group_norm", lib.sq_nhwc_group_norm, m.data_ptr(), out.data_ptr(), _dtype_code(m, "m"),
+         _dense(gamma, "gamma", index, torch.float32), _dense(beta, "beta", index, torch.float32), N, C, H, W, groups, eps,
+         int(act), ld_in, ld_out, address, nbytes)
     return out
 
 
-def sq_linear_workspace_bytes(dtype, rows, Cin, Cout) -> int:
-    """dtype: SQ_F32 or SQ_BF16, the type of the inputs."""
-    return int(lib.sq_linear_workspace_bytes(dtype, rows, Cin, Cout))
-
-
-def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None, workspace=None):
+def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None):
     """act(x @ w.T + b) + residual.  x [..., Cin] and w [Cout][Cin] (a 1x1 convolution's [Cout][Cin][1][1] too), float32 or
     both bfloat16; b [Cout] float32 or None; out and residual [..., Cout] of out_dtype (default: that of x, residual or
     out).  `residual` may be `out` itself."""
-    if w.dim() not in (2, 4) or w.dim() == 4 and tuple(w.shape[2:]) != (1, 1) or x.shape[-1] != w.shape[1]:
+    index = _gpu_of(x, "x")
+    kernels = w.shape
+    if len(kernels) not in (2, 4) or len(kernels) == 4 and tuple(kernels[2:]) != (1, 1) or x.shape[-1] != kernels[1]:
         raise ValueError("kernel shape does not match the input")
-    if x.dtype != w.dtype:
-        raise ValueError("x and w must both be float32 or both bfloat16")
-    Cout, Cin = w.shape[0], w.shape[1]
+    Cout, Cin = kernels[0], kernels[1]
     shape = x.shape[:-1] + (Cout,)
     if out is None:
         out = torch.empty(shape, device=x.device, dtype=out_dtype or (x.dtype if residual is None else residual.dtype))
     elif out.shape != shape or out_dtype not in (None, out.dtype):
         raise ValueError("out has the wrong shape or type")
-    if residual is not None and (residual.shape != shape or residual.dtype != out.dtype):
-        raise ValueError("residual must have the shape and type of the result")
+    ld_res, res = 0, None
+    if residual is not None:
+        if residual.shape != shape or residual.dtype != out.dtype:
+            raise ValueError("residual must have the shape and type of the result")
+        ld_res, res = _rows_of(residual, "residual", index), residual.data_ptr()
     if b is not None and b.numel() != Cout:
         raise ValueError("b must have one value per output layer")
-    _same_device(x, (w, "w"), (b, "b"), (residual, "residual"), (out, "out"), (workspace, "workspace"))
-    ld_in, ld_out = _rows_of(x, "x"), _rows_of(out, "out")
-    ld_res = 0 if residual is None else _rows_of(residual, "residual")
+    ld_in, ld_out = _rows_of(x, "x", index), _rows_of(out, "out", index)
     rows = x.numel() // Cin if Cin else 0
-    if rows > _MAX_INT or max(Cin, Cout) > _MAX_INT:
+    if rows > _MAX_INT or Cin > _MAX_INT or Cout > _MAX_INT:
         _check(-3, "sq_linear_forward")
-    code = _dtype_code(x, "x")
-    workspace, nbytes = _scratch(workspace, lib.sq_linear_workspace_bytes(code, rows, Cin, Cout), x)
-    _run(x, "sq_linear_forward", lib.sq_linear_forward, x.data_ptr(), _dev(w, None, "w"), _dev(b, torch.float32, "b"),
-         None if residual is None else residual.data_ptr(), out.data_ptr(), code, _dtype_code(out, "out"), rows, Cin, Cout,
-         int(act), ld_in, ld_res, ld_out, _dev(workspace), nbytes)
+    _run(index, "sq_linear_forward", lib.sq_linear_forward, x.data_ptr(), _dense(w, "w", index, x.dtype),
+         _dense(b, "b", index, torch.float32), res, out.data_ptr(), _dtype_code(x, "x"), _dtype_code(out, "out"), rows, Cin, Cout,
+         int(act), ld_in, ld_res, ld_out)
     return out
 
 

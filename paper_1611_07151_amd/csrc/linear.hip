@@ -579,6 +579,7 @@ __global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, 
 template <typename TI, typename TO, int RT, int CT, int MAXW> int launch_wave(const LinearArgs &p, int waves)
 {
     const int tr = (p.rows - 1) / RT + 1, tj = (p.Cout - 1) / CT + 1;
+    if (!one_launch((double)tr * tj, 64 * MAXW)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_wave", linear_flops(p), linear_bytes(p));
     hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW>), dim3((unsigned)tr * tj), dim3(64 * std::max(1, std::min(waves, MAXW))), 0,
                        current_stream(), p, tr, tj);
@@ -588,6 +589,7 @@ template <typename TI, typename TO, int RT, int CT, int MAXW> int launch_wave(co
 template <typename TO, int BM, int BN, int WR, int WC, int NS> int launch_tile_bf16(const LinearArgs &p)
 {
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
+    if (!one_launch((double)tr * tj, 64 * WR * WC)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_tile_bf16", linear_flops(p), linear_bytes(p));
     hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC, NS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
     return check_launch();
@@ -596,6 +598,7 @@ template <typename TO, int BM, int BN, int WR, int WC, int NS> int launch_tile_b
 template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF> int launch_tile(const LinearArgs &p)
 {
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
+    if (!one_launch((double)tr * tj, 64 * WR * WC)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_tile", linear_flops(p), linear_bytes(p), (sizeof(TI) == 4 ? 6.0 : 1.0) * linear_flops(p));
     hipLaunchKernelGGL((linear_tile_kernel<TI, TO, BM, BN, WR, WC, PF>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
     return check_launch();
@@ -659,8 +662,6 @@ template <typename TI, typename TO> int by_size(const LinearArgs &p)
 }
 
 }  // namespace
-
-size_t linear_workspace_bytes(int, int, int, int) { return 0; }
 
 int linear(const LinearArgs &p)
 {

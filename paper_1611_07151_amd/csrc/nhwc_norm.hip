@@ -568,6 +568,7 @@ Plan make_plan(int N, int C, long long HW, int G, int size)
 template <typename T, int VB, int KEEP> int launch_fused(const NormArgs &p, const Plan &q)
 {
     const double values = (double)p.N * p.HW * p.C;
+    if (!one_launch((double)p.N * q.blocks, q.threads)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("group_norm", 10.0 * values, 2.0 * sizeof(T) * values, 0.0);
     hipLaunchKernelGGL((group_norm_fused<T, VB, KEEP / VB>), dim3((unsigned)p.N * q.blocks), dim3(q.threads), 0, current_stream(), p);
     return check_launch();
@@ -584,6 +585,7 @@ template <typename T, int VB> int launch(const NormArgs &p, const Plan &q)
             return launch_fused<T, VB, keep_most(VB)>(p, q);
         }
         const double values = (double)p.N * p.HW * p.C;
+        if (!one_launch((double)p.N * q.blocks * q.chunks, 256)) return SQ_ERR_UNSUPPORTED;
         const unsigned grid = (unsigned)p.N * q.blocks * q.chunks;
         {
             const LaunchScope prof("group_norm_moments", 4.0 * values, sizeof(T) * values, 0.0);

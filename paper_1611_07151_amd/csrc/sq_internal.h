@@ -203,6 +203,8 @@ int avgpool_global(const float *in, float *out, int N, int C, int H, int W);
 int softmax(const float *in, float *out, int N, int C);
 
 // Channels-last maps: [N][HW] rows of ld values, the first C of them the operator's (nhwc_layout.hip, nhwc_norm.hip).
+// Whether `blocks` workgroups of `threads` fit one launch (the runtime counts the threads of a grid in 32 bits).
+inline bool one_launch(double blocks, int threads) { return blocks * threads < 4294967296.0; }
 int nhwc_pack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld);
 int nhwc_unpack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld, int out_channels);
 size_t nhwc_group_norm_workspace_bytes(int N, int C, long long HW, int G);
@@ -217,8 +219,6 @@ struct LinearArgs {
     int in_dtype, out_dtype;      // of in and w; of residual and out
     int rows, Cin, Cout, act;
     long long ld_in, ld_res, ld_out;
-    void *ws;
-    size_t ws_bytes;
 };
 inline double linear_flops(const LinearArgs &a) { return 2.0 * a.rows * a.Cin * a.Cout; }
 inline double linear_bytes(const LinearArgs &a)
@@ -226,7 +226,6 @@ inline double linear_bytes(const LinearArgs &a)
     const double si = a.in_dtype == SQ_BF16 ? 2.0 : 4.0, so = a.out_dtype == SQ_BF16 ? 2.0 : 4.0;
     return si * ((double)a.rows * a.Cin + (double)a.Cout * a.Cin) + so * (double)a.rows * a.Cout * (a.residual ? 2 : 1) + 4.0 * a.Cout;
 }
-size_t linear_workspace_bytes(int in_dtype, int rows, int Cin, int Cout);
 int linear(const LinearArgs &a);
 
 // Optional per-launch timing (sq_profile_begin/end).  A LaunchScope brackets one kernel

@@ -19,7 +19,6 @@ def lib():
     i, vp = ctypes.c_int, ctypes.c_void_p
     l.sq_nhwc_group_norm.argtypes = [vp, vp, i, vp, vp] + [i] * 5 + [ctypes.c_float] + [i] * 3 + [vp, SZ]
     l.sq_nhwc_group_norm_workspace_bytes.restype = SZ
-    l.sq_linear_workspace_bytes.restype = SZ
     return l
 
 
@@ -62,16 +61,16 @@ def test_group_norm(lib):
 
 
 def test_linear(lib):
-    def f(inp=P, w=P, b=P, res=P, out=P, ti=0, to=0, rows=8, cin=16, cout=24, act=0, ldi=16, ldr=24, ldo=24, ws=NULL, nb=0):
-        return lib.sq_linear_forward(inp, w, b, res, out, ti, to, rows, cin, cout, act, ldi, ldr, ldo, ws, SZ(nb))
+    def f(inp=P, w=P, b=P, res=P, out=P, ti=0, to=0, rows=8, cin=16, cout=24, act=0, ldi=16, ldr=24, ldo=24):
+        return lib.sq_linear_forward(inp, w, b, res, out, ti, to, rows, cin, cout, act, ldi, ldr, ldo)
     assert f(inp=NULL) == -1 and f(w=NULL) == -1 and f(out=NULL) == -1
     for k in ("rows", "cin", "cout"):
         assert f(**{k: 0}) == -2 and f(**{k: -1}) == -2
     assert f(ldi=15) == -2 and f(ldr=23) == -2 and f(ldo=23) == -2
     assert f(ti=2) == -3 and f(to=2) == -3 and f(ti=0, to=1) == -3 and f(act=4) == -3 and f(act=-1) == -3
     assert f(inp=ODD) == -3 and f(w=ODD) == -3 and f(b=ODD) == -3 and f(res=ODD) == -3 and f(out=ctypes.c_void_p(0x1002)) == -3
-    assert f(ws=ctypes.c_void_p(0x1010), nb=1 << 20) == -4
-    assert lib.sq_linear_workspace_bytes(2, 8, 16, 24) == 0 and lib.sq_linear_workspace_bytes(0, 0, 16, 24) == 0
+    # more threads than a launch has
+    assert f(rows=2**31 - 1, cin=1, cout=2**31 - 1, ldi=1, ldr=2**31 - 1, ldo=2**31 - 1) == -3
 
 
 def test_the_binding_checks_its_tensors():
@@ -108,7 +107,8 @@ def test_the_binding_checks_its_tensors():
 
 class _OnGpu:
     """Shape and strides of a tensor, as the row check sees one on the GPU."""
-    is_cuda = True
+    def get_device(self):
+        return 0
 
     def __init__(self, t):
         self.shape, self.stride, self.is_contiguous = t.shape, t.stride, t.is_contiguous
@@ -116,7 +116,7 @@ class _OnGpu:
 
 def test_which_tensors_are_rows():
     from paper_1611_07151_amd.binding import SqError, _rows_of
-    ok = lambda t: _rows_of(_OnGpu(t), "t")
+    ok = lambda t: _rows_of(_OnGpu(t), "t", 0)
     t = torch.zeros((2, 3, 5, 16))
     assert ok(t) == 16 and ok(t[..., 4:12]) == 16 and ok(t[:1]) == 16
     assert ok(t[0, 0, :1, :7]) == 7                       # a single row has no stride
