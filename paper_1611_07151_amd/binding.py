@@ -504,12 +504,14 @@ def sq_squeezenet_forward_packed(x, params, packed, workspace=None, probs=None, 
     return (probs, taps) if want_taps else probs
 
 
+_CODES = {torch.float32: SQ_F32, torch.bfloat16: SQ_BF16}
+
+
 def _dtype_code(t, name):
-    if t.dtype == torch.float32:
-        return SQ_F32
-    if t.dtype == torch.bfloat16:
-        return SQ_BF16
-    raise ValueError(f"{name} must be float32 or bfloat16")
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32 or bfloat16")
+    return code
 
 
 def sq_blocked_map_bytes(N, C, H, W) -> int:
@@ -747,7 +749,7 @@ def _rows_of(t, name, index):
         ld = length if ld is None else ld
         if (stride[-1] != 1 and length > 1) or ld < length:
             raise ValueError(f"{name} must be contiguous or a slice of the last dimension of a contiguous tensor")
-    if ld > _MAX_INT or max(shape) > _MAX_INT:
+    if ld > _MAX_INT or t.numel() > _MAX_INT and max(shape) > _MAX_INT:
         _check(-3, name)
     return ld
 
@@ -791,11 +793,13 @@ def sq_nhwc_pack(x, dtype=None, out=None):
     N, C, H, W = x.shape
     index = _gpu_of(x, "x")
     if out is None:
-        out = torch.empty((N, H, W, C), device=x.device, dtype=dtype or x.dtype)
-    elif tuple(out.shape) != (N, H, W, C) or dtype not in (None, out.dtype):
-        raise ValueError("out has the wrong shape or type")
+        out, ld = x.new_empty((N, H, W, C), dtype=dtype or x.dtype), C
+    else:
+        if tuple(out.shape) != (N, H, W, C) or dtype not in (None, out.dtype):
+            raise ValueError("out has the wrong shape or type")
+        ld = _rows_of(out, "out", index)
     _run(index, "sq_nhwc_pack", lib.sq_nhwc_pack, _dense(x, "x", index, x.dtype), _dtype_code(x, "x"), out.data_ptr(),
-         _dtype_code(out, "out"), N, C, H, W, _rows_of(out, "out", index))
+         _dtype_code(out, "out"), N, C, H, W, ld)
     return out
 
 
@@ -803,13 +807,16 @@ def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
     """Channels-last map [N][H][W][C] -> NCHW of `dtype`.  `out` may be a larger [N][C'][H][W] tensor; the result lands in
     layers [c_offset, c_offset + C) and its type is that of out."""
     N, H, W, C = m.shape
-    index = _gpu_of(m, "m")
+    index, c_offset = _gpu_of(m, "m"), int(c_offset)
     if out is None:
-        out = torch.empty((N, C + c_offset, H, W), device=m.device, dtype=dtype)
-    if out.dim() != 4 or (out.shape[0], out.shape[2], out.shape[3]) != (N, H, W):
-        raise ValueError("out has the wrong shape")
-    _run(index, "sq_nhwc_unpack", lib.sq_nhwc_unpack, m.data_ptr(), _dtype_code(m, "m"), _dense(out, "out", index, out.dtype),
-         _dtype_code(out, "out"), N, C, H, W, _rows_of(m, "m", index), out.shape[1], int(c_offset))
+        out = m.new_empty((N, C + c_offset, H, W), dtype=dtype)
+        address = out.data_ptr()
+    else:
+        if out.dim() != 4 or (out.shape[0], out.shape[2], out.shape[3]) != (N, H, W):
+            raise ValueError("out has the wrong shape")
+        address = _dense(out, "out", index, out.dtype)
+    _run(index, "sq_nhwc_unpack", lib.sq_nhwc_unpack, m.data_ptr(), _dtype_code(m, "m"), address, _dtype_code(out, "out"),
+         N, C, H, W, _rows_of(m, "m", index), out.shape[1], c_offset)
     return out
 
 
@@ -823,12 +830,11 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
     N, H, W, C = m.shape
     index = _gpu_of(m, "m")
     if out is None:
-        out = torch.empty((N, H, W, C), device=m.device, dtype=m.dtype)
+        out = torch.empty_like(m)
     elif out.shape != m.shape or out.dtype != m.dtype:
         raise ValueError("out has the wrong shape or type")
-    for t, name in ((gamma, "gamma"), (beta, "beta")):
-        if t is not None and t.numel() != C:
-            raise ValueError(f"{name} must have one value per layer")
+    if gamma is not None and gamma.numel() != C or beta is not None and beta.numel() != C:
+        raise ValueError("gamma and beta must have one value per layer")
     ld_in, ld_out, groups = _rows_of(m, "m", index), _rows_of(out, "out", index), int(groups)
     workspace, address, nbytes = _scratch(workspace, lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups), m, index)
     _run(index, "sq_nhwc_group_norm", lib.sq_nhwc_group_norm, m.data_ptr(), out.data_ptr(), _dtype_code(m, "m"),
@@ -848,9 +854,11 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
     Cout, Cin = kernels[0], kernels[1]
     shape = x.shape[:-1] + (Cout,)
     if out is None:
-        out = torch.empty(shape, device=x.device, dtype=out_dtype or (x.dtype if residual is None else residual.dtype))
-    elif out.shape != shape or out_dtype not in (None, out.dtype):
-        raise ValueError("out has the wrong shape or type")
+        out, ld_out = x.new_empty(shape, dtype=out_dtype or (x.dtype if residual is None else residual.dtype)), Cout
+    else:
+        if out.shape != shape or out_dtype not in (None, out.dtype):
+            raise ValueError("out has the wrong shape or type")
+        ld_out = _rows_of(out, "out", index)
     ld_res, res = 0, None
     if residual is not None:
         if residual.shape != shape or residual.dtype != out.dtype:
@@ -858,7 +866,7 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
         ld_res, res = _rows_of(residual, "residual", index), residual.data_ptr()
     if b is not None and b.numel() != Cout:
         raise ValueError("b must have one value per output layer")
-    ld_in, ld_out = _rows_of(x, "x", index), _rows_of(out, "out", index)
+    ld_in = _rows_of(x, "x", index)
     rows = x.numel() // Cin if Cin else 0
     if rows > _MAX_INT or Cin > _MAX_INT or Cout > _MAX_INT:
         _check(-3, "sq_linear_forward")

@@ -640,7 +640,7 @@ template <typename TI, typename TO> int by_size(const LinearArgs &p)
         return launch_wave<TI, TO, 32, 32, 8>(p, steps);
     }
     if constexpr (sizeof(TI) == 4) {
-        static const Tiling kF32[] = {{64, 64, 768, 2.0, 1.25, 0.6}, {128, 128, 256, 3.0, 1.36, 1.2}, {256, 128, 256, 5.0, 2.45, 2.1}};
+        static const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6}, {128, 128, 256, 4.5, 1.36, 1.2}, {256, 128, 256, 8.5, 2.45, 2.1}};
         switch (cheapest(kF32, p, steps)) {
             case 0: return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
             case 1: return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);

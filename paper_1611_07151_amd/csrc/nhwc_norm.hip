@@ -155,67 +155,59 @@ __device__ __forceinline__ float team_sum(float v, int shift)
 }
 
 // Sums of v[i], which belong to a thread's n layers, over the threads and layers of each group of the block, in v[i].
-// First over the rows, folded in half step by step through LDS, a value per vector where its layers are of one group
-// and per layer else; then each group's by a team of threads of its own.
+// A value per vector where its layers are of one group, per layer else.  First over the rows a wavefront holds, lane to
+// lane (narrow rows: lanes a row apart hold the same vector), then through LDS over wavefronts (or rows) and layers, each
+// group by a team of threads.
 template <int n> __device__ __forceinline__ void group_sums(const NormArgs &p, const Place &at, float (&v)[n], float *lds, float *sums)
 {
-    const int cg = p.parts > 1 ? at.width : p.C / p.G;
-    const bool one = n == 1 || cg % n == 0;
+    const int cg = p.parts > 1 ? at.width : p.C / p.G, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    const bool one = n == 1 || p.groups == 1 || cg % n == 0;
     if (one) {
 #pragma unroll
         for (int i = 1; i < n; ++i) v[0] += v[i];
     }
-    __syncthreads();
-    if (p.groups == 1) {
-        if constexpr (n > 1)
-            if (!one) {
 #pragma unroll
-                for (int i = 1; i < n; ++i) v[0] += v[i];
-            }
-        float all = at.live ? v[0] : 0.f;
+    for (int i = 0; i < n; ++i) v[i] = at.live ? v[i] : 0.f;
+    __syncthreads();        // the areas' last readers are done
+    if (p.groups == 1) {
+        float all = v[0];
 #pragma unroll
         for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = all;
+        if (lane == 0) lds[wave] = all;
         __syncthreads();
         all = lds[0];
-        for (int w = 1; w < (int)blockDim.x >> 6; ++w) all += lds[w];
+        for (int w = 1; w < waves; ++w) all += lds[w];
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] = all;
         return;
     }
     const int items = one ? at.vectors : at.width;      // per row
-    float *const mine = lds + at.row * items + at.vector * (one ? 1 : n);
-    for (int rows = at.rows; rows > 1;) {
-        const int half = (rows + 1) / 2;
-        if (at.live && at.row >= half && at.row < rows) {
-            mine[0] = v[0];
-            if (!one)
+    const bool narrow = at.vectors <= 32;
+    if (narrow)
+        for (int d = at.vectors; d < 64; d <<= 1) {
 #pragma unroll
-                for (int i = 1; i < n; ++i) mine[i] = v[i];
+            for (int i = 0; i < n; ++i)
+                if (i == 0 || !one) {
+                    const float other = __shfl_down(v[i], d);
+                    v[i] += lane + d < 64 ? other : 0.f;
+                }
         }
-        __syncthreads();
-        if (at.live && at.row + half < rows) {
-            const float *other = mine + half * items;
-            v[0] += other[0];
-            if (!one)
-#pragma unroll
-                for (int i = 1; i < n; ++i) v[i] += other[i];
-        }
-        rows = half;
-    }
-    if (at.live && at.row == 0) {       // what others read of this row was read before the last barrier
+    const int parts = narrow ? waves : at.rows;
+    if (narrow ? lane < at.vectors : at.live) {
+        float *const mine = lds + (narrow ? wave : at.row) * items + at.vector * (one ? 1 : n);
         mine[0] = v[0];
         if (!one)
 #pragma unroll
             for (int i = 1; i < n; ++i) mine[i] = v[i];
     }
     __syncthreads();
-    const int each = items / p.groups, shift = team_shift(p.groups, each), lane = threadIdx.x & ((1 << shift) - 1);
+    const int each = items / p.groups, shift = team_shift(p.groups, each), member = threadIdx.x & ((1 << shift) - 1);
     for (int g = threadIdx.x >> shift; g < p.groups; g += blockDim.x >> shift) {
         float s = 0.f;
-        for (int m = lane; m < each; m += 1 << shift) s += lds[g * each + m];
+        for (int m = member; m < each; m += 1 << shift)
+            for (int r = 0; r < parts; ++r) s += lds[r * items + g * each + m];
         s = team_sum(s, shift);
-        if (lane == 0) sums[g] = s;
+        if (member == 0) sums[g] = s;
     }
     __syncthreads();
     each_group<n>(at.vector * n, cg, [&](int i, int g) { v[i] = sums[g]; });
@@ -492,7 +484,7 @@ double fused_us(const Plan &q, int N, int cg, long long HW, int size)
 {
     const double slab = (double)HW * q.width, each = (size == 2 ? 1.15e-6 : 1.45e-6) * slab * N * q.blocks;
     const int piece = q.blocks > 1 ? q.width * size : 64;
-    return 4.5 + std::max(0.2e-3 * slab * (q.vec == 2 ? 2.5 : q.vec == 4 ? 1.3 : 1.0), each * (piece < 32 ? 1.35 : piece < 64 ? 1.1 : 1.0) * (q.groups > 1 && cg % (q.vec / size) ? 1.4 : 1.0));
+    return 4.5 + std::max(0.2e-3 * slab * (q.vec == 2 ? 2.5 : q.vec == 4 ? 1.3 : 1.0), each * (piece < 16 ? 5.0 : piece < 32 ? 1.35 : piece < 64 ? 1.1 : 1.0) * (q.groups > 1 && cg % (q.vec / size) ? 1.4 : 1.0));
 }
 
 Plan make_plan(int N, int C, long long HW, int G, int size)
@@ -537,7 +529,7 @@ Plan make_plan(int N, int C, long long HW, int G, int size)
     }
     if (q.fused) return q;
     // chunks, 256 threads
-    if (cg > 256 * (16 / size) || vector_bytes(cg, size) * 256 < cg * size) {
+    if ((long long)cg * size > 256ll * vector_bytes(cg, size)) {     // a group is wider than a workgroup
         q.vec = vector_bytes(cg, size);
         q.width = 256 * (q.vec / size);
         q.groups = 1;

@@ -111,7 +111,7 @@ class _OnGpu:
         return 0
 
     def __init__(self, t):
-        self.shape, self.stride, self.is_contiguous = t.shape, t.stride, t.is_contiguous
+        self.shape, self.stride, self.is_contiguous, self.numel = t.shape, t.stride, t.is_contiguous, t.numel
 
 
 def test_which_tensors_are_rows():
@@ -126,6 +126,6 @@ def test_which_tensors_are_rows():
             ok(bad)
     with pytest.raises(ValueError):
         ok(torch.zeros(8))
-    huge = torch.empty((2, 1), device="meta").as_strided((2, 1), (2**31, 1))
-    with pytest.raises(SqError):
-        ok(huge)
+    for shape, strides in (((2, 1), (2**31, 1)), ((2**31, 2), (2, 1)), ((1, 2**31), (2**31, 1))):
+        with pytest.raises(SqError):
+            ok(torch.empty(1, device="meta").as_strided(shape, strides))
