@@ -303,7 +303,8 @@ int sq_init(void)
     void *unused = nullptr;
     const int rs = static_scratch(&unused);
     if (rs) return rs;
-    const bool ok = conv_mfma_register_kernels() & blocked_register_kernels() & split_register_kernels() & stem_register_kernels() & fire_bf16_register_kernels();
+    const bool ok = conv_mfma_register_kernels() & blocked_register_kernels() & split_register_kernels() & stem_register_kernels() & fire_bf16_register_kernels() &
+                    nhwc_layout_register_kernels() & nhwc_norm_register_kernels() & linear_register_kernels();
     if (!ok) {
         const int rc = check_launch();
         return rc ? rc : SQ_ERR_HIP;

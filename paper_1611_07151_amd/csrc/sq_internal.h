@@ -202,9 +202,9 @@ int maxpool(const float *in, float *out, int N, int C, int H, int W, int K, int 
 int avgpool_global(const float *in, float *out, int N, int C, int H, int W);
 int softmax(const float *in, float *out, int N, int C);
 
-// Channels-last maps: [N][HW] rows of ld values, the first C of them the operator's (nhwc_layout.hip, nhwc_norm.hip).
 // Whether `blocks` workgroups of `threads` fit one launch (the runtime counts the threads of a grid in 32 bits).
 inline bool one_launch(double blocks, int threads) { return blocks * threads < 4294967296.0; }
+// Channels-last maps: [N][HW] rows of ld values, the first C of them the operator's (nhwc_layout.hip, nhwc_norm.hip).
 int nhwc_pack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld);
 int nhwc_unpack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld, int out_channels);
 size_t nhwc_group_norm_workspace_bytes(int N, int C, long long HW, int G);
@@ -227,6 +227,10 @@ inline double linear_bytes(const LinearArgs &a)
     return si * ((double)a.rows * a.Cin + (double)a.Cout * a.Cin) + so * (double)a.rows * a.Cout * (a.residual ? 2 : 1) + 4.0 * a.Cout;
 }
 int linear(const LinearArgs &a);
+// Loads the code of these kernels onto the current device (sq_init).
+bool nhwc_layout_register_kernels();
+bool nhwc_norm_register_kernels();
+bool linear_register_kernels();
 
 // Optional per-launch timing (sq_profile_begin/end).  A LaunchScope brackets one kernel
 // launch with a pair of HIP events on the library's stream when profiling is on and

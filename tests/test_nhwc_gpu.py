@@ -318,6 +318,35 @@ def test_linear_gives_the_same_bits_again(sq, rows, cin, cout, dt):
         assert torch.equal(sq.sq_linear_forward(x, w, act=2), first)
 
 
+@pytest.mark.parametrize("act", (1, 2, 3))
+def test_activations_by_themselves(sq, act):
+    """One layer with kernel 1: the result is the activation of the input.
+    SiLU: the exponent's argument is rounded (|x| u), exponential, sum and reciprocal add 3u, all through x s(1 - s), and two
+    products.  GELU: the tail's fit is good to 1.5e-7 of at most 1/2, its exponent t^2/2 has three roundings (t^2 Q < 0.22), some
+    twenty more operations of u each on at most 1/2, and two on the result: 7.5e-8 + 13 u of |x|."""
+    x = torch.cat((torch.linspace(-20, 20, 40001), torch.logspace(-30, 30, 121), -torch.logspace(-30, 2, 65), torch.tensor([0.0, -0.0])))
+    got = sq.sq_linear_forward(x.reshape(-1, 1).cuda(), torch.ones((1, 1), device="cuda"), act=act).cpu().double().reshape(-1)
+    x = x.double()
+    ref, sig = act64(x, act), 1 / (1 + torch.exp(-x))
+    bound = {1: torch.zeros_like(x), 2: x.abs() * sig * (1 - sig) * (x.abs() + 3) * U + 4 * U * ref.abs(),
+             3: (7.5e-8 + 13 * U) * x.abs()}[act]
+    check(got, ref, bound + torch.finfo(F32).smallest_normal, act)
+    odd = torch.tensor([float("inf"), -float("inf"), float("nan")])
+    got = sq.sq_linear_forward(odd.reshape(-1, 1).cuda(), torch.ones((1, 1), device="cuda"), act=act).cpu().reshape(-1)
+    want = act64(odd.double(), act)
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~want.isnan()].double(), want[~want.isnan()])
+
+
+def test_kernels_of_a_1x1_convolution_as_they_lie(sq):
+    """The same layer as sq_conv2d_forward on the NCHW map: both within the products' bound of the definition."""
+    g = gen(91)
+    x, w, b = torch.randn((2, 48, 9, 11), generator=g).cuda(), torch.randn((40, 48, 1, 1), generator=g).cuda(), torch.randn(40, generator=g).cuda()
+    conv = sq.sq_conv2d_forward(x, w, b, relu=True)
+    rows = sq.sq_linear_forward(sq.sq_nhwc_pack(x), w, b, act=sq.SQ_ACT_RELU)
+    sums = torch.nn.functional.conv2d(x.abs().double().cpu(), w.abs().double().cpu(), b.abs().double().cpu())
+    check(sq.sq_nhwc_unpack(rows), conv.cpu().double(), 2 * (48 + 16) * 2 * U * sums, "conv")
+
+
 # ------------------------------------------------------------------------------------------------------- together
 def block(sq, x, p, ws=None):
     """conv -> channels last -> normalise -> widen -> back, added -> NCHW."""
@@ -397,22 +426,67 @@ def test_two_streams_at_once(sq):
         assert all(torch.equal(g, want[i]) for g in got[i])
 
 
-def test_offsets_past_32_bits(sq):
-    """Rows that begin more than 2^31 elements (and 2^32 bytes) into their map."""
-    rows, ld = 4100, 600000
-    big = torch.empty((rows, ld), dtype=BF16, device="cuda")
+def test_two_host_threads_at_once(sq):
+    """Each with a stream of its own; the library's stream belongs to the calling thread."""
+    import threading
+    ps = [block_params(F32, 16), block_params(BF16, 17)]
+    xs = [torch.randn((3, 16, 27, 27), generator=gen(s)).cuda() for s in (11, 12)]
+    want = [block(sq, x, p) for x, p in zip(xs, ps)]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def worker(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(10):
+                    got[i].append(block(sq, xs[i], ps[i]))
+            stream.synchronize()
+        except Exception as e:       # noqa: BLE001 - reported by the main thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=worker, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for i in (0, 1):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+@pytest.mark.parametrize("dt,ld", [(BF16, 600000), (F32, 540000)])
+@pytest.mark.parametrize("cout", (32, 128, 384))
+def test_offsets_past_32_bits(sq, dt, ld, cout):
+    """Rows that begin more than 2^31 elements (and 2^32 bytes) into their map; few and many results."""
+    rows = 4100
+    big = torch.empty((rows, ld), dtype=dt, device="cuda")
     x = big[:, ld - 64:]
     x.copy_(torch.randn((rows, 64), generator=gen(1)))
-    w = torch.randn((32, 64), generator=gen(2)).to(BF16).cuda()
+    w = torch.randn((cout, 64), generator=gen(2)).to(dt).cuda()
     dense = x.contiguous()
     want = sq.sq_linear_forward(dense, w, act=1)
-    assert torch.equal(sq.sq_linear_forward(x, w, act=1, out=big[:, :32]), want)
+    assert torch.equal(sq.sq_linear_forward(x, w, act=1, out=big[:, :cout]), want)
+    again = sq.sq_linear_forward(dense, w, act=1, residual=want)
+    assert torch.equal(sq.sq_linear_forward(x, w, act=1, residual=big[:, :cout], out=big[:, :cout]), again)
     m = x.unflatten(0, (1, 41, 100))
     want = sq.sq_nhwc_group_norm(dense.reshape(1, 41, 100, 64), 4, act=2)
     assert torch.equal(sq.sq_nhwc_group_norm(m, 4, act=2, out=big[:, :64].unflatten(0, (1, 41, 100))), want)
-    assert torch.equal(sq.sq_nhwc_unpack(m, dtype=BF16), dense.reshape(1, 41, 100, 64).permute(0, 3, 1, 2))
+    assert torch.equal(sq.sq_nhwc_unpack(m, dtype=dt), dense.reshape(1, 41, 100, 64).permute(0, 3, 1, 2))
     back = dense.reshape(1, 41, 100, 64).permute(0, 3, 1, 2).contiguous()
     assert torch.equal(sq.sq_nhwc_pack(back, out=big[:, 128:192].unflatten(0, (1, 41, 100))), dense.reshape(1, 41, 100, 64))
+
+
+def test_group_norm_of_a_map_past_32_bits(sq):
+    """2.2 billion values: a map of 100 equal bands has the statistics of one, so each band is the result of the band alone up to
+    the rounding of statistics summed in another order (a step of bfloat16 at most)."""
+    band = torch.randn((1, 83, 8300, 32), generator=gen(21)).to(BF16).cuda()
+    want = sq.sq_nhwc_group_norm(band, 4, act=2)
+    x = band.repeat(1, 100, 1, 1)
+    got = sq.sq_nhwc_group_norm(x, 4, act=2, out=x)
+    for i in (0, 49, 99):
+        part = got[:, 83 * i:83 * (i + 1)].float()
+        assert ((part - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-30).all(), i
 
 
 def test_profiler_sees_the_launches(sq):
