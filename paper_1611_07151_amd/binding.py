@@ -714,7 +714,9 @@ def sq_squeezenet_forward_bf16(x, params, packed, workspace=None, probs=None, wa
 # a contiguous tensor, or a slice of the last dimension of one.  All tensors of a call live on one GPU, which need
 # not be the current one; the call runs on that GPU's current stream.
 _MAX_INT = 2**31 - 1
+# the quick forms of torch.cuda.current_stream(index).cuda_stream and torch.cuda.current_device(), 3 us together
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _gpu_of(x, name):
@@ -768,7 +770,7 @@ def _dense(t, name, index, dtype):
 
 
 def _run(index, what, fn, *args):
-    if index != torch.cuda.current_device():
+    if index != _current_gpu():
         with torch.cuda.device(index):
             lib.sq_set_stream(_raw_stream(index))
             rc = fn(*args)
@@ -848,11 +850,11 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
     both bfloat16; b [Cout] float32 or None; out and residual [..., Cout] of out_dtype (default: that of x, residual or
     out).  `residual` may be `out` itself."""
     index = _gpu_of(x, "x")
-    kernels = w.shape
-    if len(kernels) not in (2, 4) or len(kernels) == 4 and tuple(kernels[2:]) != (1, 1) or x.shape[-1] != kernels[1]:
+    *outer, Cin = x.shape
+    Cout, *rest = w.shape
+    if rest != [Cin] and rest != [Cin, 1, 1]:
         raise ValueError("kernel shape does not match the input")
-    Cout, Cin = kernels[0], kernels[1]
-    shape = x.shape[:-1] + (Cout,)
+    shape = (*outer, Cout)
     if out is None:
         out, ld_out = x.new_empty(shape, dtype=out_dtype or (x.dtype if residual is None else residual.dtype)), Cout
     else:
