@@ -277,13 +277,17 @@ template <typename TO, int XB, int JB> __device__ __forceinline__ void write_row
 // Bound by the matrix unit, which a large product keeps busy two thirds of the cycles at the clock that its power leaves (1.8 GHz):
 // 8192^3 in 805 us (1365 TFLOP/s); 16224 x 4096 x 4096 in 411 us (1326), with GELU and residual 475.  What is left is one
 // barrier a step and the time it takes the wavefronts to come out of it.
-template <typename TO, int BM, int BN, int WR, int WC, int NS>
-__global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 : 1) void linear_tile_bf16_kernel(LinearArgs p, int tiles_r, int tiles_j)
+// KS teams of WR x WC wavefronts share out k for results that are too few to fill the chip with tiles, where what bounds a
+// tile is the latency of its steps: 128 x 4096 x 4096 19.8 -> 14.8 us, 729 x 1536 x 384 9.5 -> 7.7 (64 x 64 tiles, two teams).
+// p.Cin / 64 has to be a multiple of KS.
+template <typename TO, int BM, int BN, int WR, int WC, int NS, int KS>
+__global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 1024 ? 2 : 1) void linear_tile_bf16_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
     constexpr int NW = WR * WC, XB = BM / WR / 32, JB = BN / WC / 32, kImage = (BM + BN) * 8;
     constexpr int XI = BM / 8 / NW, JI = BN / 8 / NW, NI = XI + JI;       // loads of 8 rows per wavefront
-    __shared__ u32x4_t lds[NS * kImage];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ u32x4_t all[KS * NS * kImage];
+    const int lane = threadIdx.x & 63, team = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW)), wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % NW);
+    u32x4_t *const lds = all + team * NS * kImage;
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
     const int r0 = tr * BM, j0 = tj * BN;
@@ -291,7 +295,9 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 
     // lane's row is lane / 8 and its place lane % 8.  Per load the lane's row and piece are a 32-bit offset from the
     // tile's first row; k moves in the uniform offset.
     auto piece = [&](int i) { return (lane & 7) ^ (((wave * (i < XI ? XI : JI) + (i < XI ? i : i - XI)) & 1) * 4 + (lane >> 4)); };
-    const bf16_t *const x0 = (const bf16_t *)p.in + r0 * p.ld_in, *const w0 = (const bf16_t *)p.w + (long long)j0 * p.Cin;
+    // the team's share of the whole steps, the same number for each
+    const int whole = p.Cin / 64 / KS, tail = p.Cin % 64, k0 = 64 * whole * team;
+    const bf16_t *const x0 = (const bf16_t *)p.in + r0 * p.ld_in + k0, *const w0 = (const bf16_t *)p.w + (long long)j0 * p.Cin + k0;
     const u32x4_t xr = {(uint32_t)(uintptr_t)x0, (uint32_t)((uintptr_t)x0 >> 32), 0xffffffffu, 0x00020000u};
     const u32x4_t wr = {(uint32_t)(uintptr_t)w0, (uint32_t)((uintptr_t)w0 >> 32), 0xffffffffu, 0x00020000u};
     uint32_t off[NI];
@@ -300,7 +306,7 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 
         off[i] = i < XI ? (uint32_t)(row_at(r0, (wave * XI + i) * 8 + (lane >> 3), p.rows) - r0) * (uint32_t)(2 * p.ld_in) + piece(i) * 16
                         : (uint32_t)(row_at(j0, (wave * JI + i - XI) * 8 + (lane >> 3), p.Cout) - j0) * (uint32_t)(2 * p.Cin) + piece(i) * 16;
     auto place_of = [&](int i) { return i < XI ? (wave * XI + i) * 64 : BM * 8 + (wave * JI + i - XI) * 64; };
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4_t *)lds);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4_t *)all) + team * (uint32_t)(NS * kImage * 16);
     // Load i of the step at k into an image.  As an instruction of its own, because the compiler would let every later read of
     // LDS wait for it; `arrive` is what orders them.  m0 is set before each: nothing else in this kernel reads it (gfx950's
     // LDS instructions do not).
@@ -319,11 +325,10 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 
     };
     // Step s lies in image s % NS.  The part of k behind the last whole step goes first, through registers, with zeros behind
     // its end, as step -1 in the last image.
-    const int whole = p.Cin / 64, tail = p.Cin - 64 * whole;
-    if (tail) {
+    if (tail) {         // by the last team; the others' share of it is zeros
 #pragma unroll 1
         for (int i = 0; i < NI; ++i)
-            lds[(NS - 1) * kImage + place_of(i) + lane] = load16_tail((const bf16_t *)((const char *)((i < XI ? x0 : w0) + 64 * whole) + off[i]), tail - piece(i) * 8);
+            lds[(NS - 1) * kImage + place_of(i) + lane] = load16_tail((const bf16_t *)((const char *)((i < XI ? x0 : w0) + 64 * whole) + off[i]), team == KS - 1 ? tail - piece(i) * 8 : 0);
     }
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -381,9 +386,34 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 128 * NS <= 80 * 1024 ? 2 
         img = next;
     }
     __syncthreads();
+    if constexpr (KS > 1) {     // the first team adds the others' sums, in their order
+        constexpr int kSums = XB * JB * 4 * 64;     // 16-byte pieces of a wavefront
+        static_assert(kSums * NW <= NS * kImage, "a team's sums fit its images");
+        if (team > 0) {
+#pragma unroll
+            for (int m = 0; m < XB * JB; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4_t v = {acc[m / JB][m % JB][4 * q], acc[m / JB][m % JB][4 * q + 1], acc[m / JB][m % JB][4 * q + 2], acc[m / JB][m % JB][4 * q + 3]};
+                    ((f32x4_t *)lds)[wave * kSums + (m * 4 + q) * 64 + lane] = v;
+                }
+        }
+        __syncthreads();
+        if (team > 0) return;
+#pragma unroll
+        for (int t = 1; t < KS; ++t)
+#pragma unroll
+            for (int m = 0; m < XB * JB; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4_t v = ((const f32x4_t *)(all + t * NS * kImage))[wave * kSums + (m * 4 + q) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[m / JB][m % JB][4 * q + e] += v[e];
+                }
+    }
     constexpr int kBuf = 32 * (32 * JB + 4);
     static_assert(kBuf * 4 * NW <= NS * kImage * 16, "the wavefronts' exchange areas fit the images");
-    write_rows<TO, XB, JB>(p, (float *)lds + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
+    write_rows<TO, XB, JB>(p, (float *)all + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
 }
 
 // The same tiles through registers: operands that memory-to-LDS loads cannot take (rows at any address, any number of
@@ -595,12 +625,12 @@ template <typename TI, typename TO, int RT, int CT, int MAXW> int launch_wave(co
     return check_launch();
 }
 
-template <typename TO, int BM, int BN, int WR, int WC, int NS> int launch_tile_bf16(const LinearArgs &p)
+template <typename TO, int BM, int BN, int WR, int WC, int NS, int KS = 1> int launch_tile_bf16(const LinearArgs &p)
 {
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
-    if (!one_launch((double)tr * tj, 64 * WR * WC)) return SQ_ERR_UNSUPPORTED;
+    if (!one_launch((double)tr * tj, 64 * WR * WC * KS)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_tile_bf16", linear_flops(p), linear_bytes(p));
-    hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC, NS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
+    hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC, NS, KS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC * KS), 0, current_stream(), p, tr, tj);
     return check_launch();
 }
 
@@ -623,7 +653,7 @@ double tiling_us(const Tiling &t, const LinearArgs &p, int steps)
     if (tiles <= 256) return t.fixed + t.alone * steps;
     return (double)((tiles + t.slots - 1) / t.slots) * (t.fixed + t.step * steps);
 }
-template <int n> int cheapest(const Tiling (&t)[n], const LinearArgs &p, int steps)
+int cheapest(const Tiling *t, int n, const LinearArgs &p, int steps)
 {
     int best = 0;
     for (int i = 1; i < n; ++i)
@@ -633,8 +663,9 @@ template <int n> int cheapest(const Tiling (&t)[n], const LinearArgs &p, int ste
 
 // Few results: the wavefronts, in blocks of 16 x 16 up to 2^16 results, a short sum or 16 rows, else 32 x 32 (us, 16 / 32: 586 x
 // 1952 x 64 bf16 5.4 / 7.8, 99 x 3088 x 80 7.0 / 10.9; 45 x 1792 x 3520 12.9 / 9.5, 3458 x 2016 x 56 13.1 / 8.2).  Tiles through LDS
-// from as many results on as they need to fill the chip: 2^18 bf16 (us, wavefronts / tiles: 461 x 64 x 2752 7.8 / 3.8, 729 x 1536
-// x 384 14.2 / 10.4; 1959 x 3224 x 72 11.9 / 17.8), 2^17 where rows lie at any address (905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
+// from as many results on as they need to fill the chip: bf16 2^16 where two teams can share k (us, wavefronts / tiles: 32 x 4096 x
+// 4096 19.0 / 13.6, 64 x 1024 x 1024 6.7 / 5.8; 300 x 2048 x 300 10.2 / 10.0), else 2^18 (461 x 64 x 2752 7.8 / 3.8; 1959 x 3224 x 72
+// 11.9 / 17.8), 2^17 where rows lie at any address (905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
 // 16.1 / 18.1), 2^20 fp32 (461 x 64 x 2752 8.9 / 6.3, 3506 x 416 x 1096 58 / 27; 409 x 576 x 1184 12.2 / 14.1, 729 x 1536 x 384 26 / 29).
 template <typename TI, typename TO> int by_size(const LinearArgs &p)
 {
@@ -643,29 +674,31 @@ template <typename TI, typename TO> int by_size(const LinearArgs &p)
     // memory-to-LDS loads: whole 16-byte pieces, a tile's rows within 32-bit offsets
     const bool direct = sizeof(TI) == 2 && p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
                         p.ld_in < (1 << 22) && p.Cin < (1 << 22);
-    if (p.rows <= 16 || results <= 65536 || steps <= 2) {
-        if (p.rows <= 16 || results < (direct ? 1 << 18 : sizeof(TI) == 2 ? 1 << 17 : 1 << 20)) return launch_wave<TI, TO, 16, 16, 16>(p, 2 * steps);
-    } else if (results < (direct ? 1 << 18 : sizeof(TI) == 2 ? 1 << 17 : 1 << 20)) {
-        return launch_wave<TI, TO, 32, 32, 8>(p, steps);
-    }
+    const bool teams = direct && p.Cin / 64 % 2 == 0 && p.Cin >= 256;       // two teams share k evenly
+    const double many = teams ? 1 << 16 : direct ? 1 << 18 : sizeof(TI) == 2 ? 1 << 17 : 1 << 20;
+    if (p.rows <= 16 || results < many)
+        return p.rows <= 16 || results <= 65536 || steps <= 2 ? launch_wave<TI, TO, 16, 16, 16>(p, 2 * steps) : launch_wave<TI, TO, 32, 32, 8>(p, steps);
     if constexpr (sizeof(TI) == 4) {
         static const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6}, {128, 128, 256, 4.5, 1.36, 1.2}, {256, 128, 256, 8.5, 2.45, 2.1}};
-        switch (cheapest(kF32, p, steps)) {
+        switch (cheapest(kF32, 3, p, steps)) {
             case 0: return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
             case 1: return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
             default: return launch_tile<TI, TO, 256, 128, 4, 2, 1>(p);
         }
     } else if (direct) {
-        static const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29}, {128, 128, 256, 2.5, 0.57, 0.5}, {128, 128, 512, 4.4, 1.0, 0.75}, {256, 256, 256, 9.0, 1.5, 1.25}};
-        switch (cheapest(kDirect, p, steps)) {
+        static const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29},  {128, 128, 256, 2.5, 0.57, 0.5}, {128, 128, 512, 4.4, 1.0, 0.75},
+                                         {256, 256, 256, 9.0, 1.5, 1.25}, {64, 64, 256, 2.5, 0.22, 0.19}, {128, 64, 256, 3.5, 0.32, 0.3}};
+        switch (teams ? cheapest(kDirect, 6, p, steps) : cheapest(kDirect, 4, p, steps)) {
             case 0: return launch_tile_bf16<TO, 64, 64, 2, 2, 4>(p);
             case 1: return launch_tile_bf16<TO, 128, 128, 2, 4, 4>(p);
             case 2: return launch_tile_bf16<TO, 128, 128, 2, 2, 2>(p);
-            default: return launch_tile_bf16<TO, 256, 256, 2, 4, 2>(p);
+            case 3: return launch_tile_bf16<TO, 256, 256, 2, 4, 2>(p);
+            case 4: return launch_tile_bf16<TO, 64, 64, 2, 2, 4, 2>(p);
+            default: return launch_tile_bf16<TO, 128, 64, 2, 2, 3, 2>(p);
         }
     } else {
         static const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45}, {128, 128, 512, 4.0, 1.8, 0.85}};
-        if (cheapest(kAny, p, steps) == 0) return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
+        if (cheapest(kAny, 2, p, steps) == 0) return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
         return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
     }
 }

@@ -244,7 +244,10 @@ def test_linear_shapes(sq, rows, cin, cout, ti, to):
 LINEAR_LARGE = [(1024, 2048, 1024), (2100, 1032, 1000), (3601, 328, 3584), (13000, 200, 1000), (129, 4096, 4104), (9000, 2056, 130),
                 (2187, 1000, 1001), (4100, 777, 1030), (5400, 520, 2048), (6100, 72, 1801), (905, 193, 704), (1100, 33, 520), (905, 200, 704),
                 (700, 72, 600), (300, 1536, 200), (150, 2048, 500), (257, 1000, 333), (600, 40, 520), (600, 8, 520), (2100, 31, 600),
-                (1500, 64, 700), (1500, 128, 700), (1500, 96, 1032), (1200, 256, 1024)]
+                (1500, 64, 700), (1500, 128, 700), (1500, 96, 1032), (1200, 256, 1024),
+                # bf16: two teams that share k, with and without a part step, ragged edges
+                (64, 1024, 1024), (70, 1032, 1000), (129, 264, 520), (33, 4096, 2050), (300, 2048, 300), (500, 4096, 4096), (490, 2056, 4001),
+                (20000, 256, 8), (200, 320, 400)]
 
 
 @pytest.mark.parametrize("ti,to", TYPES)
