@@ -554,7 +554,7 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
  *     ld_out values; both of out_dtype: SQ_F32 with SQ_F32 inputs, either with SQ_BF16 inputs
  *     (otherwise SQ_ERR_UNSUPPORTED).  residual may be out itself with the same ld; apart from that
  *     out must not overlap any input.
- *   fp32: from about a million results on, the products run on the bfloat16 matrix instructions with
+ *   fp32: above 65536 results the products may run on the bfloat16 matrix instructions with
  *     each operand as the exact sum of three bfloat16 values and fp32 sums: the error stays that of fp32
  *     sums of the same terms, except that operands below 2^-110 in magnitude keep fewer bits.  An
  *     infinity or NaN reaches the results of its row or kernel and no others.

@@ -417,7 +417,9 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
 }
 
 // The same tiles through registers: operands that memory-to-LDS loads cannot take (rows at any address, any number of
-// layers) and fp32.  A step is 128 bytes of a row, PF of them on their way in registers, two images in LDS.
+// layers) and fp32.  A step is 128 bytes of a row, PF of them on their way in registers, two images in LDS.  KS teams as above,
+// of any number of steps (fp32: 729 x 1536 x 384 34 -> 24 us, 1024^3 25 -> 19; bf16 gained nothing, its unaligned loads are the
+// bound).
 //
 // fp32 products run on the bf16 instructions: every operand is the sum of three bfloat16 values, x = h + m + l with h its
 // upper half, m = round(x - h) and l = x - h - m, all three exact (24 bits in pieces of at most 8), and of the nine products the
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
 //
 // Bound by the matrix unit and the vector instructions of the splitting beside it: 10816 x 2048 x 2048 fp32 with GELU and residual in
 // 466 us (195 TFLOP/s; the fp32 instructions reach 154 in a large library product), 8192 x 4096 x 4096 in 1250 us (220); bf16 rows at
-// any address 2001^3 in 34 us (468 TFLOP/s), 14301 x 1649 x 2808 in 233 us (568).
+// any address 2001^3 in 33 us (468 TFLOP/s), 14301 x 1649 x 2808 in 233 us (568).
 template <typename TI> struct Image;
 template <> struct Image<bf16_t> {
     static constexpr int kStep = 64, kPlanes = 1;
@@ -460,8 +462,8 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t &h, uint32
     l = bf16_pair(a - __builtin_bit_cast(float, m << 16), b - __builtin_bit_cast(float, m & 0xffff0000u));
 }
 
-template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF>
-__global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, int tiles_r, int tiles_j)
+template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF, int KS>
+__global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
     using I = Image<TI>;
     constexpr int NW = WR * WC, XB = BM / WR / 32, JB = BN / WC / 32, kRows = BM + BN, kStep = I::kStep;
@@ -470,18 +472,21 @@ __global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, 
     static_assert(NP * 64 * NW == kRows * 8 && BM * 8 % (64 * NW) == 0, "whole pieces per thread");
     constexpr int kBuf = 32 * (32 * JB + 4);
     static_assert(kBuf * 4 * NW <= kImage * 32, "the wavefronts' exchange areas fit the images");
-    __shared__ u32x4_t lds[2 * kImage];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ u32x4_t all[KS * 2 * kImage];
+    const int lane = threadIdx.x & 63, team = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW)), wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % NW);
+    u32x4_t *const lds = all + team * 2 * kImage;
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
     const int r0 = tr * BM, j0 = tj * BN;
-    // thread t takes piece t % 8 of rows t / 8 + i * (threads / 8): BM rows of the input, then BN of the kernels
-    const int q = threadIdx.x & 7, row = threadIdx.x >> 3;
+    // KS teams share out the whole steps evenly; what is left of them and the part step are for the last team
+    const int whole = p.Cin / kStep / KS, left = whole * KS * kStep, k0 = whole * kStep * team;
+    // thread t of a team takes piece t % 8 of rows t / 8 + i * (threads / 8): BM rows of the input, then BN of the kernels
+    const int q = threadIdx.x & 7, row = (threadIdx.x % (64 * NW)) >> 3;
     const TI *src[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int r = row + i * 8 * NW;
-        src[i] = (i * 8 * NW < BM ? (const TI *)p.in + row_at(r0, r, p.rows) * p.ld_in : (const TI *)p.w + row_at(j0, r - BM, p.Cout) * p.Cin) + q * kPiece;
+        src[i] = (i * 8 * NW < BM ? (const TI *)p.in + row_at(r0, r, p.rows) * p.ld_in : (const TI *)p.w + row_at(j0, r - BM, p.Cout) * p.Cin) + q * kPiece + k0;
     }
     auto fetch = [&](u32x4_t (&to)[NP], int k) {
 #pragma unroll
@@ -542,16 +547,17 @@ __global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, 
 #pragma unroll
             for (int c = 0; c < JB; ++c) acc[i][c] = f32x16_t{};
         // Image s % 2 holds step s, ring entry s % PF what is to become step s; loads behind the last step take it again.
-        const int whole = p.Cin / kStep, tail = p.Cin - whole * kStep;
         u32x4_t ring[PF][NP];
 #pragma unroll
         for (int i = 0; i < PF; ++i)
             if (whole) fetch(ring[i], min(i, whole - 1) * kStep);
         __syncthreads();
-        if (tail) {     // the part of k behind the last whole step goes first, with zeros behind its end
+#pragma unroll 1
+        for (int k = left; k < p.Cin; k += kStep) {     // at most KS of them, first; zeros behind the end and for the other teams
             u32x4_t rest[NP];
+            const int have = team == KS - 1 ? p.Cin - k - q * kPiece : 0;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) rest[i] = load16_tail(src[i] + whole * kStep, tail - q * kPiece);
+            for (int i = 0; i < NP; ++i) rest[i] = load16_tail(src[i] + k - k0, have);
             store(rest, lds);
             __syncthreads();
             multiply(lds);
@@ -587,15 +593,45 @@ __global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, 
             __syncthreads();
         }
     };
+    // the first team adds the others' sums to its own, in their order
+    constexpr int kSums = XB * JB * 4 * 64;         // 16-byte pieces of a wavefront
+    static_assert(KS == 1 || kSums * NW <= 2 * kImage, "a team's sums fit its images");
+    auto add_up = [&]() {
+        if constexpr (KS > 1) {
+            if (team > 0) {
+#pragma unroll
+                for (int m = 0; m < XB * JB * 4; ++m) {
+                    const f32x16_t &v = acc[m / 4 / JB][m / 4 % JB];
+                    const f32x4_t part = {v[m % 4 * 4], v[m % 4 * 4 + 1], v[m % 4 * 4 + 2], v[m % 4 * 4 + 3]};
+                    ((f32x4_t *)lds)[wave * kSums + m * 64 + lane] = part;
+                }
+            }
+            __syncthreads();
+            if (team == 0) {
+#pragma unroll
+                for (int t = 1; t < KS; ++t)
+#pragma unroll
+                    for (int m = 0; m < XB * JB * 4; ++m) {
+                        const f32x4_t part = ((const f32x4_t *)(all + t * 2 * kImage))[wave * kSums + m * 64 + lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[m / 4 / JB][m / 4 % JB][m % 4 * 4 + e] += part[e];
+                    }
+            }
+            __syncthreads();
+        }
+    };
     sums(std::false_type{});
+    add_up();
     if constexpr (sizeof(TI) == 4) {
         int odd = 0;
+        if (team == 0) {
 #pragma unroll
-        for (int i = 0; i < XB; ++i)
+            for (int i = 0; i < XB; ++i)
 #pragma unroll
-            for (int c = 0; c < JB; ++c)
+                for (int c = 0; c < JB; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) odd |= !__builtin_isfinite(acc[i][c][e]);
+                    for (int e = 0; e < 16; ++e) odd |= !__builtin_isfinite(acc[i][c][e]);
+        }
         if (__syncthreads_or(odd)) {
             f32x16_t fine[XB][JB];
 #pragma unroll
@@ -603,6 +639,7 @@ __global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, 
 #pragma unroll
                 for (int c = 0; c < JB; ++c) fine[i][c] = acc[i][c];
             sums(std::true_type{});
+            add_up();
 #pragma unroll
             for (int i = 0; i < XB; ++i)
 #pragma unroll
@@ -611,7 +648,8 @@ __global__ __launch_bounds__(64 * WR *WC) void linear_tile_kernel(LinearArgs p, 
                     for (int e = 0; e < 16; ++e) acc[i][c][e] = __builtin_isfinite(fine[i][c][e]) ? fine[i][c][e] : acc[i][c][e];
         }
     }
-    write_rows<TO, XB, JB>(p, (float *)lds + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
+    if (team > 0) return;
+    write_rows<TO, XB, JB>(p, (float *)all + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
@@ -634,24 +672,26 @@ template <typename TO, int BM, int BN, int WR, int WC, int NS, int KS = 1> int l
     return check_launch();
 }
 
-template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF> int launch_tile(const LinearArgs &p)
+template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF, int KS = 1> int launch_tile(const LinearArgs &p)
 {
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
-    if (!one_launch((double)tr * tj, 64 * WR * WC)) return SQ_ERR_UNSUPPORTED;
+    if (!one_launch((double)tr * tj, 64 * WR * WC * KS)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_tile", linear_flops(p), linear_bytes(p), (sizeof(TI) == 4 ? 6.0 : 1.0) * linear_flops(p));
-    hipLaunchKernelGGL((linear_tile_kernel<TI, TO, BM, BN, WR, WC, PF>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), p, tr, tj);
+    hipLaunchKernelGGL((linear_tile_kernel<TI, TO, BM, BN, WR, WC, PF, KS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC * KS), 0, current_stream(), p, tr, tj);
     return check_launch();
 }
 
 // Microseconds of a tiling, from what it measured (products of 128 to 8192 rows, layers and results): `fixed` for filling the
 // pipeline and writing the results, `step` for 128 bytes of k when `slots` workgroups share the chip, `alone` when each
 // has a compute unit to itself.
-struct Tiling { int BM, BN, slots; double fixed, step, alone; };
+struct Tiling { int BM, BN, slots; double fixed, step, alone; int teams = 0; };
 double tiling_us(const Tiling &t, const LinearArgs &p, int steps)
 {
     const long long tiles = (long long)((p.rows - 1) / t.BM + 1) * ((p.Cout - 1) / t.BN + 1);
-    if (tiles <= 256) return t.fixed + t.alone * steps;
-    return (double)((tiles + t.slots - 1) / t.slots) * (t.fixed + t.step * steps);
+    // through registers, the steps that teams cannot share evenly and the part step come one at a time
+    const int whole = p.Cin / 32, odd = p.in_dtype == SQ_F32 ? (t.teams ? whole % t.teams : 0) + (p.Cin % 32 != 0) : 0;
+    if (tiles <= 256) return t.fixed + t.alone * steps + 2.0 * odd;
+    return (double)((tiles + t.slots - 1) / t.slots) * (t.fixed + t.step * steps + odd);
 }
 int cheapest(const Tiling *t, int n, const LinearArgs &p, int steps)
 {
@@ -665,8 +705,9 @@ int cheapest(const Tiling *t, int n, const LinearArgs &p, int steps)
 // 1952 x 64 bf16 5.4 / 7.8, 99 x 3088 x 80 7.0 / 10.9; 45 x 1792 x 3520 12.9 / 9.5, 3458 x 2016 x 56 13.1 / 8.2).  Tiles through LDS
 // from as many results on as they need to fill the chip: bf16 2^16 where two teams can share k (us, wavefronts / tiles: 32 x 4096 x
 // 4096 19.0 / 13.6, 64 x 1024 x 1024 6.7 / 5.8; 300 x 2048 x 300 10.2 / 10.0), else 2^18 (461 x 64 x 2752 7.8 / 3.8; 1959 x 3224 x 72
-// 11.9 / 17.8), 2^17 where rows lie at any address (905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
-// 16.1 / 18.1), 2^20 fp32 (461 x 64 x 2752 8.9 / 6.3, 3506 x 416 x 1096 58 / 27; 409 x 576 x 1184 12.2 / 14.1, 729 x 1536 x 384 26 / 29).
+// 11.9 / 17.8), 2^16 too where rows lie at any address (300 x 2049 x 300 27.7 / 16.1, 905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
+// 16.1 / 18.1), by estimate for fp32 (3506 x 416 x 1096 58 / 27, 1024^3 35 / 19, 729 x 1536 x 384 26.5 / 23.7; 300 x 2048 x 300 17.5 /
+// 27.8, 64 x 4096 x 4096 34 / 52).
 template <typename TI, typename TO> int by_size(const LinearArgs &p)
 {
     const double results = (double)p.rows * p.Cout;
@@ -675,15 +716,21 @@ template <typename TI, typename TO> int by_size(const LinearArgs &p)
     const bool direct = sizeof(TI) == 2 && p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
                         p.ld_in < (1 << 22) && p.Cin < (1 << 22);
     const bool teams = direct && p.Cin / 64 % 2 == 0 && p.Cin >= 256;       // two teams share k evenly
-    const double many = teams ? 1 << 16 : direct ? 1 << 18 : sizeof(TI) == 2 ? 1 << 17 : 1 << 20;
-    if (p.rows <= 16 || results < many)
+    const double many = direct && !teams ? 1 << 18 : 1 << 16;
+    if (p.rows <= 16 || results <= many || (sizeof(TI) == 4 && steps <= 2 && results < 1 << 20))
         return p.rows <= 16 || results <= 65536 || steps <= 2 ? launch_wave<TI, TO, 16, 16, 16>(p, 2 * steps) : launch_wave<TI, TO, 32, 32, 8>(p, steps);
     if constexpr (sizeof(TI) == 4) {
-        static const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6}, {128, 128, 256, 4.5, 1.36, 1.2}, {256, 128, 256, 8.5, 2.45, 2.1}};
-        switch (cheapest(kF32, 3, p, steps)) {
+        static const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6}, {128, 128, 256, 4.5, 1.36, 1.2}, {256, 128, 256, 8.5, 2.45, 2.1}, {64, 64, 256, 3.5, 0.55, 0.43, 2}};
+        // the wavefronts: a compute unit goes through a 32 x 32 block in 7.3 us per 1000 of k (14 shapes, 100 to 4100 blocks)
+        const long long blocks = (long long)((p.rows - 1) / 32 + 1) * ((p.Cout - 1) / 32 + 1);
+        const double us_waves = 4.0 + (double)((blocks + 255) / 256) * 0.0073 * p.Cin;
+        const int best = cheapest(kF32, 4, p, steps);
+        if (us_waves < tiling_us(kF32[best], p, steps)) return launch_wave<TI, TO, 32, 32, 8>(p, steps);
+        switch (best) {
             case 0: return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
             case 1: return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
-            default: return launch_tile<TI, TO, 256, 128, 4, 2, 1>(p);
+            case 2: return launch_tile<TI, TO, 256, 128, 4, 2, 1>(p);
+            default: return launch_tile<TI, TO, 64, 64, 2, 2, 2, 2>(p);
         }
     } else if (direct) {
         static const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29},  {128, 128, 256, 2.5, 0.57, 0.5}, {128, 128, 512, 4.4, 1.0, 0.75},

@@ -247,7 +247,9 @@ LINEAR_LARGE = [(1024, 2048, 1024), (2100, 1032, 1000), (3601, 328, 3584), (1300
                 (1500, 64, 700), (1500, 128, 700), (1500, 96, 1032), (1200, 256, 1024),
                 # bf16: two teams that share k, with and without a part step, ragged edges
                 (64, 1024, 1024), (70, 1032, 1000), (129, 264, 520), (33, 4096, 2050), (300, 2048, 300), (500, 4096, 4096), (490, 2056, 4001),
-                (20000, 256, 8), (200, 320, 400)]
+                (20000, 256, 8), (200, 320, 400),
+                # fp32: two teams, with an odd step and a part step left over
+                (729, 1536, 384), (1024, 1024, 1024), (1000, 992, 1000), (900, 1000, 999), (2146, 1057, 288)]
 
 
 @pytest.mark.parametrize("ti,to", TYPES)
@@ -281,7 +283,7 @@ def test_linear_far_magnitudes(sq, rows, cin, cout, spread):
 
 
 @pytest.mark.parametrize("ti,to", TYPES)
-@pytest.mark.parametrize("rows,cin,cout", [(3, 64, 40), (70, 128, 72), (300, 96, 264), (20, 45, 33), (300, 2048, 70)])
+@pytest.mark.parametrize("rows,cin,cout", [(3, 64, 40), (70, 128, 72), (300, 96, 264), (20, 45, 33), (300, 2048, 70), (1000, 992, 1000), (1100, 257, 1300)])
 def test_linear_infinities_and_nan(sq, rows, cin, cout, ti, to):
     """An infinity or NaN in a row or a kernel reaches what its products reach, and nothing else."""
     g = gen(70)
