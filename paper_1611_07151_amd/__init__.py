@@ -19,5 +19,5 @@ from .binding import (  # noqa: F401
     sq_blocked_maxpool, sq_blocked_avgpool_global, sq_squeezenet_bf16_packed_bytes,
     sq_squeezenet_bf16_pack_params, sq_squeezenet_bf16_workspace_bytes, sq_squeezenet_forward_bf16, sq_squeezenet_workspace_bytes, sq_strerror, TAP_NAMES, TAP_SHAPES,
     SQ_ACT_NONE, SQ_ACT_RELU, SQ_ACT_SILU, SQ_ACT_GELU, sq_nhwc_pack, sq_nhwc_unpack, sq_nhwc_group_norm,
-    sq_nhwc_group_norm_workspace_bytes, sq_linear_forward,
+    sq_nhwc_group_norm_workspace_bytes, sq_linear_forward, sq_linear_workspace_bytes,
     sq_tune_conv2d_forward_poolcols, sq_tune_fire_forward_poolcols, sq_tune_poolrows_conv2d_forward)

@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -94,7 +95,9 @@ lib.sq_nhwc_unpack.argtypes = [_vp, _i, _vp, _i] + [_i] * 7
 lib.sq_nhwc_group_norm_workspace_bytes.restype = _sz
 lib.sq_nhwc_group_norm_workspace_bytes.argtypes = [_i] * 5
 lib.sq_nhwc_group_norm.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 5 + [ctypes.c_float] + [_i] * 3 + [_vp, _sz]
-lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9
+lib.sq_linear_workspace_bytes.restype = _sz
+lib.sq_linear_workspace_bytes.argtypes = [_i] * 4
+lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9 + [_vp, _sz]
 
 lib.sq_profile_begin.argtypes = [_i]
 lib.sq_profile_get_mfma_flops.argtypes = [_i, ctypes.POINTER(ctypes.c_double)]
@@ -845,7 +848,16 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
     return out
 
 
-def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None):
+@functools.lru_cache(maxsize=4096)
+def _linear_need(rows, Cin, Cout, code):
+    return int(lib.sq_linear_workspace_bytes(rows, Cin, Cout, code))
+
+
+def sq_linear_workspace_bytes(rows, Cin, Cout, dtype=torch.float32) -> int:
+    return _linear_need(rows, Cin, Cout, _CODES[dtype])
+
+
+def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None, workspace=None):
     """act(x @ w.T + b) + residual.  x [..., Cin] and w [Cout][Cin] (a 1x1 convolution's [Cout][Cin][1][1] too), float32 or
     both bfloat16; b [Cout] float32 or None; out and residual [..., Cout] of out_dtype (default: that of x, residual or
     out).  `residual` may be `out` itself."""
@@ -872,9 +884,11 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
     rows = x.numel() // Cin if Cin else 0
     if rows > _MAX_INT or Cin > _MAX_INT or Cout > _MAX_INT:
         _check(-3, "sq_linear_forward")
+    code = _dtype_code(x, "x")
+    workspace, address, nbytes = _scratch(workspace, _linear_need(rows, Cin, Cout, code), x, index)
     _run(index, "sq_linear_forward", lib.sq_linear_forward, x.data_ptr(), _dense(w, "w", index, x.dtype),
-         _dense(b, "b", index, torch.float32), res, out.data_ptr(), _dtype_code(x, "x"), _dtype_code(out, "out"), rows, Cin, Cout,
-         int(act), ld_in, ld_res, ld_out)
+         _dense(b, "b", index, torch.float32), res, out.data_ptr(), code, _dtype_code(out, "out"), rows, Cin, Cout,
+         int(act), ld_in, ld_res, ld_out, address, nbytes)
     return out
 
 

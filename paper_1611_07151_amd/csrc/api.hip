@@ -1395,8 +1395,15 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
     return nhwc_group_norm(in, out, dtype, gamma, beta, N, C, (long long)H * W, G, eps, act, ld_in, ld_out, workspace, workspace_bytes);
 }
 
+size_t sq_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype)
+{
+    if (rows <= 0 || Cin <= 0 || Cout <= 0 || !known_dtype(in_dtype)) return 0;
+    return linear_workspace_bytes(rows, Cin, Cout, in_dtype);
+}
+
 int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out, sq_dtype in_dtype,
-                      sq_dtype out_dtype, int rows, int Cin, int Cout, int act, int ld_in, int ld_res, int ld_out)
+                      sq_dtype out_dtype, int rows, int Cin, int Cout, int act, int ld_in, int ld_res, int ld_out, void *workspace,
+                      size_t workspace_bytes)
 {
     if (!in || !w || !out) return SQ_ERR_NULL;
     if (rows <= 0 || Cin <= 0 || Cout <= 0 || ld_in < Cin || ld_out < Cout || (residual && ld_res < Cout)) return SQ_ERR_SHAPE;
@@ -1405,11 +1412,14 @@ int sq_linear_forward(const void *in, const void *w, const float *b, const void 
     if (!aligned_to(in, in_dtype) || !aligned_to(w, in_dtype) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype) ||
         !aligned_to(b, SQ_F32))
         return SQ_ERR_UNSUPPORTED;
-    LinearArgs a;
+    const size_t need = sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype);
+    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+    LinearArgs a{};
     a.in = in; a.w = w; a.b = b; a.residual = residual; a.out = out;
     a.in_dtype = in_dtype; a.out_dtype = out_dtype;
     a.rows = rows; a.Cin = Cin; a.Cout = Cout; a.act = act;
     a.ld_in = ld_in; a.ld_res = ld_res; a.ld_out = ld_out;
+    a.workspace = workspace;
     return linear(a);
 }
 

@@ -2,6 +2,7 @@
 #include "nhwc_common.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace sq {
 namespace {
@@ -96,6 +97,17 @@ __device__ __forceinline__ void tile_at(int b, int tiles, int tiles_r, int tiles
     tr = band * 8 + in_band - tj * high;
 }
 
+// The y-th workgroup of a tile takes the y-th share of k; with more than one, what it writes is its share's sums, each share
+// its own [rows][ld_out] in the workspace, which linear_join_kernel adds up.
+template <typename TI, typename TO> __device__ __forceinline__ void take_share(LinearArgs &p)
+{
+    const int first = blockIdx.y * p.share;
+    p.in = (const TI *)p.in + first;
+    p.w = (const TI *)p.w + first;
+    p.out = (TO *)p.out + (long long)blockIdx.y * p.rows * p.ld_out;
+    p.Cin = blockIdx.y + 1 < gridDim.y ? p.share : p.Cin - first;      // the last also what is left of k
+}
+
 // ---- few results: wavefronts that share out the sum ---------------------------------------------------------------
 // A workgroup makes CT layers of RT rows; its wavefronts share out k in pieces of 64 bytes of a row ("steps"), each
 // holding the whole RT x CT block of sums in registers, and add up through LDS, in order of wavefronts.  Operands go
@@ -119,7 +131,7 @@ __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, in
 #pragma unroll
     for (int i = 0; i < RB; ++i) xr[i] = (const TI *)p.in + row_at(r0, 16 * i + l16, p.rows) * p.ld_in + piece * kPiece;
 #pragma unroll
-    for (int i = 0; i < CB; ++i) wr[i] = (const TI *)p.w + row_at(j0, 16 * i + l16, p.Cout) * p.Cin + piece * kPiece;
+    for (int i = 0; i < CB; ++i) wr[i] = (const TI *)p.w + row_at(j0, 16 * i + l16, p.Cout) * p.ld_w + piece * kPiece;
     f32x4_t acc[CB][RB] = {};
     auto multiply = [&](const u32x4_t (&a)[CB], const u32x4_t (&b)[RB]) {
 #pragma unroll
@@ -290,6 +302,7 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
     u32x4_t *const lds = all + team * NS * kImage;
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
+    take_share<bf16_t, TO>(p);
     const int r0 = tr * BM, j0 = tj * BN;
     // Loads 0 to XI - 1 of a wavefront are rows of the input, the others of the kernels; load i takes rows 8 g to 8 g + 7, the
     // lane's row is lane / 8 and its place lane % 8.  Per load the lane's row and piece are a 32-bit offset from the
@@ -297,14 +310,14 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
     auto piece = [&](int i) { return (lane & 7) ^ (((wave * (i < XI ? XI : JI) + (i < XI ? i : i - XI)) & 1) * 4 + (lane >> 4)); };
     // the team's share of the whole steps, the same number for each
     const int whole = p.Cin / 64 / KS, tail = p.Cin % 64, k0 = 64 * whole * team;
-    const bf16_t *const x0 = (const bf16_t *)p.in + r0 * p.ld_in + k0, *const w0 = (const bf16_t *)p.w + (long long)j0 * p.Cin + k0;
+    const bf16_t *const x0 = (const bf16_t *)p.in + r0 * p.ld_in + k0, *const w0 = (const bf16_t *)p.w + j0 * p.ld_w + k0;
     const u32x4_t xr = {(uint32_t)(uintptr_t)x0, (uint32_t)((uintptr_t)x0 >> 32), 0xffffffffu, 0x00020000u};
     const u32x4_t wr = {(uint32_t)(uintptr_t)w0, (uint32_t)((uintptr_t)w0 >> 32), 0xffffffffu, 0x00020000u};
     uint32_t off[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
         off[i] = i < XI ? (uint32_t)(row_at(r0, (wave * XI + i) * 8 + (lane >> 3), p.rows) - r0) * (uint32_t)(2 * p.ld_in) + piece(i) * 16
-                        : (uint32_t)(row_at(j0, (wave * JI + i - XI) * 8 + (lane >> 3), p.Cout) - j0) * (uint32_t)(2 * p.Cin) + piece(i) * 16;
+                        : (uint32_t)(row_at(j0, (wave * JI + i - XI) * 8 + (lane >> 3), p.Cout) - j0) * (uint32_t)(2 * p.ld_w) + piece(i) * 16;
     auto place_of = [&](int i) { return i < XI ? (wave * XI + i) * 64 : BM * 8 + (wave * JI + i - XI) * 64; };
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4_t *)all) + team * (uint32_t)(NS * kImage * 16);
     // Load i of the step at k into an image.  As an instruction of its own, because the compiler would let every later read of
@@ -325,10 +338,13 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
     };
     // Step s lies in image s % NS.  The part of k behind the last whole step goes first, through registers, with zeros behind
     // its end, as step -1 in the last image.
-    if (tail) {         // by the last team; the others' share of it is zeros
-#pragma unroll 1
+    if (tail) {         // by the last team; the others' share of it is zeros.  A piece is whole or behind the end (Cin is a multiple of 8).
+        u32x4_t rest[NI];
+#pragma unroll
         for (int i = 0; i < NI; ++i)
-            lds[(NS - 1) * kImage + place_of(i) + lane] = load16_tail((const bf16_t *)((const char *)((i < XI ? x0 : w0) + 64 * whole) + off[i]), team == KS - 1 ? tail - piece(i) * 8 : 0);
+            rest[i] = team == KS - 1 && piece(i) * 8 < tail ? load16((const bf16_t *)((const char *)((i < XI ? x0 : w0) + 64 * whole) + off[i])) : u32x4_t{};
+#pragma unroll
+        for (int i = 0; i < NI; ++i) lds[(NS - 1) * kImage + place_of(i) + lane] = rest[i];
     }
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -477,6 +493,7 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
     u32x4_t *const lds = all + team * 2 * kImage;
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
+    take_share<TI, TO>(p);
     const int r0 = tr * BM, j0 = tj * BN;
     // KS teams share out the whole steps evenly; what is left of them and the part step are for the last team
     const int whole = p.Cin / kStep / KS, left = whole * KS * kStep, k0 = whole * kStep * team;
@@ -486,7 +503,7 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int r = row + i * 8 * NW;
-        src[i] = (i * 8 * NW < BM ? (const TI *)p.in + row_at(r0, r, p.rows) * p.ld_in : (const TI *)p.w + row_at(j0, r - BM, p.Cout) * p.Cin) + q * kPiece + k0;
+        src[i] = (i * 8 * NW < BM ? (const TI *)p.in + row_at(r0, r, p.rows) * p.ld_in : (const TI *)p.w + row_at(j0, r - BM, p.Cout) * p.ld_w) + q * kPiece + k0;
     }
     auto fetch = [&](u32x4_t (&to)[NP], int k) {
 #pragma unroll
@@ -652,6 +669,22 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
     write_rows<TO, XB, JB>(p, (float *)all + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
 }
 
+// ---- the shares' sums ----------------------------------------------------------------------------------------------
+// A thread adds up four neighbouring results of a row, in order of the shares, and finishes them.  In LinearArgs `in` is the
+// shares' sums in rows of ld_in, a multiple of four.  Bound by its launch.
+template <typename TO> __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p)
+{
+    const unsigned quads = (unsigned)(p.Cout - 1) / 4 + 1, e = blockIdx.x * 256 + threadIdx.x, r = e / quads;
+    if (r >= (unsigned)p.rows) return;
+    const int j = (int)(e - r * quads) * 4;
+    const float *at = (const float *)p.in + r * p.ld_in + j;
+    f32x4_t s = *(const f32x4_t *)at;
+#pragma unroll 4
+    for (int i = 1; i < p.shares; ++i) s += *(const f32x4_t *)(at + i * (p.rows * p.ld_in));
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    finish<TO>(p, r, j, p.Cout - j, v);
+}
+
 // ---- which of them ------------------------------------------------------------------------------------------------
 template <typename TI, typename TO, int RT, int CT, int MAXW> int launch_wave(const LinearArgs &p, int waves)
 {
@@ -668,7 +701,7 @@ template <typename TO, int BM, int BN, int WR, int WC, int NS, int KS = 1> int l
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
     if (!one_launch((double)tr * tj, 64 * WR * WC * KS)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_tile_bf16", linear_flops(p), linear_bytes(p));
-    hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC, NS, KS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC * KS), 0, current_stream(), p, tr, tj);
+    hipLaunchKernelGGL((linear_tile_bf16_kernel<TO, BM, BN, WR, WC, NS, KS>), dim3((unsigned)tr * tj, p.shares), dim3(64 * WR * WC * KS), 0, current_stream(), p, tr, tj);
     return check_launch();
 }
 
@@ -677,29 +710,34 @@ template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF, int 
     const int tr = (p.rows - 1) / BM + 1, tj = (p.Cout - 1) / BN + 1;
     if (!one_launch((double)tr * tj, 64 * WR * WC * KS)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_tile", linear_flops(p), linear_bytes(p), (sizeof(TI) == 4 ? 6.0 : 1.0) * linear_flops(p));
-    hipLaunchKernelGGL((linear_tile_kernel<TI, TO, BM, BN, WR, WC, PF, KS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC * KS), 0, current_stream(), p, tr, tj);
+    hipLaunchKernelGGL((linear_tile_kernel<TI, TO, BM, BN, WR, WC, PF, KS>), dim3((unsigned)tr * tj, p.shares), dim3(64 * WR * WC * KS), 0, current_stream(), p, tr, tj);
     return check_launch();
 }
 
 // Microseconds of a tiling, from what it measured (products of 128 to 8192 rows, layers and results): `fixed` for filling the
 // pipeline and writing the results, `step` for 128 bytes of k when `slots` workgroups share the chip, `alone` when each
 // has a compute unit to itself.
-struct Tiling { int BM, BN, slots; double fixed, step, alone; int teams = 0; };
-double tiling_us(const Tiling &t, const LinearArgs &p, int steps)
+struct Tiling { int BM, BN, slots; double fixed, step, alone; int teams; };
+double tiling_us(const Tiling &t, const LinearArgs &p, int Cin, int shares)
 {
-    const long long tiles = (long long)((p.rows - 1) / t.BM + 1) * ((p.Cout - 1) / t.BN + 1);
-    // through registers, the steps that teams cannot share evenly and the part step come one at a time
-    const int whole = p.Cin / 32, odd = p.in_dtype == SQ_F32 ? (t.teams ? whole % t.teams : 0) + (p.Cin % 32 != 0) : 0;
-    if (tiles <= 256) return t.fixed + t.alone * steps + 2.0 * odd;
-    return (double)((tiles + t.slots - 1) / t.slots) * (t.fixed + t.step * steps + odd);
+    const long long tiles = (long long)((p.rows - 1) / t.BM + 1) * ((p.Cout - 1) / t.BN + 1) * shares;
+    const int unit = p.in_dtype == SQ_F32 ? 32 : 64, whole = Cin / unit, steps = (Cin - 1) / unit + 1;
+    // fp32: the steps that teams cannot share evenly and the part step come one at a time
+    const int odd = p.in_dtype == SQ_F32 ? whole % t.teams + (Cin % unit != 0) : 0;
+    // full rounds of the chip, and a last one with fewer to a compute unit
+    auto round = [&](double step, double part) { return t.fixed + step * steps + part * odd; };
+    const long long full = tiles / t.slots, rest = tiles % t.slots;
+    const int each = (int)((rest + 255) / 256), most = t.slots / 256;
+    return full * round(t.step, 1.0) + (rest ? round(most == 1 ? t.alone : t.alone + (t.step - t.alone) * (each - 1) / (most - 1), each == 1 ? 2.0 : 1.0) : 0.0);
 }
-int cheapest(const Tiling *t, int n, const LinearArgs &p, int steps)
-{
-    int best = 0;
-    for (int i = 1; i < n; ++i)
-        if (tiling_us(t[i], p, steps) < tiling_us(t[best], p, steps)) best = i;
-    return best;
-}
+const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6, 1}, {128, 128, 256, 4.5, 1.36, 1.2, 1}, {256, 128, 256, 8.5, 2.45, 2.1, 1}, {64, 64, 256, 3.5, 0.55, 0.43, 2}};
+const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29, 1},  {128, 128, 256, 2.5, 0.57, 0.5, 1},  {128, 128, 512, 4.4, 1.0, 0.75, 1},
+                          {256, 256, 256, 9.0, 1.5, 1.25, 1}, {64, 64, 256, 2.5, 0.22, 0.19, 2}, {128, 64, 256, 3.5, 0.32, 0.3, 2}};
+const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45, 1}, {128, 128, 512, 4.0, 1.8, 0.85, 1}};
+
+// How a product is made: by wavefronts in blocks of 16 x 16 or 32 x 32, or by a tiling, with k in shares of `share` values.
+enum { kWave16 = -1, kWave32 = -2 };
+struct Plan { int which, share, shares; };
 
 // Few results: the wavefronts, in blocks of 16 x 16 up to 2^16 results, a short sum or 16 rows, else 32 x 32 (us, 16 / 32: 586 x
 // 1952 x 64 bf16 5.4 / 7.8, 99 x 3088 x 80 7.0 / 10.9; 45 x 1792 x 3520 12.9 / 9.5, 3458 x 2016 x 56 13.1 / 8.2).  Tiles through LDS
@@ -708,34 +746,69 @@ int cheapest(const Tiling *t, int n, const LinearArgs &p, int steps)
 // 11.9 / 17.8), 2^16 too where rows lie at any address (300 x 2049 x 300 27.7 / 16.1, 905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
 // 16.1 / 18.1), by estimate for fp32 (3506 x 416 x 1096 58 / 27, 1024^3 35 / 19, 729 x 1536 x 384 26.5 / 23.7; 300 x 2048 x 300 17.5 /
 // 27.8, 64 x 4096 x 4096 34 / 52).
-template <typename TI, typename TO> int by_size(const LinearArgs &p)
+// Where one workgroup's way through k leaves the chip idle, tiles in shares of k and a second launch that adds them up (4.5 us and
+// the sums' bytes), if that is to save 8 % (us, without / with: 300 x 4000 x 1000 fp32 50.5 / 26.6, 24 x 3691 x 3000 bf16 24.9 /
+// 11.7, 17 x 4096 x 4096 14.2 / 10.2; 42 x 728 x 7032 fp32 14.4 / 14.5, 64 x 1280 x 3712 bf16 7.0 / 8.8, 40 x 2500 x 150 6.2 / 9.1).
+Plan plan_of(const LinearArgs &p, bool direct)
 {
+    const bool f32 = p.in_dtype == SQ_F32;
     const double results = (double)p.rows * p.Cout;
-    const int steps = (int)(((long long)p.Cin * sizeof(TI) + 127) / 128);
-    // memory-to-LDS loads: whole 16-byte pieces, a tile's rows within 32-bit offsets
-    const bool direct = sizeof(TI) == 2 && p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
-                        p.ld_in < (1 << 22) && p.Cin < (1 << 22);
+    const int unit = f32 ? 32 : 64, steps = (p.Cin - 1) / unit + 1;
     const bool teams = direct && p.Cin / 64 % 2 == 0 && p.Cin >= 256;       // two teams share k evenly
+    const Tiling *const all = f32 ? kF32 : direct ? kDirect : kAny;
+    const int n = f32 ? 4 : direct ? (teams ? 6 : 4) : 2;
+    Plan best{0, p.Cin, 1};
+    double us = tiling_us(all[0], p, p.Cin, 1);
+    for (int i = 1; i < n; ++i) {
+        const double t = tiling_us(all[i], p, p.Cin, 1);
+        if (t < us) us = t, best.which = i;
+    }
+    // the wavefronts: us for 1000 of k, of a block by itself and of a full chip's 256 (30 products); bf16 rows that do not begin at
+    // whole 8 bytes take their loads in parts
+    const bool small = p.rows <= 16 || results <= 65536 || steps <= 2;
+    const int B = small ? 16 : 32;
+    const double blocks = ((p.rows - 1) / B + 1.0) * ((p.Cout - 1) / B + 1.0);
+    const double one = small ? (f32 ? 2.0 : p.Cin % 4 == 0 ? 1.0 : p.Cin % 2 == 0 ? 2.1 : 3.7) : (f32 ? 7.3 : direct ? 3.3 : 11.5);
+    const double all256 = small ? (f32 ? 3.5 : 1.6 * one) : one;
+    const double waves = 4.0 + std::max(std::ceil(blocks / 256) * one, blocks / 256 * all256) * p.Cin * 1e-3;
     const double many = direct && !teams ? 1 << 18 : 1 << 16;
-    if (p.rows <= 16 || results <= many || (sizeof(TI) == 4 && steps <= 2 && results < 1 << 20))
-        return p.rows <= 16 || results <= 65536 || steps <= 2 ? launch_wave<TI, TO, 16, 16, 16>(p, 2 * steps) : launch_wave<TI, TO, 32, 32, 8>(p, steps);
+    if (p.rows <= 16 || results <= many || (f32 && (waves < us || (steps <= 2 && results < 1 << 20)))) us = waves, best.which = small ? kWave16 : kWave32;
+    if (steps < 16) return best;
+    us *= 0.92;
+    for (int i = 0; i < n; ++i) {
+        const Tiling &t = all[i];
+        const double tiles = ((p.rows - 1) / t.BM + 1.0) * ((p.Cout - 1) / t.BN + 1.0);
+        const int units = p.Cin / (unit * t.teams);
+        for (int want = 2; want <= 16 && tiles * want <= 512; ++want) {
+            const int share = ((units - 1) / want + 1) * unit * t.teams, shares = (units * unit * t.teams - 1) / share + 1;
+            if (shares != want) continue;
+            const double join = 4.5 + results * shares * 8.0 / 5e6, cost = tiling_us(t, p, std::max(share, p.Cin - (shares - 1) * share), shares) + join;
+            if (cost < us) us = cost, best = Plan{i, share, shares};
+        }
+    }
+    return best;
+}
+
+// Memory-to-LDS loads: whole 16-byte pieces, a tile's rows within 32-bit offsets.
+bool direct_loads(const LinearArgs &p)
+{
+    return p.in_dtype == SQ_BF16 && p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
+           p.ld_in < (1 << 22) && p.Cin < (1 << 22);
+}
+// Rows of the shares' sums begin at whole lines.
+long long share_row(int Cout) { return ((long long)Cout + 31) / 32 * 32; }
+
+template <typename TI, typename TO> int launch_tiling(const LinearArgs &p, int which, bool direct)
+{
     if constexpr (sizeof(TI) == 4) {
-        static const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6}, {128, 128, 256, 4.5, 1.36, 1.2}, {256, 128, 256, 8.5, 2.45, 2.1}, {64, 64, 256, 3.5, 0.55, 0.43, 2}};
-        // the wavefronts: a compute unit goes through a 32 x 32 block in 7.3 us per 1000 of k (14 shapes, 100 to 4100 blocks)
-        const long long blocks = (long long)((p.rows - 1) / 32 + 1) * ((p.Cout - 1) / 32 + 1);
-        const double us_waves = 4.0 + (double)((blocks + 255) / 256) * 0.0073 * p.Cin;
-        const int best = cheapest(kF32, 4, p, steps);
-        if (us_waves < tiling_us(kF32[best], p, steps)) return launch_wave<TI, TO, 32, 32, 8>(p, steps);
-        switch (best) {
+        switch (which) {
             case 0: return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
             case 1: return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
             case 2: return launch_tile<TI, TO, 256, 128, 4, 2, 1>(p);
             default: return launch_tile<TI, TO, 64, 64, 2, 2, 2, 2>(p);
         }
     } else if (direct) {
-        static const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29},  {128, 128, 256, 2.5, 0.57, 0.5}, {128, 128, 512, 4.4, 1.0, 0.75},
-                                         {256, 256, 256, 9.0, 1.5, 1.25}, {64, 64, 256, 2.5, 0.22, 0.19}, {128, 64, 256, 3.5, 0.32, 0.3}};
-        switch (teams ? cheapest(kDirect, 6, p, steps) : cheapest(kDirect, 4, p, steps)) {
+        switch (which) {
             case 0: return launch_tile_bf16<TO, 64, 64, 2, 2, 4>(p);
             case 1: return launch_tile_bf16<TO, 128, 128, 2, 4, 4>(p);
             case 2: return launch_tile_bf16<TO, 128, 128, 2, 2, 2>(p);
@@ -744,10 +817,28 @@ template <typename TI, typename TO> int by_size(const LinearArgs &p)
             default: return launch_tile_bf16<TO, 128, 64, 2, 2, 3, 2>(p);
         }
     } else {
-        static const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45}, {128, 128, 512, 4.0, 1.8, 0.85}};
-        if (cheapest(kAny, 2, p, steps) == 0) return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
-        return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
+        return which == 0 ? launch_tile<TI, TO, 64, 64, 2, 2, 2>(p) : launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
     }
+}
+
+template <typename TI, typename TO> int by_size(LinearArgs p)
+{
+    const bool direct = direct_loads(p);
+    const Plan plan = plan_of(p, direct);
+    p.ld_w = p.Cin;
+    p.share = plan.share, p.shares = plan.shares;
+    if (plan.which == kWave16) return launch_wave<TI, TO, 16, 16, 16>(p, 2 * ((p.Cin - 1) / (128 / (int)sizeof(TI)) + 1));
+    if (plan.which == kWave32) return launch_wave<TI, TO, 32, 32, 8>(p, (p.Cin - 1) / (128 / (int)sizeof(TI)) + 1);
+    if (plan.shares == 1) return launch_tiling<TI, TO>(p, plan.which, direct);
+    LinearArgs part = p;
+    part.b = nullptr, part.residual = nullptr, part.act = SQ_ACT_NONE;
+    part.out = p.workspace, part.out_dtype = SQ_F32, part.ld_out = share_row(p.Cout);
+    if (const int rc = launch_tiling<TI, float>(part, plan.which, direct)) return rc;
+    p.in = p.workspace, p.ld_in = part.ld_out;
+    const unsigned threads = (unsigned)p.rows * ((unsigned)(p.Cout - 1) / 4 + 1);       // fewer than 512 tiles' results
+    const LaunchScope prof("linear_join", 0, 4.0 * plan.shares * p.rows * p.Cout + (sizeof(TO) * (p.residual ? 2.0 : 1.0)) * p.rows * p.Cout);
+    hipLaunchKernelGGL((linear_join_kernel<TO>), dim3((threads - 1) / 256 + 1), dim3(256), 0, current_stream(), p);
+    return check_launch();
 }
 
 }  // namespace
@@ -756,6 +847,15 @@ bool linear_register_kernels()
 {
     hipFuncAttributes a;
     return hipFuncGetAttributes(&a, (const void *)linear_wave_kernel<float, float, 16, 16, 16>) == hipSuccess;
+}
+
+size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype)
+{
+    LinearArgs p{};
+    p.rows = rows, p.Cin = Cin, p.Cout = Cout, p.in_dtype = in_dtype;
+    int shares = plan_of(p, false).shares;
+    if (in_dtype == SQ_BF16 && Cin % 8 == 0) shares = std::max(shares, plan_of(p, true).shares);      // whatever the addresses
+    return shares == 1 ? 0 : (size_t)shares * rows * share_row(Cout) * sizeof(float);
 }
 
 int linear(const LinearArgs &p)

@@ -219,7 +219,11 @@ struct LinearArgs {
     int in_dtype, out_dtype;      // of in and w; of residual and out
     int rows, Cin, Cout, act;
     long long ld_in, ld_res, ld_out;
+    void *workspace;
+    long long ld_w;               // of a row of w
+    int share, shares;            // of k: one workgroup's, and how many (1: no sums to join)
 };
+size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype);
 inline double linear_flops(const LinearArgs &a) { return 2.0 * a.rows * a.Cin * a.Cout; }
 inline double linear_bytes(const LinearArgs &a)
 {

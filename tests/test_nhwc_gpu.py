@@ -259,6 +259,65 @@ def test_linear_large(sq, rows, cin, cout, ti, to):
     linear_case(sq, rows, cin, cout, 0, ti, to, rows + cin, residual=(rows + cout) % 2 == 1, pads=(8, 3, 8))
 
 
+# k in shares and a second launch that adds them up: even shares, a short or long last one, part steps, rows at any address
+LINEAR_SHARES = [(17, 2056, 4000), (24, 3691, 3000), (33, 4095, 130), (300, 2048, 300), (130, 1111, 2000), (500, 2500, 150), (129, 4160, 999),
+                 (1000, 8200, 64), (17, 4099, 77), (729, 1536, 384), (200, 1992, 640), (257, 4000, 1000), (64, 5000, 2001)]
+
+
+@pytest.mark.parametrize("ti,to", TYPES)
+@pytest.mark.parametrize("rows,cin,cout", LINEAR_SHARES)
+def test_linear_in_shares_of_k(sq, rows, cin, cout, ti, to):
+    need = sq.sq_linear_workspace_bytes(rows, cin, cout, ti)
+    assert need or sq.sq_linear_workspace_bytes(rows, cin, cout, BF16 if ti is F32 else F32)
+    for act in (0, 3):
+        linear_case(sq, rows, cin, cout, act, ti, to, rows + cin, residual=act == 3, pads=(0, 3, 5) if act else (0, 0, 0))
+    linear_case(sq, rows, cin, cout, 1, ti, to, rows, pads=(8, 0, 8))
+    linear_case(sq, rows, cin, cout, 2, ti, to, rows, bias=False, pads=(1, 0, 0))
+    # a workspace of the caller's, full of NaN, with a guard behind it; and the same bits as with one of the binding's
+    x, w = torch.randn((rows, cin), generator=gen(1)).to(ti).cuda(), torch.randn((cout, cin), generator=gen(2)).to(ti).cuda()
+    space = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    got = sq.sq_linear_forward(x, w, out_dtype=to, workspace=space)
+    assert torch.equal(got, sq.sq_linear_forward(x, w, out_dtype=to)) and not got.isnan().any()
+    assert (space[need:] == 255).all()
+    if need:
+        with pytest.raises(RuntimeError):
+            sq.sq_linear_forward(x, w, out_dtype=to, workspace=space[:need - 1])
+        with pytest.raises(RuntimeError):
+            sq.sq_linear_forward(x, w, out_dtype=to, workspace=space[16:])
+    # in place, captured and replayed
+    out = torch.randn((rows, cout), generator=gen(3)).to(to).cuda()
+    first = out.clone()
+    want = sq.sq_linear_forward(x, w, act=3, residual=first)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        sq.sq_linear_forward(x, w, act=3, residual=out, out=out, workspace=space)
+    stream.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sq.sq_linear_forward(x, w, act=3, residual=out, out=out, workspace=space)
+    for _ in range(3):
+        out.copy_(first)
+        space.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rows,cin,cout", LINEAR_SHAPES[::4] + LINEAR_LARGE[::4] + LINEAR_SHARES[::3])
+@pytest.mark.parametrize("ti", (F32, BF16))
+def test_linear_stays_inside_its_workspace(sq, rows, cin, cout, ti):
+    """Whatever the addresses: rows of whole 16 bytes, and rows that begin at odd ones."""
+    need = sq.sq_linear_workspace_bytes(rows, cin, cout, ti)
+    space = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    w = torch.randn((cout, cin), generator=gen(2)).to(ti).cuda()
+    for pad in (0, 1):
+        _, x = wide(torch.randn((rows, cin), generator=gen(1)), pad, pad, ti)
+        sq.sq_linear_forward(x, w, workspace=space)
+        assert (space[need:] == 255).all()
+
+
 @pytest.mark.parametrize("ti,to", TYPES)
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("rows,cin,cout", [(3, 64, 40), (70, 128, 72), (600, 64, 264)])
@@ -283,7 +342,8 @@ def test_linear_far_magnitudes(sq, rows, cin, cout, spread):
 
 
 @pytest.mark.parametrize("ti,to", TYPES)
-@pytest.mark.parametrize("rows,cin,cout", [(3, 64, 40), (70, 128, 72), (300, 96, 264), (20, 45, 33), (300, 2048, 70), (1000, 992, 1000), (1100, 257, 1300)])
+@pytest.mark.parametrize("rows,cin,cout", [(3, 64, 40), (70, 128, 72), (300, 96, 264), (20, 45, 33), (300, 2048, 70), (1000, 992, 1000), (1100, 257, 1300),
+                                           (70, 4000, 1000), (130, 1111, 2000), (24, 3691, 700)])
 def test_linear_infinities_and_nan(sq, rows, cin, cout, ti, to):
     """An infinity or NaN in a row or a kernel reaches what its products reach, and nothing else."""
     g = gen(70)

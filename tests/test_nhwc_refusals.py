@@ -19,6 +19,8 @@ def lib():
     i, vp = ctypes.c_int, ctypes.c_void_p
     l.sq_nhwc_group_norm.argtypes = [vp, vp, i, vp, vp] + [i] * 5 + [ctypes.c_float] + [i] * 3 + [vp, SZ]
     l.sq_nhwc_group_norm_workspace_bytes.restype = SZ
+    l.sq_linear_forward.argtypes = [vp] * 5 + [i] * 9 + [vp, SZ]
+    l.sq_linear_workspace_bytes.restype = SZ
     return l
 
 
@@ -61,14 +63,20 @@ def test_group_norm(lib):
 
 
 def test_linear(lib):
-    def f(inp=P, w=P, b=P, res=P, out=P, ti=0, to=0, rows=8, cin=16, cout=24, act=0, ldi=16, ldr=24, ldo=24):
-        return lib.sq_linear_forward(inp, w, b, res, out, ti, to, rows, cin, cout, act, ldi, ldr, ldo)
+    def f(inp=P, w=P, b=P, res=P, out=P, ti=0, to=0, rows=8, cin=16, cout=24, act=0, ldi=16, ldr=24, ldo=24, ws=NULL, nb=0):
+        return lib.sq_linear_forward(inp, w, b, res, out, ti, to, rows, cin, cout, act, ldi, ldr, ldo, ws, nb)
     assert f(inp=NULL) == -1 and f(w=NULL) == -1 and f(out=NULL) == -1
     for k in ("rows", "cin", "cout"):
         assert f(**{k: 0}) == -2 and f(**{k: -1}) == -2
     assert f(ldi=15) == -2 and f(ldr=23) == -2 and f(ldo=23) == -2
     assert f(ti=2) == -3 and f(to=2) == -3 and f(ti=0, to=1) == -3 and f(act=4) == -3 and f(act=-1) == -3
     assert f(inp=ODD) == -3 and f(w=ODD) == -3 and f(b=ODD) == -3 and f(res=ODD) == -3 and f(out=ctypes.c_void_p(0x1002)) == -3
+    for bad in ((0, 16, 24, 0), (8, 0, 24, 0), (8, 16, -1, 0), (8, 16, 24, 2)):
+        assert lib.sq_linear_workspace_bytes(*bad) == 0
+    long = dict(rows=300, cin=2048, cout=300, ldi=2048, ldr=300, ldo=300)
+    need = lib.sq_linear_workspace_bytes(300, 2048, 300, 0)
+    assert need > 0
+    assert f(**long) == -4 and f(**long, ws=P, nb=need - 1) == -4 and f(**long, ws=ctypes.c_void_p(0x1010), nb=need) == -4
     # more threads than a launch has
     assert f(rows=2**31 - 1, cin=1, cout=2**31 - 1, ldi=1, ldr=2**31 - 1, ldo=2**31 - 1) == -3
 
