@@ -831,7 +831,8 @@ def sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups) -> int:
 
 def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NONE, out=None, workspace=None):
     """Group norm with an activation on a channels-last map [N][H][W][C] (float32 or bfloat16); gamma, beta [C] float32 or
-    None.  `out` may be m itself."""
+    None.  `out` may be m itself.  `workspace`: sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups) bytes on the same GPU, which
+    no other call may use at the time; without it the call takes what it needs from torch."""
     N, H, W, C = m.shape
     index = _gpu_of(m, "m")
     if out is None:
@@ -854,13 +855,16 @@ def _linear_need(rows, Cin, Cout, code):
 
 
 def sq_linear_workspace_bytes(rows, Cin, Cout, dtype=torch.float32) -> int:
+    if dtype not in _CODES:
+        raise ValueError("dtype must be float32 or bfloat16")
     return _linear_need(rows, Cin, Cout, _CODES[dtype])
 
 
 def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None, workspace=None):
     """act(x @ w.T + b) + residual.  x [..., Cin] and w [Cout][Cin] (a 1x1 convolution's [Cout][Cin][1][1] too), float32 or
     both bfloat16; b [Cout] float32 or None; out and residual [..., Cout] of out_dtype (default: that of x, residual or
-    out).  `residual` may be `out` itself."""
+    out).  `residual` may be `out` itself.  `workspace`: sq_linear_workspace_bytes(rows, Cin, Cout, x.dtype) bytes on the same
+    GPU, which no other call may use at the time; without it the call takes what it needs from torch."""
     index = _gpu_of(x, "x")
     *outer, Cin = x.shape
     Cout, *rest = w.shape

@@ -1352,13 +1352,15 @@ namespace {
 bool known_dtype(int d) { return d == SQ_F32 || d == SQ_BF16; }
 bool aligned_to(const void *p, int dtype) { return ((uintptr_t)p & (dtype == SQ_BF16 ? 1 : 3)) == 0; }
 bool known_act(int act) { return act >= SQ_ACT_NONE && act <= SQ_ACT_GELU; }
+// more values than there is memory for, and than the sizes derived from them can hold
+bool no_such_map(int N, int C, int H, int W) { return (double)N * C * H * W > 1e15; }
 }  // namespace
 
 int sq_nhwc_pack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dtype, int N, int C, int H, int W, int ld_out)
 {
     if (!in || !out) return SQ_ERR_NULL;
     if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || ld_out < C) return SQ_ERR_SHAPE;
-    if (!known_dtype(in_dtype) || !known_dtype(out_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (!known_dtype(in_dtype) || !known_dtype(out_dtype) || no_such_map(N, C, H, W)) return SQ_ERR_UNSUPPORTED;
     if (!aligned_to(in, in_dtype) || !aligned_to(out, out_dtype)) return SQ_ERR_UNSUPPORTED;
     return nhwc_pack(in, in_dtype, out, out_dtype, N, C, (long long)H * W, ld_out);
 }
@@ -1369,7 +1371,7 @@ int sq_nhwc_unpack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dt
     if (!in || !out) return SQ_ERR_NULL;
     if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || ld_in < C) return SQ_ERR_SHAPE;
     if (c_offset < 0 || out_channels < C || c_offset > out_channels - C) return SQ_ERR_SHAPE;
-    if (!known_dtype(in_dtype) || !known_dtype(out_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (!known_dtype(in_dtype) || !known_dtype(out_dtype) || no_such_map(N, C, H, W)) return SQ_ERR_UNSUPPORTED;
     if (!aligned_to(in, in_dtype) || !aligned_to(out, out_dtype)) return SQ_ERR_UNSUPPORTED;
     char *first = (char *)out + (size_t)c_offset * H * W * (out_dtype == SQ_BF16 ? 2 : 4);
     return nhwc_unpack(in, in_dtype, first, out_dtype, N, C, (long long)H * W, ld_in, out_channels);
@@ -1377,7 +1379,7 @@ int sq_nhwc_unpack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dt
 
 size_t sq_nhwc_group_norm_workspace_bytes(int N, int C, int H, int W, int G)
 {
-    if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || G <= 0 || C % G) return 0;
+    if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || G <= 0 || C % G || no_such_map(N, C, H, W)) return 0;
     return nhwc_group_norm_workspace_bytes(N, C, (long long)H * W, G);
 }
 
@@ -1387,7 +1389,7 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
     if (!in || !out) return SQ_ERR_NULL;
     if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || G <= 0 || C % G || ld_in < C || ld_out < C) return SQ_ERR_SHAPE;
     if (!(eps >= 0.f)) return SQ_ERR_SHAPE;
-    if (!known_dtype(dtype) || !known_act(act)) return SQ_ERR_UNSUPPORTED;
+    if (!known_dtype(dtype) || !known_act(act) || no_such_map(N, C, H, W)) return SQ_ERR_UNSUPPORTED;
     if (!aligned_to(in, dtype) || !aligned_to(out, dtype) || !aligned_to(gamma, SQ_F32) || !aligned_to(beta, SQ_F32))
         return SQ_ERR_UNSUPPORTED;
     const size_t need = sq_nhwc_group_norm_workspace_bytes(N, C, H, W, G);

@@ -768,7 +768,7 @@ Plan plan_of(const LinearArgs &p, bool direct)
     const bool small = p.rows <= 16 || results <= 65536 || steps <= 2;
     const int B = small ? 16 : 32;
     const double blocks = ((p.rows - 1) / B + 1.0) * ((p.Cout - 1) / B + 1.0);
-    const double one = small ? (f32 ? 2.0 : p.Cin % 4 == 0 ? 1.0 : p.Cin % 2 == 0 ? 2.1 : 3.7) : (f32 ? 7.3 : direct ? 3.3 : 11.5);
+    const double one = small ? (f32 ? 2.0 : p.Cin % 4 == 0 ? 1.0 : p.Cin % 2 == 0 ? 2.1 : 3.7) : (f32 ? 7.3 : 3.3);
     const double all256 = small ? (f32 ? 3.5 : 1.6 * one) : one;
     const double waves = 4.0 + std::max(std::ceil(blocks / 256) * one, blocks / 256 * all256) * p.Cin * 1e-3;
     const double many = direct && !teams ? 1 << 18 : 1 << 16;

@@ -81,11 +81,24 @@ def test_linear(lib):
     assert f(rows=2**31 - 1, cin=1, cout=2**31 - 1, ldi=1, ldr=2**31 - 1, ldo=2**31 - 1) == -3
 
 
+def test_sizes_whose_products_pass_64_bits(lib):
+    m = 2**31 - 1
+    lib.sq_nhwc_pack.argtypes = [ctypes.c_void_p, ctypes.c_int] * 2 + [ctypes.c_int] * 5
+    lib.sq_nhwc_unpack.argtypes = [ctypes.c_void_p, ctypes.c_int] * 2 + [ctypes.c_int] * 7
+    for n, c, h, w in ((m, m, m, m), (1, 64, m, m), (1, 256, 2**30, 2**30), (2**16, 2**16, 2**16, 2**16), (1, 1, m, m)):
+        assert lib.sq_nhwc_pack(P, 0, P, 1, n, c, h, w, c) == -3
+        assert lib.sq_nhwc_unpack(P, 1, P, 0, n, c, h, w, c, c, 0) == -3
+        assert lib.sq_nhwc_group_norm_workspace_bytes(n, c, h, w, 1) == 0
+        assert lib.sq_nhwc_group_norm(P, P, 0, NULL, NULL, n, c, h, w, 1, 1e-5, 0, c, c, P, 2**62) == -3
+
+
 def test_the_binding_checks_its_tensors():
     import paper_1611_07151_amd as sq
     x, w = torch.zeros((4, 8)), torch.zeros((6, 8))
     with pytest.raises(ValueError):
         sq.sq_linear_forward(x, w)                                    # not on the GPU
+    with pytest.raises(ValueError):
+        sq.sq_linear_workspace_bytes(4, 8, 6, torch.float16)
     with pytest.raises(ValueError):
         sq.sq_linear_forward(x, torch.zeros((6, 7)))                  # other row length
     with pytest.raises(ValueError):
