@@ -558,13 +558,14 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
  *     each operand as the exact sum of three bfloat16 values and fp32 sums: the error stays that of fp32
  *     sums of the same terms, except that operands below 2^-110 in magnitude keep fewer bits.  An
  *     infinity or NaN reaches the results of its row or kernel and no others.
- *   workspace: sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype) bytes of device scratch, 256-byte
- *     aligned (else SQ_ERR_WORKSPACE; 0 = none is needed, workspace may be NULL).  Contents on return
- *     are unspecified; two calls in flight at once need two.
+ *   workspace: sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype, ld_in, aligned) bytes of device
+ *     scratch, with aligned = whether in and w both begin at multiples of 16 bytes; 256-byte aligned
+ *     (else SQ_ERR_WORKSPACE; 0 = none is needed, workspace may be NULL).  Contents on return are
+ *     unspecified; two calls in flight at once need two.
  *   The same call gives the same bits every time.
  * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP.
  */
-size_t sq_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype);
+size_t sq_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype, int ld_in, int aligned);
 int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out,
                       sq_dtype in_dtype, sq_dtype out_dtype, int rows, int Cin, int Cout, int act,
                       int ld_in, int ld_res, int ld_out, void *workspace, size_t workspace_bytes);

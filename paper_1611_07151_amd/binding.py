@@ -96,7 +96,7 @@ lib.sq_nhwc_group_norm_workspace_bytes.restype = _sz
 lib.sq_nhwc_group_norm_workspace_bytes.argtypes = [_i] * 5
 lib.sq_nhwc_group_norm.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 5 + [ctypes.c_float] + [_i] * 3 + [_vp, _sz]
 lib.sq_linear_workspace_bytes.restype = _sz
-lib.sq_linear_workspace_bytes.argtypes = [_i] * 4
+lib.sq_linear_workspace_bytes.argtypes = [_i] * 6
 lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9 + [_vp, _sz]
 
 lib.sq_profile_begin.argtypes = [_i]
@@ -850,21 +850,24 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
 
 
 @functools.lru_cache(maxsize=4096)
-def _linear_need(rows, Cin, Cout, code):
-    return int(lib.sq_linear_workspace_bytes(rows, Cin, Cout, code))
+def _linear_need(rows, Cin, Cout, code, ld_in, aligned):
+    return int(lib.sq_linear_workspace_bytes(rows, Cin, Cout, code, ld_in, aligned))
 
 
-def sq_linear_workspace_bytes(rows, Cin, Cout, dtype=torch.float32) -> int:
+def sq_linear_workspace_bytes(rows, Cin, Cout, dtype=torch.float32, ld_in=None, aligned=None) -> int:
+    """Bytes for rows `ld_in` values apart (default: Cin), `aligned`: x and w both begin at multiples of 16 bytes (default:
+    the most that either takes)."""
     if dtype not in _CODES:
         raise ValueError("dtype must be float32 or bfloat16")
-    return _linear_need(rows, Cin, Cout, _CODES[dtype])
+    ld_in = Cin if ld_in is None else ld_in
+    return max(_linear_need(rows, Cin, Cout, _CODES[dtype], ld_in, bool(a)) for a in ((True, False) if aligned is None else (aligned,)))
 
 
 def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None, workspace=None):
     """act(x @ w.T + b) + residual.  x [..., Cin] and w [Cout][Cin] (a 1x1 convolution's [Cout][Cin][1][1] too), float32 or
     both bfloat16; b [Cout] float32 or None; out and residual [..., Cout] of out_dtype (default: that of x, residual or
-    out).  `residual` may be `out` itself.  `workspace`: sq_linear_workspace_bytes(rows, Cin, Cout, x.dtype) bytes on the same
-    GPU, which no other call may use at the time; without it the call takes what it needs from torch."""
+    out).  `residual` may be `out` itself.  `workspace`: sq_linear_workspace_bytes() bytes on the same GPU,
+    which no other call may use at the time; without it the call takes what it needs from torch."""
     index = _gpu_of(x, "x")
     *outer, Cin = x.shape
     Cout, *rest = w.shape
@@ -888,9 +891,10 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
     rows = x.numel() // Cin if Cin else 0
     if rows > _MAX_INT or Cin > _MAX_INT or Cout > _MAX_INT:
         _check(-3, "sq_linear_forward")
-    code = _dtype_code(x, "x")
-    workspace, address, nbytes = _scratch(workspace, _linear_need(rows, Cin, Cout, code), x, index)
-    _run(index, "sq_linear_forward", lib.sq_linear_forward, x.data_ptr(), _dense(w, "w", index, x.dtype),
+    code, x_at, w_at = _dtype_code(x, "x"), x.data_ptr(), _dense(w, "w", index, x.dtype)
+    need = _linear_need(rows, Cin, Cout, code, ld_in, (x_at | w_at) & 15 == 0)
+    workspace, address, nbytes = _scratch(workspace, need, x, index)
+    _run(index, "sq_linear_forward", lib.sq_linear_forward, x_at, w_at,
          _dense(b, "b", index, torch.float32), res, out.data_ptr(), code, _dtype_code(out, "out"), rows, Cin, Cout,
          int(act), ld_in, ld_res, ld_out, address, nbytes)
     return out

@@ -1397,10 +1397,10 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
     return nhwc_group_norm(in, out, dtype, gamma, beta, N, C, (long long)H * W, G, eps, act, ld_in, ld_out, workspace, workspace_bytes);
 }
 
-size_t sq_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype)
+size_t sq_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype, int ld_in, int aligned)
 {
-    if (rows <= 0 || Cin <= 0 || Cout <= 0 || !known_dtype(in_dtype)) return 0;
-    return linear_workspace_bytes(rows, Cin, Cout, in_dtype);
+    if (rows <= 0 || Cin <= 0 || Cout <= 0 || ld_in < Cin || !known_dtype(in_dtype)) return 0;
+    return linear_workspace_bytes(rows, Cin, Cout, in_dtype, ld_in, aligned != 0);
 }
 
 int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out, sq_dtype in_dtype,
@@ -1414,7 +1414,7 @@ int sq_linear_forward(const void *in, const void *w, const float *b, const void 
     if (!aligned_to(in, in_dtype) || !aligned_to(w, in_dtype) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype) ||
         !aligned_to(b, SQ_F32))
         return SQ_ERR_UNSUPPORTED;
-    const size_t need = sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype);
+    const size_t need = sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype, ld_in, (((uintptr_t)in | (uintptr_t)w) & 15) == 0);
     if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
     LinearArgs a{};
     a.in = in; a.w = w; a.b = b; a.residual = residual; a.out = out;

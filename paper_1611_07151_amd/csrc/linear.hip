@@ -790,10 +790,9 @@ Plan plan_of(const LinearArgs &p, bool direct)
 }
 
 // Memory-to-LDS loads: whole 16-byte pieces, a tile's rows within 32-bit offsets.
-bool direct_loads(const LinearArgs &p)
+bool direct_loads(int in_dtype, int Cin, long long ld_in, bool aligned)
 {
-    return p.in_dtype == SQ_BF16 && p.Cin % 8 == 0 && p.ld_in % 8 == 0 && ((uintptr_t)p.in & 15) == 0 && ((uintptr_t)p.w & 15) == 0 &&
-           p.ld_in < (1 << 22) && p.Cin < (1 << 22);
+    return in_dtype == SQ_BF16 && Cin % 8 == 0 && ld_in % 8 == 0 && aligned && ld_in < (1 << 22) && Cin < (1 << 22);
 }
 // Rows of the shares' sums begin at whole lines.
 long long share_row(int Cout) { return ((long long)Cout + 31) / 32 * 32; }
@@ -823,7 +822,7 @@ template <typename TI, typename TO> int launch_tiling(const LinearArgs &p, int w
 
 template <typename TI, typename TO> int by_size(LinearArgs p)
 {
-    const bool direct = direct_loads(p);
+    const bool direct = direct_loads(p.in_dtype, p.Cin, p.ld_in, (((uintptr_t)p.in | (uintptr_t)p.w) & 15) == 0);
     const Plan plan = plan_of(p, direct);
     p.ld_w = p.Cin;
     p.share = plan.share, p.shares = plan.shares;
@@ -849,12 +848,11 @@ bool linear_register_kernels()
     return hipFuncGetAttributes(&a, (const void *)linear_wave_kernel<float, float, 16, 16, 16>) == hipSuccess;
 }
 
-size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype)
+size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype, long long ld_in, bool aligned)
 {
     LinearArgs p{};
     p.rows = rows, p.Cin = Cin, p.Cout = Cout, p.in_dtype = in_dtype;
-    int shares = plan_of(p, false).shares;
-    if (in_dtype == SQ_BF16 && Cin % 8 == 0) shares = std::max(shares, plan_of(p, true).shares);      // whatever the addresses
+    const int shares = plan_of(p, direct_loads(in_dtype, Cin, ld_in, aligned)).shares;
     return shares == 1 ? 0 : (size_t)shares * rows * share_row(Cout) * sizeof(float);
 }
 

@@ -223,7 +223,7 @@ struct LinearArgs {
     long long ld_w;               // of a row of w
     int share, shares;            // of k: one workgroup's, and how many (1: no sums to join)
 };
-size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype);
+size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype, long long ld_in, bool aligned);
 inline double linear_flops(const LinearArgs &a) { return 2.0 * a.rows * a.Cin * a.Cout; }
 inline double linear_bytes(const LinearArgs &a)
 {

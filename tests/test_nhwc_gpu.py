@@ -267,8 +267,8 @@ LINEAR_SHARES = [(17, 2056, 4000), (24, 3691, 3000), (33, 4095, 130), (300, 2048
 @pytest.mark.parametrize("ti,to", TYPES)
 @pytest.mark.parametrize("rows,cin,cout", LINEAR_SHARES)
 def test_linear_in_shares_of_k(sq, rows, cin, cout, ti, to):
-    need = sq.sq_linear_workspace_bytes(rows, cin, cout, ti)
-    assert need or sq.sq_linear_workspace_bytes(rows, cin, cout, BF16 if ti is F32 else F32)
+    need = sq.sq_linear_workspace_bytes(rows, cin, cout, ti, cin, True)
+    assert any(sq.sq_linear_workspace_bytes(rows, cin, cout, t) for t in (F32, BF16))
     for act in (0, 3):
         linear_case(sq, rows, cin, cout, act, ti, to, rows + cin, residual=act == 3, pads=(0, 3, 5) if act else (0, 0, 0))
     linear_case(sq, rows, cin, cout, 1, ti, to, rows, pads=(8, 0, 8))
@@ -309,11 +309,12 @@ def test_linear_in_shares_of_k(sq, rows, cin, cout, ti, to):
 @pytest.mark.parametrize("ti", (F32, BF16))
 def test_linear_stays_inside_its_workspace(sq, rows, cin, cout, ti):
     """Whatever the addresses: rows of whole 16 bytes, and rows that begin at odd ones."""
-    need = sq.sq_linear_workspace_bytes(rows, cin, cout, ti)
-    space = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
     w = torch.randn((cout, cin), generator=gen(2)).to(ti).cuda()
     for pad in (0, 1):
         _, x = wide(torch.randn((rows, cin), generator=gen(1)), pad, pad, ti)
+        need = sq.sq_linear_workspace_bytes(rows, cin, cout, ti, cin + 2 * pad, pad == 0)
+        assert need <= sq.sq_linear_workspace_bytes(rows, cin, cout, ti)
+        space = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
         sq.sq_linear_forward(x, w, workspace=space)
         assert (space[need:] == 255).all()
 

@@ -71,10 +71,10 @@ def test_linear(lib):
     assert f(ldi=15) == -2 and f(ldr=23) == -2 and f(ldo=23) == -2
     assert f(ti=2) == -3 and f(to=2) == -3 and f(ti=0, to=1) == -3 and f(act=4) == -3 and f(act=-1) == -3
     assert f(inp=ODD) == -3 and f(w=ODD) == -3 and f(b=ODD) == -3 and f(res=ODD) == -3 and f(out=ctypes.c_void_p(0x1002)) == -3
-    for bad in ((0, 16, 24, 0), (8, 0, 24, 0), (8, 16, -1, 0), (8, 16, 24, 2)):
+    for bad in ((0, 16, 24, 0, 16, 1), (8, 0, 24, 0, 16, 1), (8, 16, -1, 0, 16, 1), (8, 16, 24, 2, 16, 1), (300, 2048, 300, 0, 2047, 1)):
         assert lib.sq_linear_workspace_bytes(*bad) == 0
     long = dict(rows=300, cin=2048, cout=300, ldi=2048, ldr=300, ldo=300)
-    need = lib.sq_linear_workspace_bytes(300, 2048, 300, 0)
+    need = lib.sq_linear_workspace_bytes(300, 2048, 300, 0, 2048, 1)
     assert need > 0
     assert f(**long) == -4 and f(**long, ws=P, nb=need - 1) == -4 and f(**long, ws=ctypes.c_void_p(0x1010), nb=need) == -4
     # more threads than a launch has
