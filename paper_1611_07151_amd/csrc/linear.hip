@@ -287,7 +287,7 @@ template <typename TO, int XB, int JB> __device__ __forceinline__ void write_row
 // cycles of every read were conflicts).  NS images of a step in LDS, loaded from memory directly; up to NS steps are on
 // their way or in use.
 // Bound by the matrix unit, which a large product keeps busy two thirds of the cycles at the clock that its power leaves (1.8 GHz):
-// 8192^3 in 805 us (1365 TFLOP/s); 16224 x 4096 x 4096 in 411 us (1326), with GELU and residual 475.  What is left is one
+// 8192^3 in 796 us (1381 TFLOP/s); 16224 x 4096 x 4096 in 402 us (1354), with GELU and residual 463.  What is left is one
 // barrier a step and the time it takes the wavefronts to come out of it.
 // KS teams of WR x WC wavefronts share out k for results that are too few to fill the chip with tiles, where what bounds a
 // tile is the latency of its steps: 128 x 4096 x 4096 19.8 -> 14.8 us, 729 x 1536 x 384 9.5 -> 7.7 (64 x 64 tiles, two teams).
@@ -773,8 +773,8 @@ Plan plan_of(const LinearArgs &p, bool direct)
     const double waves = 4.0 + std::max(std::ceil(blocks / 256) * one, blocks / 256 * all256) * p.Cin * 1e-3;
     const double many = direct && !teams ? 1 << 18 : 1 << 16;
     if (p.rows <= 16 || results <= many || (f32 && (waves < us || (steps <= 2 && results < 1 << 20)))) us = waves, best.which = small ? kWave16 : kWave32;
-    if (steps < 16) return best;
     us *= 0.92;
+    if (steps < 16 || us < 4.5 + 1.9) return best;
     for (int i = 0; i < n; ++i) {
         const Tiling &t = all[i];
         const double tiles = ((p.rows - 1) / t.BM + 1.0) * ((p.Cout - 1) / t.BN + 1.0);
