@@ -825,6 +825,7 @@ def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
     return out
 
 
+@functools.lru_cache(maxsize=4096)      # a function of the sizes alone
 def sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups) -> int:
     return int(lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups))
 
@@ -842,14 +843,14 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
     if gamma is not None and gamma.numel() != C or beta is not None and beta.numel() != C:
         raise ValueError("gamma and beta must have one value per layer")
     ld_in, ld_out, groups = _rows_of(m, "m", index), _rows_of(out, "out", index), int(groups)
-    workspace, address, nbytes = _scratch(workspace, lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups), m, index)
+    workspace, address, nbytes = _scratch(workspace, sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups), m, index)
     _run(index, "sq_nhwc_group_norm", lib.sq_nhwc_group_norm, m.data_ptr(), out.data_ptr(), _dtype_code(m, "m"),
          _dense(gamma, "gamma", index, torch.float32), _dense(beta, "beta", index, torch.float32), N, C, H, W, groups, eps,
          int(act), ld_in, ld_out, address, nbytes)
     return out
 
 
-@functools.lru_cache(maxsize=4096)
+@functools.lru_cache(maxsize=4096)      # a function of the sizes alone
 def _linear_need(rows, Cin, Cout, code, ld_in, aligned):
     return int(lib.sq_linear_workspace_bytes(rows, Cin, Cout, code, ld_in, aligned))
 

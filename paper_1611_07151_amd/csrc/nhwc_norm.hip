@@ -8,7 +8,7 @@
 // Else a launch for (mean, sum of squared deviations) per chunk, which are combined as
 //   mean = sum n_i mean_i / m,  M2 = sum M2_i + n_i (mean_i - mean)^2,
 // and one for the result, which reads x again (from the last-level cache where it fits its 256 MB).
-// Measured: 13 x 13 x 512 fp32 5.5 us, 16 x 27 x 27 x 384 bf16 10.8 us (launch and two sums across a workgroup), 64 x 55 x 55 x 256
+// Measured: 13 x 13 x 512 fp32 5.2 us, 16 x 27 x 27 x 384 bf16 10.2 us (launch and two sums across a workgroup), 64 x 55 x 55 x 256
 // fp32 105 us (3.8 TB/s) in one launch; 64 x 111 x 111 x 96 bf16 with SiLU 80 us in two (5.7 TB/s for what they move, 3.7 for x and
 // the result once; in one launch 126 us: one workgroup a compute unit, whose loads, arithmetic and stores follow each other).
 #include "nhwc_common.h"
@@ -150,10 +150,31 @@ __device__ __forceinline__ int team_shift(int groups, int work)
     while (shift < 6 && (groups << (shift + 1)) <= (int)blockDim.x && (1 << shift) < work) ++shift;
     return shift;
 }
-// the sum over a team, whose threads are all here
+// the sum over a team, whose threads are all here: within 16 lanes by the operand's own lane moves, beyond by exchanging rows of
+// lanes (through LDS each of the six steps would wait for it: 16 x 27 x 27 x 384 bfloat16 10.8 us instead of 10.2)
+template <int control> __device__ __forceinline__ float plus_moved(float v)
+{
+    const int u = __builtin_bit_cast(int, v);
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, control, 0xf, 0xf, false));
+}
 __device__ __forceinline__ float team_sum(float v, int shift)
 {
-    for (int d = (1 << shift) >> 1; d; d >>= 1) v += __shfl_xor(v, d);
+    if (shift > 0) v = plus_moved<0xb1>(v);        // lane ^ 1
+    if (shift > 1) v = plus_moved<0x4e>(v);        // lane ^ 2
+    if (shift > 2) v = plus_moved<0x141>(v);       // lane ^ 7: the other four of eight, which hold one sum by now
+    if (shift > 3) v = plus_moved<0x140>(v);       // lane ^ 15
+    if (shift > 4) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, v);
+        const auto both = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        const uint32_t a = both[0], b = both[1];
+        v = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+    }
+    if (shift > 5) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, v);
+        const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        const uint32_t a = both[0], b = both[1];
+        v = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+    }
     return v;
 }
 
@@ -173,9 +194,7 @@ template <int n> __device__ __forceinline__ void group_sums(const NormArgs &p, c
     for (int i = 0; i < n; ++i) v[i] = at.live ? v[i] : 0.f;
     __syncthreads();        // the areas' last readers are done
     if (p.groups == 1) {
-        float all = v[0];
-#pragma unroll
-        for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
+        float all = team_sum(v[0], 6);
         if (lane == 0) lds[wave] = all;
         __syncthreads();
         all = lds[0];
@@ -361,17 +380,22 @@ __device__ __forceinline__ void combine(const NormArgs &p, long long g0, int gro
     const int cg = p.C / p.G, total = p.chunks * p.parts, shift = team_shift(groups, total), lane = threadIdx.x & ((1 << shift) - 1);
     const float m = (float)p.HW * (float)cg;
     auto count = [&](int i) {
-        const int chunk = i / p.parts;
+        const int chunk = p.parts > 1 ? i / p.parts : i;
         return (float)min(p.chunk, p.HW - chunk * p.chunk) * (float)(p.parts > 1 ? min(p.width, cg - (i - chunk * p.parts) * p.width) : cg);
     };
     for (int g = threadIdx.x >> shift; g < groups; g += blockDim.x >> shift) {
         const float2 *from = (const float2 *)p.partial + (g0 + g) * total;
         constexpr int B = 8;        // loads that fly together
+        float2 v[B];
+        auto load = [&](int i0) {
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = from[min(i0 + (b << shift), total - 1)];
+        };
+        load(lane);
+        const bool again = total > B << shift;      // else what is loaded is all there is
         auto each = [&](auto f) {
             for (int i0 = lane; i0 < total; i0 += B << shift) {
-                float2 v[B];
-#pragma unroll
-                for (int b = 0; b < B; ++b) v[b] = from[min(i0 + (b << shift), total - 1)];
+                if (again) load(i0);
 #pragma unroll
                 for (int b = 0; b < B; ++b)
                     if (i0 + (b << shift) < total) f(v[b], count(i0 + (b << shift)));
