@@ -434,7 +434,8 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
 
 // The same tiles through registers: operands that memory-to-LDS loads cannot take (rows at any address, any number of
 // layers) and fp32.  A step is 128 bytes of a row, PF of them on their way in registers, two images in LDS.  KS teams as above,
-// of any number of steps (fp32: 729 x 1536 x 384 34 -> 24 us, 1024^3 25 -> 19; bf16 gained nothing, its unaligned loads are the
+// of any number of steps (fp32: 729 x 1536 x 384 34 -> 24 us, 1024^3 25 -> 19; tiles of 32 rows where there are no more, 17 x 4000 x 4000
+// in shares of k 23.4 -> 20.6; bf16 gained nothing, its unaligned loads are the
 // bound).
 //
 // fp32 products run on the bf16 instructions: every operand is the sum of three bfloat16 values, x = h + m + l with h its
@@ -448,7 +449,7 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
 // that were not finite take its values.
 //
 // Bound by the matrix unit and the vector instructions of the splitting beside it: 10816 x 2048 x 2048 fp32 with GELU and residual in
-// 466 us (195 TFLOP/s; the fp32 instructions reach 154 in a large library product), 8192 x 4096 x 4096 in 1250 us (220); bf16 rows at
+// 454 us (200 TFLOP/s; the fp32 instructions reach 154 in a large library product), 8192 x 4096 x 4096 in 1250 us (220); bf16 rows at
 // any address 2001^3 in 33 us (468 TFLOP/s), 14301 x 1649 x 2808 in 233 us (568).
 template <typename TI> struct Image;
 template <> struct Image<bf16_t> {
@@ -730,7 +731,8 @@ double tiling_us(const Tiling &t, const LinearArgs &p, int Cin, int shares)
     const int each = (int)((rest + 255) / 256), most = t.slots / 256;
     return full * round(t.step, 1.0) + (rest ? round(most == 1 ? t.alone : t.alone + (t.step - t.alone) * (each - 1) / (most - 1), each == 1 ? 2.0 : 1.0) : 0.0);
 }
-const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6, 1}, {128, 128, 256, 4.5, 1.36, 1.2, 1}, {256, 128, 256, 8.5, 2.45, 2.1, 1}, {64, 64, 256, 3.5, 0.55, 0.43, 2}};
+const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6, 1}, {128, 128, 256, 4.5, 1.36, 1.2, 1}, {256, 128, 256, 8.5, 2.45, 2.1, 1},
+                       {64, 64, 256, 3.5, 0.55, 0.43, 2}, {32, 128, 256, 3.5, 0.66, 0.54, 2}};
 const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29, 1},  {128, 128, 256, 2.5, 0.57, 0.5, 1},  {128, 128, 512, 4.4, 1.0, 0.75, 1},
                           {256, 256, 256, 9.0, 1.5, 1.25, 1}, {64, 64, 256, 2.5, 0.22, 0.19, 2}, {128, 64, 256, 3.5, 0.32, 0.3, 2}};
 const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45, 1}, {128, 128, 512, 4.0, 1.8, 0.85, 1}};
@@ -756,7 +758,7 @@ Plan plan_of(const LinearArgs &p, bool direct)
     const int unit = f32 ? 32 : 64, steps = (p.Cin - 1) / unit + 1;
     const bool teams = direct && p.Cin / 64 % 2 == 0 && p.Cin >= 256;       // two teams share k evenly
     const Tiling *const all = f32 ? kF32 : direct ? kDirect : kAny;
-    const int n = f32 ? 4 : direct ? (teams ? 6 : 4) : 2;
+    const int n = f32 ? 5 : direct ? (teams ? 6 : 4) : 2;
     Plan best{0, p.Cin, 1};
     double us = tiling_us(all[0], p, p.Cin, 1);
     for (int i = 1; i < n; ++i) {
@@ -804,7 +806,8 @@ template <typename TI, typename TO> int launch_tiling(const LinearArgs &p, int w
             case 0: return launch_tile<TI, TO, 64, 64, 2, 2, 2>(p);
             case 1: return launch_tile<TI, TO, 128, 128, 2, 4, 1>(p);
             case 2: return launch_tile<TI, TO, 256, 128, 4, 2, 1>(p);
-            default: return launch_tile<TI, TO, 64, 64, 2, 2, 2, 2>(p);
+            case 3: return launch_tile<TI, TO, 64, 64, 2, 2, 2, 2>(p);
+            default: return launch_tile<TI, TO, 32, 128, 1, 4, 2, 2>(p);
         }
     } else if (direct) {
         switch (which) {
