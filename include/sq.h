@@ -488,7 +488,7 @@ int sq_squeezenet_forward_bf16(const void *in, sq_dtype in_dtype, const void *co
  * layers: normalise, project every pixel (a 1x1 convolution = a matrix product of rows), add.
  *   ld (ld_in, ld_out, ld_res): values from one row to the next, at least the row's own length
  *     (else SQ_ERR_SHAPE).  A larger one makes the operand a slice of a wider map: pass the address
- *     of its first layer; the other layers of the rows are neither read nor written.
+ *     of its first layer; the other layers of the rows have no influence and are not written.
  *   dtype: SQ_F32 or SQ_BF16 (2 bytes a value); anything else SQ_ERR_UNSUPPORTED.  Sums, statistics
  *     and activations are fp32 in both, a bfloat16 result is rounded once, to nearest even.
  *   act: one of the codes below; anything else SQ_ERR_UNSUPPORTED.

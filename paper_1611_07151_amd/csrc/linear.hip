@@ -85,6 +85,46 @@ template <typename TI> __device__ __forceinline__ u32x4_t load16(const TI *p)
     return __builtin_bit_cast(u32x4_t, load_n<16 / (int)sizeof(TI)>(p));
 }
 
+// A lane's place in a row.  ODD: bfloat16 rows that may begin between words; 16 bytes at such an address in lanes of sixteen rows take four
+// times as long to load as at a whole word's, so the words that hold them are loaded, none beyond, and shifted (8 x 1111 x 2000 7.4 -> 5.8
+// us; not in the tiles, whose eight lanes take 128 bytes of a row: 1000 x 1111 x 2000 18.9 -> 20.0).
+template <typename TI, bool ODD> struct Row {
+    struct Loaded {
+        u32x4_t v;
+        uint32_t behind[ODD ? 1 : 0];
+    };
+    const TI *p;
+    uint32_t shift;
+    __device__ __forceinline__ void set(const TI *at)
+    {
+        shift = ODD ? ((uint32_t)(uintptr_t)at & 2) * 8 : 0;
+        p = ODD ? (const TI *)((uintptr_t)at & ~(uintptr_t)3) : at;
+    }
+    __device__ __forceinline__ Loaded load(int k) const
+    {
+        Loaded l;
+        if constexpr (ODD) {
+            const uint32_t *const words = (const uint32_t *)(p + k);
+            __builtin_memcpy(&l.v, words, 16);
+            l.behind[0] = words[shift ? 4 : 3];
+        } else {
+            l.v = load16(p + k);
+        }
+        return l;
+    }
+    __device__ __forceinline__ u32x4_t whole(const Loaded &l) const
+    {
+        if constexpr (ODD) {
+            const uint32_t a = l.v[0], b = l.v[1], c = l.v[2], d = l.v[3];
+            return u32x4_t{__builtin_amdgcn_alignbit(b, a, shift), __builtin_amdgcn_alignbit(c, b, shift), __builtin_amdgcn_alignbit(d, c, shift),
+                           __builtin_amdgcn_alignbit(l.behind[0], d, shift)};
+        } else {
+            return l.v;
+        }
+    }
+    __device__ __forceinline__ u32x4_t tail(int k, int have) const { return load16_tail(p + k + (ODD ? (int)(shift / 16) : 0), have); }
+};
+
 // Rows and layers of the b-th tile: neighbouring workgroups of one XCD take a band of eight row tiles, row tile fastest,
 // so that what one of its L2 holds is eight row tiles and a few layer tiles.
 __device__ __forceinline__ void tile_at(int b, int tiles, int tiles_r, int tiles_j, int &tr, int &tj)
@@ -116,7 +156,7 @@ template <typename TI, typename TO> __device__ __forceinline__ void take_share(L
 // Bound by reading the kernels, and for small ones by the latency of one round of loads: 8 rows by 4096 x 4096 bf16 kernels take
 // 10.9 us (3.1 TB/s, launch included; 16 wavefronts have all of a 16-layer block's 128 KB in flight at once), one row by
 // 512 x 1000 fp32 4.8 us.
-template <typename TI, typename TO, int RT, int CT, int MAXW>
+template <typename TI, typename TO, int RT, int CT, int MAXW, bool ODD>
 __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
     constexpr int RB = RT / 16, CB = CT / 16, kStep = 64 / (int)sizeof(TI), kPiece = 16 / (int)sizeof(TI), kRow = CT + 4;
@@ -127,11 +167,11 @@ __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, in
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
     const int r0 = tr * RT, j0 = tj * CT;
-    const TI *xr[RB], *wr[CB];
+    Row<TI, ODD> xr[RB], wr[CB];
 #pragma unroll
-    for (int i = 0; i < RB; ++i) xr[i] = (const TI *)p.in + row_at(r0, 16 * i + l16, p.rows) * p.ld_in + piece * kPiece;
+    for (int i = 0; i < RB; ++i) xr[i].set((const TI *)p.in + row_at(r0, 16 * i + l16, p.rows) * p.ld_in + piece * kPiece);
 #pragma unroll
-    for (int i = 0; i < CB; ++i) wr[i] = (const TI *)p.w + row_at(j0, 16 * i + l16, p.Cout) * p.ld_w + piece * kPiece;
+    for (int i = 0; i < CB; ++i) wr[i].set((const TI *)p.w + row_at(j0, 16 * i + l16, p.Cout) * p.ld_w + piece * kPiece);
     f32x4_t acc[CB][RB] = {};
     auto multiply = [&](const u32x4_t (&a)[CB], const u32x4_t (&b)[RB]) {
 #pragma unroll
@@ -149,16 +189,23 @@ __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, in
     };
     auto steps = [&](auto count, int k) {
         constexpr int S = decltype(count)::value;
-        u32x4_t a[S][CB], b[S][RB];
+        typename Row<TI, ODD>::Loaded a[S][CB], b[S][RB];
 #pragma unroll
         for (int s = 0; s < S; ++s) {
 #pragma unroll
-            for (int c = 0; c < CB; ++c) a[s][c] = load16(wr[c] + k + s * kStep);
+            for (int c = 0; c < CB; ++c) a[s][c] = wr[c].load(k + s * kStep);
 #pragma unroll
-            for (int r = 0; r < RB; ++r) b[s][r] = load16(xr[r] + k + s * kStep);
+            for (int r = 0; r < RB; ++r) b[s][r] = xr[r].load(k + s * kStep);
         }
 #pragma unroll
-        for (int s = 0; s < S; ++s) multiply(a[s], b[s]);
+        for (int s = 0; s < S; ++s) {
+            u32x4_t w[CB], x[RB];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) w[c] = wr[c].whole(a[s][c]);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) x[r] = xr[r].whole(b[s][r]);
+            multiply(w, x);
+        }
     };
     const int whole = p.Cin / kStep;
     int at = (int)((long long)whole * wave / nw);
@@ -173,9 +220,9 @@ __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, in
         const int k = whole * kStep, have = p.Cin - k - piece * kPiece;
         u32x4_t a[CB], b[RB];
 #pragma unroll
-        for (int c = 0; c < CB; ++c) a[c] = load16_tail(wr[c] + k, have);
+        for (int c = 0; c < CB; ++c) a[c] = wr[c].tail(k, have);
 #pragma unroll
-        for (int r = 0; r < RB; ++r) b[r] = load16_tail(xr[r] + k, have);
+        for (int r = 0; r < RB; ++r) b[r] = xr[r].tail(k, have);
         multiply(a, b);
     }
     // lane holds, of row l16 of every block of rows, four neighbouring layers of every block of layers
@@ -687,12 +734,12 @@ template <typename TO> __global__ __launch_bounds__(256) void linear_join_kernel
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
-template <typename TI, typename TO, int RT, int CT, int MAXW> int launch_wave(const LinearArgs &p, int waves)
+template <typename TI, typename TO, int RT, int CT, int MAXW, bool ODD> int launch_wave(const LinearArgs &p, int waves)
 {
     const int tr = (p.rows - 1) / RT + 1, tj = (p.Cout - 1) / CT + 1;
     if (!one_launch((double)tr * tj, 64 * MAXW)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_wave", linear_flops(p), linear_bytes(p));
-    hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW>), dim3((unsigned)tr * tj), dim3(64 * std::max(1, std::min(waves, MAXW))), 0,
+    hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW, ODD>), dim3((unsigned)tr * tj), dim3(64 * std::max(1, std::min(waves, MAXW))), 0,
                        current_stream(), p, tr, tj);
     return check_launch();
 }
@@ -765,12 +812,12 @@ Plan plan_of(const LinearArgs &p, bool direct)
         const double t = tiling_us(all[i], p, p.Cin, 1);
         if (t < us) us = t, best.which = i;
     }
-    // the wavefronts: us for 1000 of k, of a block by itself and of a full chip's 256 (30 products); bf16 rows that do not begin at
-    // whole 8 bytes take their loads in parts
+    // the wavefronts: us for 1000 of k, of a block by itself and of a full chip's 256 (30 products); bf16 rows that begin
+    // between words take more
     const bool small = p.rows <= 16 || results <= 65536 || steps <= 2;
     const int B = small ? 16 : 32;
     const double blocks = ((p.rows - 1) / B + 1.0) * ((p.Cout - 1) / B + 1.0);
-    const double one = small ? (f32 ? 2.0 : p.Cin % 4 == 0 ? 1.0 : p.Cin % 2 == 0 ? 2.1 : 3.7) : (f32 ? 7.3 : 3.3);
+    const double one = small ? (f32 ? 2.0 : p.Cin % 2 == 0 ? 1.0 : 1.6) : (f32 ? 7.3 : 3.3);
     const double all256 = small ? (f32 ? 3.5 : 1.6 * one) : one;
     const double waves = 4.0 + std::max(std::ceil(blocks / 256) * one, blocks / 256 * all256) * p.Cin * 1e-3;
     const double many = direct && !teams ? 1 << 18 : 1 << 16;
@@ -796,6 +843,8 @@ bool direct_loads(int in_dtype, int Cin, long long ld_in, bool aligned)
 {
     return in_dtype == SQ_BF16 && Cin % 8 == 0 && ld_in % 8 == 0 && aligned && ld_in < (1 << 22) && Cin < (1 << 22);
 }
+// Whether bfloat16 rows may begin between words.
+bool between_words(const LinearArgs &p) { return p.in_dtype == SQ_BF16 && ((p.Cin | p.ld_in) % 2 || (((uintptr_t)p.in | (uintptr_t)p.w) & 3)); }
 // Rows of the shares' sums begin at whole lines.
 long long share_row(int Cout) { return ((long long)Cout + 31) / 32 * 32; }
 
@@ -829,8 +878,13 @@ template <typename TI, typename TO> int by_size(LinearArgs p)
     const Plan plan = plan_of(p, direct);
     p.ld_w = p.Cin;
     p.share = plan.share, p.shares = plan.shares;
-    if (plan.which == kWave16) return launch_wave<TI, TO, 16, 16, 16>(p, 2 * ((p.Cin - 1) / (128 / (int)sizeof(TI)) + 1));
-    if (plan.which == kWave32) return launch_wave<TI, TO, 32, 32, 8>(p, (p.Cin - 1) / (128 / (int)sizeof(TI)) + 1);
+    const int steps = (p.Cin - 1) / (128 / (int)sizeof(TI)) + 1;
+    if (plan.which == kWave16) {
+        if constexpr (sizeof(TI) == 2)
+            if (between_words(p)) return launch_wave<TI, TO, 16, 16, 16, true>(p, 2 * steps);
+        return launch_wave<TI, TO, 16, 16, 16, false>(p, 2 * steps);
+    }
+    if (plan.which == kWave32) return launch_wave<TI, TO, 32, 32, 8, false>(p, steps);
     if (plan.shares == 1) return launch_tiling<TI, TO>(p, plan.which, direct);
     LinearArgs part = p;
     part.b = nullptr, part.residual = nullptr, part.act = SQ_ACT_NONE;
@@ -848,7 +902,7 @@ template <typename TI, typename TO> int by_size(LinearArgs p)
 bool linear_register_kernels()
 {
     hipFuncAttributes a;
-    return hipFuncGetAttributes(&a, (const void *)linear_wave_kernel<float, float, 16, 16, 16>) == hipSuccess;
+    return hipFuncGetAttributes(&a, (const void *)linear_wave_kernel<float, float, 16, 16, 16, false>) == hipSuccess;
 }
 
 size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype, long long ld_in, bool aligned)
