@@ -154,8 +154,8 @@ template <typename TI, typename TO> __device__ __forceinline__ void take_share(L
 // from memory straight into the lanes of v_mfma_f32_16x16x32_bf16 / _16x16x4_f32: lane l takes 16 bytes of row l % 16 at
 // piece l / 16 of the step (fp32: value i of every lane's four is one instruction; both operands number k alike).
 // Bound by reading the kernels, and for small ones by the latency of one round of loads: 8 rows by 4096 x 4096 bf16 kernels take
-// 10.9 us (3.1 TB/s, launch included; 16 wavefronts have all of a 16-layer block's 128 KB in flight at once), one row by
-// 512 x 1000 fp32 4.8 us.
+// 9.5 us (3.5 TB/s, launch included; fp32 15.9, 4.2 TB/s; one compute unit reads one block of 16 layers), one row by 512 x 1000
+// fp32 4.2 us.  Loads of the next steps held before the products of these changed nothing (fp32 15.9 -> 16.1).
 template <typename TI, typename TO, int RT, int CT, int MAXW, bool ODD>
 __global__ __launch_bounds__(64 * MAXW) void linear_wave_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {
@@ -891,7 +891,7 @@ template <typename TI, typename TO> int by_size(LinearArgs p)
     part.out = p.workspace, part.out_dtype = SQ_F32, part.ld_out = share_row(p.Cout);
     if (const int rc = launch_tiling<TI, float>(part, plan.which, direct)) return rc;
     p.in = p.workspace, p.ld_in = part.ld_out;
-    const unsigned threads = (unsigned)p.rows * ((unsigned)(p.Cout - 1) / 4 + 1);       // fewer than 512 tiles' results
+    const unsigned threads = (unsigned)p.rows * ((unsigned)(p.Cout - 1) / 4 + 1);       // at most 512 tiles' results
     const LaunchScope prof("linear_join", 0, 4.0 * plan.shares * p.rows * p.Cout + (sizeof(TO) * (p.residual ? 2.0 : 1.0)) * p.rows * p.Cout);
     hipLaunchKernelGGL((linear_join_kernel<TO>), dim3((threads - 1) / 256 + 1), dim3(256), 0, current_stream(), p);
     return check_launch();
