@@ -555,6 +555,97 @@ def test_group_norm_of_a_map_past_32_bits(sq):
         assert ((part - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-30).all(), i
 
 
+def shifted(values, offset, dtype):
+    """`values` as a dense tensor that begins `offset` values behind a 512-byte boundary, NaN around it."""
+    flat = torch.full((values.numel() + 2 * offset + 8,), float("nan"), dtype=dtype, device="cuda")
+    at = flat[offset:offset + values.numel()].view(values.shape)
+    at.copy_(values)
+    return flat, at
+
+
+@pytest.mark.parametrize("offset", (1, 2, 3, 4, 8))
+@pytest.mark.parametrize("ti,to", TYPES)
+@pytest.mark.parametrize("rows,cin,cout", [(1, 512, 100), (8, 1111, 200), (17, 64, 33), (70, 96, 1000), (300, 2048, 300), (33, 4096, 130), (600, 200, 520),
+                                           (1300, 136, 1301)])
+def test_linear_operands_at_any_address(sq, rows, cin, cout, ti, to, offset):
+    g = gen(90 + offset)
+    xv, wv = torch.randn((rows, cin), generator=g).to(ti), (torch.randn((cout, cin), generator=g) / math.sqrt(cin)).to(ti)
+    bv, rv = torch.randn(cout, generator=g), torch.randn((rows, cout), generator=g).to(to)
+    sums = xv.double().cuda() @ wv.double().cuda().t() + bv.double().cuda()
+    terms = xv.double().abs().cuda() @ wv.double().abs().cuda().t() + bv.double().abs().cuda()
+    ref = (sums + rv.double().cuda()).cpu()
+    bound = (1.13 * (cin + 16) * 2 * U * terms).cpu() + U * ref.abs()
+    for moved in ("xw", "x", "w", "out"):
+        x = shifted(xv, offset, ti)[1] if "x" in moved else xv.cuda()
+        w = shifted(wv, offset, ti)[1] if "w" in moved else wv.cuda()
+        b, res = shifted(bv, offset, F32)[1], shifted(rv, offset, to)[1]
+        flat, out = shifted(torch.zeros((rows, cout)), offset if moved == "out" else 0, to)
+        print(f"linear {rows}x{cin}x{cout} {ti}->{to} offset={offset} moved={moved}", flush=True)
+        sq.sq_linear_forward(x, w, b, residual=res, out=out)
+        check(out, ref, bound + half_step(ref, to) + bound * torch.finfo(to).eps, (rows, cin, cout, ti, to, offset, moved))
+        edge = offset if moved == "out" else 0
+        assert flat[:edge].isnan().all() and flat[edge + rows * cout:].isnan().all()
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(300, 2048, 300), (1000, 992, 1000), (24, 3691, 3000), (1300, 2600, 1040)])
+@pytest.mark.parametrize("spread", (1e-20, 1e15, 1e25))
+def test_linear_far_magnitudes_in_tiles(sq, rows, cin, cout, spread):
+    linear_case(sq, rows, cin, cout, 0, F32, F32, 61, bias=False, residual=False, spread=spread)
+
+
+def test_empty_operands_are_refused(sq):
+    x, w = torch.zeros((0, 8), device="cuda"), torch.zeros((6, 8), device="cuda")
+    with pytest.raises(RuntimeError):
+        sq.sq_linear_forward(x, w)
+    with pytest.raises(RuntimeError):
+        sq.sq_linear_forward(torch.zeros((4, 0), device="cuda"), torch.zeros((6, 0), device="cuda"))
+    with pytest.raises(RuntimeError):
+        sq.sq_nhwc_group_norm(torch.zeros((0, 5, 5, 8), device="cuda"), 2)
+    with pytest.raises(RuntimeError):
+        sq.sq_nhwc_pack(torch.zeros((2, 3, 0, 5), device="cuda"))
+    with pytest.raises(RuntimeError):
+        sq.sq_nhwc_unpack(torch.zeros((2, 0, 5, 3), device="cuda"))
+
+
+def test_shares_of_k_on_two_streams_at_once(sq):
+    """Calls that take scratch, in flight together on streams of their own."""
+    sizes = [(300, 2048, 300, F32), (300, 2048, 300, BF16), (24, 3691, 3000, F32), (729, 1536, 384, F32)]
+    jobs = []
+    for i, (rows, cin, cout, dt) in enumerate(sizes):
+        x, w = torch.randn((rows, cin), generator=gen(i)).to(dt).cuda(), torch.randn((cout, cin), generator=gen(50 + i)).to(dt).cuda()
+        assert sq.sq_linear_workspace_bytes(rows, cin, cout, dt)
+        jobs.append((x, w, sq.sq_linear_forward(x, w, act=2)))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for turn in range(20):
+        for k, stream in enumerate(streams):
+            x, w, want = jobs[(turn + k) % len(jobs)]
+            with torch.cuda.stream(stream):
+                got.append((sq.sq_linear_forward(x, w, act=2), want))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in got)
+
+
+@pytest.mark.parametrize("offset", (1, 2, 3, 4))
+@pytest.mark.parametrize("dt", (F32, BF16))
+@pytest.mark.parametrize("n,h,w,c,groups", [(2, 13, 11, 64, 8), (3, 5, 7, 30, 3), (1, 70, 60, 48, 4), (1, 111, 111, 96, 8)])
+def test_maps_at_any_address(sq, n, h, w, c, groups, dt, offset):
+    """The same bits as from aligned copies: conversions move values, and a group norm's order of sums depends on sizes alone."""
+    v = torch.randn((n, c, h, w), generator=gen(offset)).to(dt)
+    dense = v.permute(0, 2, 3, 1).contiguous().cuda()
+    flat, out = shifted(torch.zeros((n, h, w, c)), offset, dt)
+    sq.sq_nhwc_pack(shifted(v, offset, dt)[1], out=out)
+    assert torch.equal(out, dense) and flat[:offset].isnan().all() and flat[offset + v.numel():].isnan().all()
+    flat, back = shifted(torch.zeros((n, c, h, w)), offset, dt)
+    sq.sq_nhwc_unpack(out, out=back)
+    assert torch.equal(back, v.cuda()) and flat[:offset].isnan().all() and flat[offset + v.numel():].isnan().all()
+    gamma, beta = torch.randn(c, generator=gen(7)), torch.randn(c, generator=gen(8))
+    want = sq.sq_nhwc_group_norm(dense, groups, gamma.cuda(), beta.cuda(), act=3)
+    flat, got = shifted(torch.zeros((n, h, w, c)), offset, dt)
+    sq.sq_nhwc_group_norm(out, groups, shifted(gamma, offset, F32)[1], shifted(beta, offset, F32)[1], act=3, out=got)
+    assert torch.equal(got, want) and flat[:offset].isnan().all() and flat[offset + v.numel():].isnan().all()
+
+
 def test_profiler_sees_the_launches(sq):
     x, w = torch.randn((64, 32), device="cuda"), torch.randn((16, 32), device="cuda")
     sq.sq_profile_begin(16)
