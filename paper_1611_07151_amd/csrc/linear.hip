@@ -720,17 +720,37 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
 // ---- the shares' sums ----------------------------------------------------------------------------------------------
 // A thread adds up four neighbouring results of a row, in order of the shares, and finishes them.  In LinearArgs `in` is the
 // shares' sums in rows of ld_in, a multiple of four.  Bound by its launch.
+constexpr int kMostShares = 16;
 template <typename TO> __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p)
 {
     const unsigned quads = (unsigned)(p.Cout - 1) / 4 + 1, e = blockIdx.x * 256 + threadIdx.x, r = e / quads;
     if (r >= (unsigned)p.rows) return;
     const int j = (int)(e - r * quads) * 4;
     const float *at = (const float *)p.in + r * p.ld_in + j;
-    f32x4_t s = *(const f32x4_t *)at;
-#pragma unroll 4
-    for (int i = 1; i < p.shares; ++i) s += *(const f32x4_t *)(at + i * (p.rows * p.ld_in));
+    const long long part = p.rows * p.ld_in;
+    // every load before the first sum
+    f32x4_t of[kMostShares];
+#pragma unroll
+    for (int i = 0; i < kMostShares; ++i)
+        if (i < p.shares) of[i] = *(const f32x4_t *)(at + i * part);
+    const bool full = j + 4 <= p.Cout;
+    Vec<float, 4> b = {};
+    Vec<TO, 4> res = {};
+    if (full && p.b) b = load_n<4>(p.b + j);
+    if (full && p.residual) res = load_n<4>((const TO *)p.residual + r * p.ld_res + j);
+    f32x4_t s = of[0];
+#pragma unroll
+    for (int i = 1; i < kMostShares; ++i)
+        if (i < p.shares) s += of[i];
     float v[4] = {s[0], s[1], s[2], s[3]};
-    finish<TO>(p, r, j, p.Cout - j, v);
+    if (!full) return finish<TO>(p, r, j, p.Cout - j, v);
+    Vec<TO, 4> o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float y = activate_by(v[i] + b.v[i], p.act);
+        o.v[i] = from_f32<TO>(p.residual ? y + to_f32(res.v[i]) : y);
+    }
+    __builtin_memcpy((TO *)p.out + r * p.ld_out + j, &o, sizeof(o));
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
@@ -828,7 +848,7 @@ Plan plan_of(const LinearArgs &p, bool direct)
         const Tiling &t = all[i];
         const double tiles = ((p.rows - 1) / t.BM + 1.0) * ((p.Cout - 1) / t.BN + 1.0);
         const int units = p.Cin / (unit * t.teams);
-        for (int want = 2; want <= 16 && tiles * want <= 512; ++want) {
+        for (int want = 2; want <= kMostShares && tiles * want <= 512; ++want) {
             const int share = ((units - 1) / want + 1) * unit * t.teams, shares = (units * unit * t.teams - 1) / share + 1;
             if (shares != want) continue;
             const double join = 4.5 + results * shares * 8.0 / 5e6, cost = tiling_us(t, p, std::max(share, p.Cin - (shares - 1) * share), shares) + join;
