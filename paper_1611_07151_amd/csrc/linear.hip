@@ -815,7 +815,7 @@ struct Plan { int which, share, shares; };
 // 11.9 / 17.8), 2^16 too where rows lie at any address (300 x 2049 x 300 27.7 / 16.1, 905 x 193 x 704 11.1 / 5.1; 129 x 2657 x 416
 // 16.1 / 18.1), by estimate for fp32 (3506 x 416 x 1096 58 / 27, 1024^3 35 / 19, 729 x 1536 x 384 26.5 / 23.7; 300 x 2048 x 300 17.5 /
 // 27.8, 64 x 4096 x 4096 34 / 52).
-// Where one workgroup's way through k leaves the chip idle, tiles in shares of k and a second launch that adds them up (4.5 us and
+// Where one workgroup's way through k leaves the chip idle, tiles in shares of k and a second launch that adds them up (3.8 us and
 // the sums' bytes), if that is to save 8 % (us, without / with: 300 x 4000 x 1000 fp32 50.5 / 26.6, 24 x 3691 x 3000 bf16 24.9 /
 // 11.7, 17 x 4096 x 4096 14.2 / 10.2; 42 x 728 x 7032 fp32 14.4 / 14.5, 64 x 1280 x 3712 bf16 7.0 / 8.8, 40 x 2500 x 150 6.2 / 9.1).
 Plan plan_of(const LinearArgs &p, bool direct)
@@ -837,13 +837,14 @@ Plan plan_of(const LinearArgs &p, bool direct)
     const bool small = p.rows <= 16 || results <= 65536 || steps <= 2;
     const int B = small ? 16 : 32;
     const double blocks = ((p.rows - 1) / B + 1.0) * ((p.Cout - 1) / B + 1.0);
+    const bool far = ((double)p.rows + p.Cout) * p.Cin > 2e6;       // rows of blocks read kernels and input again: from beyond an XCD's cache
     const double one = small ? (f32 ? 2.0 : p.Cin % 2 == 0 ? 1.0 : 1.6) : (f32 ? 7.3 : 3.3);
-    const double all256 = small ? (f32 ? 3.5 : 1.6 * one) : one;
+    const double all256 = !small ? one : p.rows <= 16 ? (f32 ? 3.0 : 1.35 * one) : f32 ? (far ? 4.3 : 2.7) : 1.6 * one;
     const double waves = 4.0 + std::max(std::ceil(blocks / 256) * one, blocks / 256 * all256) * p.Cin * 1e-3;
     const double many = direct && !teams ? 1 << 18 : 1 << 16;
     if (p.rows <= 16 || results <= many || (f32 && (waves < us || (steps <= 2 && results < 1 << 20)))) us = waves, best.which = small ? kWave16 : kWave32;
     us *= 0.92;
-    if (steps < 16 || us < 4.5 + 1.9) return best;
+    if (steps < 16 || us < 3.8 + 1.9) return best;
     for (int i = 0; i < n; ++i) {
         const Tiling &t = all[i];
         const double tiles = ((p.rows - 1) / t.BM + 1.0) * ((p.Cout - 1) / t.BN + 1.0);
@@ -851,7 +852,7 @@ Plan plan_of(const LinearArgs &p, bool direct)
         for (int want = 2; want <= kMostShares && tiles * want <= 512; ++want) {
             const int share = ((units - 1) / want + 1) * unit * t.teams, shares = (units * unit * t.teams - 1) / share + 1;
             if (shares != want) continue;
-            const double join = 4.5 + results * shares * 8.0 / 5e6, cost = tiling_us(t, p, std::max(share, p.Cin - (shares - 1) * share), shares) + join;
+            const double join = 3.8 + results * shares * 8.0 / 5e6, cost = tiling_us(t, p, std::max(share, p.Cin - (shares - 1) * share), shares) + join;
             if (cost < us) us = cost, best = Plan{i, share, shares};
         }
     }
