@@ -554,8 +554,8 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
  *     ld_out values; both of out_dtype: SQ_F32 with SQ_F32 inputs, either with SQ_BF16 inputs
  *     (otherwise SQ_ERR_UNSUPPORTED).  residual may be out itself with the same ld; apart from that
  *     out must not overlap any input.
- *   fp32: above 65536 results the products may run on the bfloat16 matrix instructions with
- *     each operand as the exact sum of three bfloat16 values and fp32 sums: the error stays that of fp32
+ *   fp32: the products may run on the bfloat16 matrix instructions (the sizes decide), with each
+ *     operand as the exact sum of three bfloat16 values and fp32 sums: the error stays that of fp32
  *     sums of the same terms, except that operands below 2^-110 in magnitude keep fewer bits.  An
  *     infinity or NaN reaches the results of its row or kernel and no others.
  *   workspace: sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype, ld_in, aligned) bytes of device
