@@ -556,7 +556,8 @@ int sq_nhwc_group_norm(const void *in, void *out, sq_dtype dtype, const float *g
  *     out must not overlap any input.
  *   fp32: the products may run on the bfloat16 matrix instructions (the sizes decide), with each
  *     operand as the exact sum of three bfloat16 values and fp32 sums: the error stays that of fp32
- *     sums of the same terms, except that operands below 2^-110 in magnitude keep fewer bits.  An
+ *     sums of the same terms, except that operands below 2^-110 in magnitude keep fewer bits (those
+ *     of 2^-133 and more) beside finite ones.  An
  *     infinity or NaN reaches the results of its row or kernel and no others.
  *   workspace: sq_linear_workspace_bytes(rows, Cin, Cout, in_dtype, ld_in, aligned) bytes of device
  *     scratch, with aligned = whether in and w both begin at multiples of 16 bytes; 256-byte aligned

@@ -492,8 +492,9 @@ __global__ __launch_bounds__(64 * WR *WC *KS, (BM + BN) * 128 * NS * KS <= 80 * 
 // matrix unit where fp32 ones take 512.  Every term keeps its own accuracy whatever lies beside it; only operands below
 // 2^-110 lose bits (their l falls below what a bfloat16 can hold).
 // An infinity has no such form (inf - inf).  It, a NaN, or sums that overflow leave a sum that is not finite; the tile is then
-// made once more from the rounded upper parts alone, whose products have the right infinities and NaN, and those results
-// that were not finite take its values.
+// made once more from the operands as they are, on the fp32 instructions, and those results that were not finite take its values.
+// (Rounded upper parts would do for ordinary numbers, but a rounded operand can change its kind: the largest numbers
+// become infinities and the smallest zeros, whose products with a zero or an infinity are NaN.)
 //
 // Bound by the matrix unit and the vector instructions of the splitting beside it: 10816 x 2048 x 2048 fp32 with GELU and residual in
 // 454 us (200 TFLOP/s; the fp32 instructions reach 154 in a large library product), 8192 x 4096 x 4096 in 1250 us (220); bf16 rows at
@@ -559,52 +560,67 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
     };
     const int xrow = wave / WC * (XB * 32) + (lane & 31), wrow = BM + wave % WC * (JB * 32) + (lane & 31);
     f32x16_t acc[XB][JB];
-    // the sums of all of k; rough: from rounded upper parts only (fp32)
-    auto sums = [&](auto rough) {
-        constexpr bool kRough = decltype(rough)::value;
+    // the sums of all of k; plain: on the fp32 instructions, a row's 128 bytes in LDS as in a bfloat16 image
+    auto sums = [&](auto plain) {
+        constexpr bool kPlain = decltype(plain)::value;
+        using Raw = Image<bf16_t>;
+        static_assert(kRows * 8 <= kImage, "a step's operands fit an image as they are");
         auto store = [&](const u32x4_t (&from)[NP], u32x4_t *to) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int r = row + i * 8 * NW;
-                if constexpr (sizeof(TI) == 2) {
-                    to[I::at(r, q)] = from[i];
+                if constexpr (sizeof(TI) == 2 || kPlain) {
+                    to[Raw::at(r, q)] = from[i];
                 } else {
                     const f32x4_t v = __builtin_bit_cast(f32x4_t, from[i]);
                     uint2 *at = (uint2 *)(to + I::at(r, q >> 1)) + (q & 1);
-                    if constexpr (kRough) {
-                        at[0] = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-                    } else {
-                        uint2 h, m, l;
-                        split_pair(v[0], v[1], h.x, m.x, l.x);
-                        split_pair(v[2], v[3], h.y, m.y, l.y);
-                        at[0] = h;
-                        at[2 * kPlane] = m;
-                        at[4 * kPlane] = l;
-                    }
+                    uint2 h, m, l;
+                    split_pair(v[0], v[1], h.x, m.x, l.x);
+                    split_pair(v[2], v[3], h.y, m.y, l.y);
+                    at[0] = h;
+                    at[2 * kPlane] = m;
+                    at[4 * kPlane] = l;
                 }
             }
         };
         auto multiply = [&](const u32x4_t *from) {
-            constexpr int NPL = kRough ? 1 : I::kPlanes;
+            if constexpr (kPlain) {
+#pragma unroll 1
+                for (int s = 0; s < 4; ++s) {       // a lane's 16 bytes of either operand are four instructions' values
+                    f32x4_t x[XB], w[JB];
 #pragma unroll
-            for (int s = 0; s < kSub; ++s) {
-                bf16x8 x[NPL][XB], w[NPL][JB];
+                    for (int i = 0; i < JB; ++i) w[i] = __builtin_bit_cast(f32x4_t, from[Raw::at(wrow + 32 * i, 2 * s + (lane >> 5))]);
 #pragma unroll
-                for (int n = 0; n < NPL; ++n) {
+                    for (int i = 0; i < XB; ++i) x[i] = __builtin_bit_cast(f32x4_t, from[Raw::at(xrow + 32 * i, 2 * s + (lane >> 5))]);
 #pragma unroll
-                    for (int i = 0; i < JB; ++i) w[n][i] = __builtin_bit_cast(bf16x8, from[n * kPlane + I::at(wrow + 32 * i, 2 * s + (lane >> 5))]);
-#pragma unroll
-                    for (int i = 0; i < XB; ++i) x[n][i] = __builtin_bit_cast(bf16x8, from[n * kPlane + I::at(xrow + 32 * i, 2 * s + (lane >> 5))]);
-                }
-                // the smallest products first
-#pragma unroll
-                for (int n = NPL - 1; n >= 0; --n)
-#pragma unroll
-                    for (int a = 0; a <= n; ++a)
+                    for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int i = 0; i < XB; ++i)
 #pragma unroll
-                            for (int c = 0; c < JB; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[a][c], x[n - a][i], acc[i][c], 0, 0, 0);
+                            for (int c = 0; c < JB; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[c][e], x[i][e], acc[i][c], 0, 0, 0);
+                }
+            } else {
+                constexpr int NPL = I::kPlanes;
+#pragma unroll
+                for (int s = 0; s < kSub; ++s) {
+                    bf16x8 x[NPL][XB], w[NPL][JB];
+#pragma unroll
+                    for (int n = 0; n < NPL; ++n) {
+#pragma unroll
+                        for (int i = 0; i < JB; ++i) w[n][i] = __builtin_bit_cast(bf16x8, from[n * kPlane + I::at(wrow + 32 * i, 2 * s + (lane >> 5))]);
+#pragma unroll
+                        for (int i = 0; i < XB; ++i) x[n][i] = __builtin_bit_cast(bf16x8, from[n * kPlane + I::at(xrow + 32 * i, 2 * s + (lane >> 5))]);
+                    }
+                    // the smallest products first
+#pragma unroll
+                    for (int n = NPL - 1; n >= 0; --n)
+#pragma unroll
+                        for (int a = 0; a <= n; ++a)
+#pragma unroll
+                            for (int i = 0; i < XB; ++i)
+#pragma unroll
+                                for (int c = 0; c < JB; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[a][c], x[n - a][i], acc[i][c], 0, 0, 0);
+                }
             }
         };
 #pragma unroll
@@ -633,8 +649,8 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
                 store(next, lds + (s + 1) % 2 * kImage);
                 fetch(next, min(s + 1 + PF, whole - 1) * kStep);
                 multiply(lds + s % 2 * kImage);
-                if constexpr (XB * JB > 1) {    // larger tiles: the loads go out between the products, not before them (3 to 6 %)
-                    constexpr int M = XB * JB * kSub * (kRough || sizeof(TI) == 2 ? 1 : 6);
+                if constexpr (XB * JB > 1 && !kPlain) {     // larger tiles: the loads go out between the products, not before them (3 to 6 %)
+                    constexpr int M = XB * JB * kSub * (sizeof(TI) == 2 ? 1 : 6);
                     __builtin_amdgcn_sched_group_barrier(0x008, M / 4, 0);
 #pragma unroll
                     for (int i = 0; i < NP; ++i) {

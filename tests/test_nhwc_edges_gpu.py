@@ -1,0 +1,77 @@
+"""Channels-last operators at the ends of the number format.
+
+u = 2^-24 is half a unit of fp32's last place.
+"""
+import pytest
+import torch
+
+from test_nhwc_gpu import F32, U, gen
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+MAX = torch.finfo(F32).max
+
+
+@pytest.fixture(scope="module")
+def sq():
+    import paper_1611_07151_amd as m
+    m.sq_init()
+    return m
+
+
+# One product or two for each way an fp32 product is made: wavefronts in small and large blocks, the five tilings, and
+# those of them that take shares of k.  Odd steps, part steps and ragged edges among them.
+FP32_FORMS = [(17, 99, 40), (300, 96, 264), (2100, 31, 600), (1300, 136, 1301), (17, 5391, 45), (5400, 520, 1400), (2806, 1343, 71),
+              (3601, 328, 3584), (5518, 1169, 129), (1000, 992, 1000), (300, 2048, 300), (2043, 85, 429), (130, 1111, 2000), (17, 1632, 2152)]
+
+
+# --------------------------------------------------------------------------------- infinities beside the format's ends
+@pytest.mark.parametrize("near", (False, True))
+@pytest.mark.parametrize("rows,cin,cout", FP32_FORMS)
+def test_infinities_beside_extreme_operands(sq, rows, cin, cout, near):
+    """Results that are not finite are those of the sums in fp32: a finite operand counts as finite, one that is not zero
+    as not zero, and a sum past the largest number as an infinity, whatever else lies in the tile.  Rows 0 to 4 and kernels 5
+    and 6 hold two operands and zeros, the other rows and kernels stay so small that no other product overflows."""
+    g = gen(rows + cin)
+    x = (torch.randn((rows, cin), generator=g) * 0.1).clamp(-0.9, 0.9)
+    w = (torch.randn((cout, cin), generator=g) * 0.1).clamp(-0.25, 0.25)
+    a, b = (cin // 2, cin // 2 + 1) if near else (0, cin - 1)
+    x[:7], w[5:7] = 0, 0
+    x[0, a], x[0, b], w[0, a], w[0, b] = -MAX, -INF, -0.5, 1.0           # finite - inf
+    x[1, a], x[1, b], w[1, a], w[1, b] = -MAX, -MAX, 2.0, 0.0            # an overflow + 0
+    x[2, a], w[2, a] = INF, 1e-42                                        # inf * subnormal
+    x[3, a], x[3, b], w[3, a], w[3, b] = 1.9060151e38, 1.4985098e38, 1.0, 1.0      # just past the largest number
+    x[4, a], x[4, b], w[4, a], w[4, b] = INF, MAX, 1.0, 0.0              # inf + finite * 0
+    w[5, a], x[5, a] = INF, 1e-42
+    w[6, a], w[6, b], x[6, a], x[6, b] = -MAX, -INF, -0.5, 1.0
+    got = sq.sq_linear_forward(x.cuda(), w.cuda()).cpu()
+    assert got[0, 0] == -INF and got[1, 1] == -INF and got[2, 2] == INF and got[3, 3] == INF and got[4, 4] == INF
+    assert got[5, 5] == INF and got[6, 6] == -INF
+    want = (x.double().cuda() @ w.double().cuda().t()).float().cpu()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got.isinf(), want.isinf()) and torch.equal(got[got.isinf()], want[want.isinf()])
+    # and what is finite keeps its accuracy: as the sums have it, and as the smallest of three bfloat16 values leaves an operand,
+    # half of 2^-133 off, times the other operand; the result itself and the reference are rounded to multiples of 2^-149
+    fin = want.isfinite()
+    clamp = lambda t: t.double().clamp(-1e300, 1e300).abs()
+    small = 2.0 ** -134 * (clamp(x).sum(1)[:, None] + clamp(w).sum(1)) + 2.0 ** -149
+    terms = (clamp(x).cuda() @ clamp(w).cuda().t()).cpu()
+    err, bound = (got.double() - want.double()).abs()[fin], ((cin + 16) * 2 * U * terms + small)[fin]
+    assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(300, 96, 264), (1000, 992, 1000), (1300, 136, 1301)])
+def test_few_and_many_rows_agree_on_what_is_not_finite(sq, rows, cin, cout):
+    """The first rows by themselves go to the wavefronts, all of them to tiles.  Left out are the sums of which a finite product
+    passes the largest number by itself: with an infinity of the other sign behind it such a sum is inf - inf, with the infinity
+    before it, where product and addition are one rounding, it is that infinity, and the order of a sum is not promised."""
+    x, w = torch.randn((rows, cin), generator=gen(1)), torch.randn((cout, cin), generator=gen(2))
+    x[::3, 7], x[1::5, cin - 1], w[::7, 3] = MAX, -INF, 1e-41
+    w[1::7, 7], x[2::9, 3] = 0.0, INF
+    x, w = x.cuda(), w.cuda()
+    many = sq.sq_linear_forward(x, w, act=1)[:64]
+    few = torch.cat([sq.sq_linear_forward(x[i:i + 8], w, act=1) for i in range(0, 64, 8)])
+    within = (x[:64, 7].double()[:, None] * w[:, 7].double()).abs() <= MAX
+    assert within.sum() > within.numel() // 2
+    assert torch.equal(few.isnan()[within], many.isnan()[within]) and torch.equal(few.isinf()[within], many.isinf()[within])
