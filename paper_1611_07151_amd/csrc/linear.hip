@@ -773,10 +773,9 @@ template <typename TO> __global__ __launch_bounds__(256) void linear_join_kernel
 template <typename TI, typename TO, int RT, int CT, int MAXW, bool ODD> int launch_wave(const LinearArgs &p, int waves)
 {
     const int tr = (p.rows - 1) / RT + 1, tj = (p.Cout - 1) / CT + 1;
-    if (!one_launch((double)tr * tj, 64 * MAXW)) return SQ_ERR_UNSUPPORTED;
+    if (!one_launch((double)tr * tj, 64 * waves)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("linear_wave", linear_flops(p), linear_bytes(p));
-    hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW, ODD>), dim3((unsigned)tr * tj), dim3(64 * std::max(1, std::min(waves, MAXW))), 0,
-                       current_stream(), p, tr, tj);
+    hipLaunchKernelGGL((linear_wave_kernel<TI, TO, RT, CT, MAXW, ODD>), dim3((unsigned)tr * tj), dim3(64 * waves), 0, current_stream(), p, tr, tj);
     return check_launch();
 }
 
@@ -800,8 +799,8 @@ template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF, int 
 
 // Microseconds of a tiling, from what it measured (products of 128 to 8192 rows, layers and results): `fixed` for filling the
 // pipeline and writing the results, `step` for 128 bytes of k when `slots` workgroups share the chip, `alone` when each
-// has a compute unit to itself.
-struct Tiling { int BM, BN, slots; double fixed, step, alone; int teams; };
+// has a compute unit to itself.  `threads` of a workgroup.
+struct Tiling { int BM, BN, slots; double fixed, step, alone; int teams, threads; };
 double tiling_us(const Tiling &t, const LinearArgs &p, int Cin, int shares)
 {
     const long long tiles = (long long)((p.rows - 1) / t.BM + 1) * ((p.Cout - 1) / t.BN + 1) * shares;
@@ -814,15 +813,18 @@ double tiling_us(const Tiling &t, const LinearArgs &p, int Cin, int shares)
     const int each = (int)((rest + 255) / 256), most = t.slots / 256;
     return full * round(t.step, 1.0) + (rest ? round(most == 1 ? t.alone : t.alone + (t.step - t.alone) * (each - 1) / (most - 1), each == 1 ? 2.0 : 1.0) : 0.0);
 }
-const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6, 1}, {128, 128, 256, 4.5, 1.36, 1.2, 1}, {256, 128, 256, 8.5, 2.45, 2.1, 1},
-                       {64, 64, 256, 3.5, 0.55, 0.43, 2}, {32, 128, 256, 3.5, 0.66, 0.54, 2}};
-const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29, 1},  {128, 128, 256, 2.5, 0.57, 0.5, 1},  {128, 128, 512, 4.4, 1.0, 0.75, 1},
-                          {256, 256, 256, 9.0, 1.5, 1.25, 1}, {64, 64, 256, 2.5, 0.22, 0.19, 2}, {128, 64, 256, 3.5, 0.32, 0.3, 2}};
-const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45, 1}, {128, 128, 512, 4.0, 1.8, 0.85, 1}};
+const Tiling kF32[] = {{64, 64, 768, 3.0, 1.25, 0.6, 1, 256}, {128, 128, 256, 4.5, 1.36, 1.2, 1, 512}, {256, 128, 256, 8.5, 2.45, 2.1, 1, 512},
+                       {64, 64, 256, 3.5, 0.55, 0.43, 2, 512}, {32, 128, 256, 3.5, 0.66, 0.54, 2, 512}};
+const Tiling kDirect[] = {{64, 64, 512, 1.9, 0.4, 0.29, 1, 256},  {128, 128, 256, 2.5, 0.57, 0.5, 1, 512},  {128, 128, 512, 4.4, 1.0, 0.75, 1, 256},
+                          {256, 256, 256, 9.0, 1.5, 1.25, 1, 512}, {64, 64, 256, 2.5, 0.22, 0.19, 2, 512}, {128, 64, 256, 3.5, 0.32, 0.3, 2, 512}};
+const Tiling kAny[] = {{64, 64, 1024, 2.0, 1.45, 0.45, 1, 256}, {128, 128, 512, 4.0, 1.8, 0.85, 1, 512}};
 
 // How a product is made: by wavefronts in blocks of 16 x 16 or 32 x 32, or by a tiling, with k in shares of `share` values.
 enum { kWave16 = -1, kWave32 = -2 };
 struct Plan { int which, share, shares; };
+// Wavefronts of a workgroup that share out a sum of `steps` times 128 bytes.
+int wave_count(int which, int steps) { return which == kWave16 ? std::min(2 * steps, 16) : std::min(steps, 8); }
+double blocks_of(const LinearArgs &p, int rows, int layers) { return ((p.rows - 1) / rows + 1.0) * ((p.Cout - 1) / layers + 1.0); }
 
 // Few results: the wavefronts, in blocks of 16 x 16 up to 2^16 results, a short sum or 16 rows, else 32 x 32 (us, 16 / 32: 586 x
 // 1952 x 64 bf16 5.4 / 7.8, 99 x 3088 x 80 7.0 / 10.9; 45 x 1792 x 3520 12.9 / 9.5, 3458 x 2016 x 56 13.1 / 8.2).  Tiles through LDS
@@ -834,6 +836,7 @@ struct Plan { int which, share, shares; };
 // Where one workgroup's way through k leaves the chip idle, tiles in shares of k and a second launch that adds them up (3.8 us and
 // the sums' bytes), if that is to save 8 % (us, without / with: 300 x 4000 x 1000 fp32 50.5 / 26.6, 24 x 3691 x 3000 bf16 24.9 /
 // 11.7, 17 x 4096 x 4096 14.2 / 10.2; 42 x 728 x 7032 fp32 14.4 / 14.5, 64 x 1280 x 3712 bf16 7.0 / 8.8, 40 x 2500 x 150 6.2 / 9.1).
+// What has more threads than a launch takes is passed over; where nothing is left the launch refuses.
 Plan plan_of(const LinearArgs &p, bool direct)
 {
     const bool f32 = p.in_dtype == SQ_F32;
@@ -843,27 +846,29 @@ Plan plan_of(const LinearArgs &p, bool direct)
     const Tiling *const all = f32 ? kF32 : direct ? kDirect : kAny;
     const int n = f32 ? 5 : direct ? (teams ? 6 : 4) : 2;
     Plan best{0, p.Cin, 1};
-    double us = tiling_us(all[0], p, p.Cin, 1);
-    for (int i = 1; i < n; ++i) {
+    double us = HUGE_VAL;
+    for (int i = 0; i < n; ++i) {
+        if (!one_launch(blocks_of(p, all[i].BM, all[i].BN), all[i].threads)) continue;
         const double t = tiling_us(all[i], p, p.Cin, 1);
         if (t < us) us = t, best.which = i;
     }
     // the wavefronts: us for 1000 of k, of a block by itself and of a full chip's 256 (30 products); bf16 rows that begin
     // between words take more
     const bool small = p.rows <= 16 || results <= 65536 || steps <= 2;
-    const int B = small ? 16 : 32;
-    const double blocks = ((p.rows - 1) / B + 1.0) * ((p.Cout - 1) / B + 1.0);
+    const int B = small ? 16 : 32, which = small ? kWave16 : kWave32;
+    const double blocks = blocks_of(p, B, B);
     const bool far = ((double)p.rows + p.Cout) * p.Cin > 2e6;       // rows of blocks read kernels and input again: from beyond an XCD's cache
     const double one = small ? (f32 ? 2.0 : p.Cin % 2 == 0 ? 1.0 : 1.6) : (f32 ? 7.3 : 3.3);
     const double all256 = !small ? one : p.rows <= 16 ? (f32 ? 3.0 : 1.35 * one) : f32 ? (far ? 4.3 : 2.7) : 1.6 * one;
     const double waves = 4.0 + std::max(std::ceil(blocks / 256) * one, blocks / 256 * all256) * p.Cin * 1e-3;
     const double many = direct && !teams ? 1 << 18 : 1 << 16;
-    if (p.rows <= 16 || results <= many || (f32 && (waves < us || (steps <= 2 && results < 1 << 20)))) us = waves, best.which = small ? kWave16 : kWave32;
+    if (one_launch(blocks, 64 * wave_count(which, steps)) && (p.rows <= 16 || results <= many || (f32 && (waves < us || (steps <= 2 && results < 1 << 20)))))
+        us = waves, best.which = which;
     us *= 0.92;
     if (steps < 16 || us < 3.8 + 1.9) return best;
     for (int i = 0; i < n; ++i) {
         const Tiling &t = all[i];
-        const double tiles = ((p.rows - 1) / t.BM + 1.0) * ((p.Cout - 1) / t.BN + 1.0);
+        const double tiles = blocks_of(p, t.BM, t.BN);
         const int units = p.Cin / (unit * t.teams);
         for (int want = 2; want <= kMostShares && tiles * want <= 512; ++want) {
             const int share = ((units - 1) / want + 1) * unit * t.teams, shares = (units * unit * t.teams - 1) / share + 1;
@@ -915,13 +920,13 @@ template <typename TI, typename TO> int by_size(LinearArgs p)
     const Plan plan = plan_of(p, direct);
     p.ld_w = p.Cin;
     p.share = plan.share, p.shares = plan.shares;
-    const int steps = (p.Cin - 1) / (128 / (int)sizeof(TI)) + 1;
+    const int waves = wave_count(plan.which, (p.Cin - 1) / (128 / (int)sizeof(TI)) + 1);
     if (plan.which == kWave16) {
         if constexpr (sizeof(TI) == 2)
-            if (between_words(p)) return launch_wave<TI, TO, 16, 16, 16, true>(p, 2 * steps);
-        return launch_wave<TI, TO, 16, 16, 16, false>(p, 2 * steps);
+            if (between_words(p)) return launch_wave<TI, TO, 16, 16, 16, true>(p, waves);
+        return launch_wave<TI, TO, 16, 16, 16, false>(p, waves);
     }
-    if (plan.which == kWave32) return launch_wave<TI, TO, 32, 32, 8, false>(p, steps);
+    if (plan.which == kWave32) return launch_wave<TI, TO, 32, 32, 8, false>(p, waves);
     if (plan.shares == 1) return launch_tiling<TI, TO>(p, plan.which, direct);
     LinearArgs part = p;
     part.b = nullptr, part.residual = nullptr, part.act = SQ_ACT_NONE;

@@ -1,4 +1,4 @@
-"""Channels-last operators at the ends of the number format.
+"""Channels-last operators at the ends of the number format and of the sizes.
 
 u = 2^-24 is half a unit of fp32's last place.
 """
@@ -75,3 +75,19 @@ def test_few_and_many_rows_agree_on_what_is_not_finite(sq, rows, cin, cout):
     within = (x[:64, 7].double()[:, None] * w[:, 7].double()).abs() <= MAX
     assert within.sum() > within.numel() // 2
     assert torch.equal(few.isnan()[within], many.isnan()[within]) and torch.equal(few.isinf()[within], many.isinf()[within])
+
+
+# --------------------------------------------------------------------------------------------------------- large sizes
+@pytest.mark.parametrize("rows,cin,cout", [(16777216, 3, 64), (67108864, 3, 8), (2 ** 29, 1, 8)])
+def test_linear_of_many_rows_with_a_short_sum(sq, rows, cin, cout):
+    """fp32, more blocks of 16 x 16 than a launch of 1024 threads each has, and (the last) than one of 128 has."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn((rows, cin), generator=g, device="cuda")
+    w = torch.randn((cout, cin), generator=g, device="cuda")
+    b = torch.randn(cout, generator=g, device="cuda")
+    got = sq.sq_linear_forward(x, w, b, act=1)
+    for r in list(range(0, rows, rows // 5)) + [rows - (1 << 20)]:
+        part = x[r:r + (1 << 20)].double()
+        ref = (part @ w.double().t() + b.double()).clamp(min=0)
+        bound = (cin + 16) * 2 * U * (part.abs() @ w.double().abs().t() + b.double().abs())
+        assert ((got[r:r + (1 << 20)].double() - ref).abs() <= bound).all(), r
