@@ -810,11 +810,13 @@ def sq_nhwc_pack(x, dtype=None, out=None):
 
 def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
     """Channels-last map [N][H][W][C] -> NCHW of `dtype`.  `out` may be a larger [N][C'][H][W] tensor; the result lands in
-    layers [c_offset, c_offset + C) and its type is that of out."""
+    layers [c_offset, c_offset + C) and its type is that of out.  Without `out` the layers before c_offset are zeros."""
     N, H, W, C = m.shape
     index, c_offset = _gpu_of(m, "m"), int(c_offset)
     if out is None:
-        out = m.new_empty((N, C + c_offset, H, W), dtype=dtype)
+        out = m.new_empty((N, C + max(0, c_offset), H, W), dtype=dtype)
+        if c_offset > 0:
+            out[:, :c_offset].zero_()
         address = out.data_ptr()
     else:
         if out.dim() != 4 or (out.shape[0], out.shape[2], out.shape[3]) != (N, H, W):

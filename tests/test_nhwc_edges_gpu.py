@@ -5,7 +5,7 @@ u = 2^-24 is half a unit of fp32's last place.
 import pytest
 import torch
 
-from test_nhwc_gpu import F32, U, gen
+from test_nhwc_gpu import BF16, F32, U, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,15 @@ def test_linear_of_many_rows_with_a_short_sum(sq, rows, cin, cout):
         ref = (part @ w.double().t() + b.double()).clamp(min=0)
         bound = (cin + 16) * 2 * U * (part.abs() @ w.double().abs().t() + b.double().abs())
         assert ((got[r:r + (1 << 20)].double() - ref).abs() <= bound).all(), r
+
+
+# ------------------------------------------------------------------------------------------------------------ conversion
+@pytest.mark.parametrize("dst", (F32, BF16))
+def test_unpack_behind_layers_that_nothing_has_written(sq, dst):
+    """Without a map to write into, the layers before c_offset are zeros."""
+    torch.full((1 << 20,), float("nan"), device="cuda")      # what the allocator hands out next is not zero
+    m = torch.randn((2, 9, 7, 5), generator=gen(1)).cuda()
+    for off in (0, 1, 3):
+        got = sq.sq_nhwc_unpack(m, dtype=dst, c_offset=off)
+        assert got.shape == (2, 5 + off, 9, 7) and not got[:, :off].any()
+        assert torch.equal(got[:, off:], m.permute(0, 3, 1, 2).to(dst))
