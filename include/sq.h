@@ -534,8 +534,9 @@ int sq_nhwc_unpack(const void *in, sq_dtype in_dtype, void *out, sq_dtype out_dt
  *   workspace: sq_nhwc_group_norm_workspace_bytes(N, C, H, W, G) bytes of device scratch, 256-byte
  *     aligned (else SQ_ERR_WORKSPACE; 0 = none is needed, workspace may be NULL).  Contents on
  *     return are unspecified; two calls in flight at once need two.
- *   An infinity or NaN makes its own image and group NaN and no other.  The squares of the values'
- *   deviations have to stay within fp32.  The same call gives the same bits every time.
+ *   An infinity or NaN makes its own image and group NaN and no other.  The sum of a group's values
+ *   and that of their squared deviations have to stay within fp32.  The same call gives the same bits
+ *   every time.
  * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE (incl. C not a multiple of G), SQ_ERR_UNSUPPORTED,
  * SQ_ERR_WORKSPACE, SQ_ERR_HIP.
  */

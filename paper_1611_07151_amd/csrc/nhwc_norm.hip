@@ -346,7 +346,7 @@ template <typename T, int VB, int K> __global__ __launch_bounds__(256) void grou
                 }
             const float d = s - mean[i];
             mean[i] = __builtin_fmaf(d, part, mean[i]);
-            m2[i] += q + d * d * cross;
+            m2[i] += q + (count > 0.f ? d * d * cross : 0.f);      // of the first rows d is the mean itself, whose square may overflow
         }
         count = both;
     };
@@ -360,7 +360,7 @@ template <typename T, int VB, int K> __global__ __launch_bounds__(256) void grou
     for (int i = 0; i < n; ++i) middle[i] = mean[i] * (count / values);
     group_sums(p, at, middle, lds, sums);
 #pragma unroll
-    for (int i = 0; i < n; ++i) m2[i] += (mean[i] - middle[i]) * (mean[i] - middle[i]) * count;
+    for (int i = 0; i < n; ++i) m2[i] += count > 0.f ? (mean[i] - middle[i]) * (mean[i] - middle[i]) * count : 0.f;     // as above
     group_sums(p, at, m2, lds, sums);
     // each group's by the thread of the first row that holds its first layer
     if (at.live && at.row == 0) {

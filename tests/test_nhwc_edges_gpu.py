@@ -5,7 +5,7 @@ u = 2^-24 is half a unit of fp32's last place.
 import pytest
 import torch
 
-from test_nhwc_gpu import BF16, F32, U, gen
+from test_nhwc_gpu import BF16, F32, U, check, gen, half_step, norm_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +103,16 @@ def test_unpack_behind_layers_that_nothing_has_written(sq, dst):
         got = sq.sq_nhwc_unpack(m, dtype=dst, c_offset=off)
         assert got.shape == (2, 5 + off, 9, 7) and not got[:, :off].any()
         assert torch.equal(got[:, off:], m.permute(0, 3, 1, 2).to(dst))
+
+
+# ------------------------------------------------------------------------------------------------------------ group norm
+@pytest.mark.parametrize("n,h,w,c,groups", [(2, 13, 13, 64, 8), (2, 80, 80, 64, 4), (1, 200, 130, 8, 1), (1, 9, 9, 5000, 2), (1, 20, 20, 9999, 1),
+                                            (2, 61, 60, 200, 4), (1, 111, 111, 96, 8), (3, 64, 64, 999, 3)])
+@pytest.mark.parametrize("far", (1e19, 4e19, -4e19, 1e22))
+def test_group_norm_of_means_whose_squares_overflow(sq, n, h, w, c, groups, far):
+    """The deviations' squares stay within fp32, the mean's does not."""
+    x = (far * (1 + torch.randn((n, h, w, c), generator=gen(8)).double() * 1e-4 * min(1.0, 1e19 / abs(far)))).float()
+    ref, bound = norm_ref(x.double(), groups, torch.ones(c).double(), torch.zeros(c).double(), 1e-5, 0)
+    got = sq.sq_nhwc_group_norm(x.cuda(), groups)
+    assert not got.isnan().any()
+    check(got, ref, bound + half_step(ref, F32), (n, h, w, c, groups, far))
