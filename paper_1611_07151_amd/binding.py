@@ -722,6 +722,20 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 _current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+def _sizes_of(t, name):
+    """Refuses a size past the library's 32 bits, which ctypes would cut."""
+    if t.numel() > _MAX_INT and max(t.shape) > _MAX_INT:
+        _check(-3, name)
+
+
+def _int(value, status, what):
+    """`value` as an int, refused past 32 bits."""
+    value = int(value)
+    if not -_MAX_INT <= value <= _MAX_INT:
+        _check(status, what)
+    return value
+
+
 def _gpu_of(x, name):
     index = x.get_device()
     if index < 0:
@@ -797,6 +811,7 @@ def sq_nhwc_pack(x, dtype=None, out=None):
     """NCHW float32 / bfloat16 -> channels-last map [N][H][W][C] of `dtype` (default: that of x or of out)."""
     N, C, H, W = x.shape
     index = _gpu_of(x, "x")
+    _sizes_of(x, "x")
     if out is None:
         out, ld = x.new_empty((N, H, W, C), dtype=dtype or x.dtype), C
     else:
@@ -812,7 +827,7 @@ def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
     """Channels-last map [N][H][W][C] -> NCHW of `dtype`.  `out` may be a larger [N][C'][H][W] tensor; the result lands in
     layers [c_offset, c_offset + C) and its type is that of out.  Without `out` the layers before c_offset are zeros."""
     N, H, W, C = m.shape
-    index, c_offset = _gpu_of(m, "m"), int(c_offset)
+    index, c_offset = _gpu_of(m, "m"), _int(c_offset, -2, "sq_nhwc_unpack")
     if out is None:
         out = m.new_empty((N, C + max(0, c_offset), H, W), dtype=dtype)
         if c_offset > 0:
@@ -821,6 +836,7 @@ def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
     else:
         if out.dim() != 4 or (out.shape[0], out.shape[2], out.shape[3]) != (N, H, W):
             raise ValueError("out has the wrong shape")
+        _sizes_of(out, "out")
         address = _dense(out, "out", index, out.dtype)
     _run(index, "sq_nhwc_unpack", lib.sq_nhwc_unpack, m.data_ptr(), _dtype_code(m, "m"), address, _dtype_code(out, "out"),
          N, C, H, W, _rows_of(m, "m", index), out.shape[1], c_offset)
@@ -829,6 +845,8 @@ def sq_nhwc_unpack(m, dtype=torch.float32, out=None, c_offset=0):
 
 @functools.lru_cache(maxsize=4096)      # a function of the sizes alone
 def sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups) -> int:
+    if max(N, C, H, W, groups) > _MAX_INT or min(N, C, H, W, groups) <= 0:
+        return 0
     return int(lib.sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups))
 
 
@@ -844,16 +862,18 @@ def sq_nhwc_group_norm(m, groups, gamma=None, beta=None, eps=1e-5, act=SQ_ACT_NO
         raise ValueError("out has the wrong shape or type")
     if gamma is not None and gamma.numel() != C or beta is not None and beta.numel() != C:
         raise ValueError("gamma and beta must have one value per layer")
-    ld_in, ld_out, groups = _rows_of(m, "m", index), _rows_of(out, "out", index), int(groups)
+    ld_in, ld_out, groups = _rows_of(m, "m", index), _rows_of(out, "out", index), _int(groups, -2, "sq_nhwc_group_norm")
     workspace, address, nbytes = _scratch(workspace, sq_nhwc_group_norm_workspace_bytes(N, C, H, W, groups), m, index)
     _run(index, "sq_nhwc_group_norm", lib.sq_nhwc_group_norm, m.data_ptr(), out.data_ptr(), _dtype_code(m, "m"),
          _dense(gamma, "gamma", index, torch.float32), _dense(beta, "beta", index, torch.float32), N, C, H, W, groups, eps,
-         int(act), ld_in, ld_out, address, nbytes)
+         _int(act, -3, "sq_nhwc_group_norm"), ld_in, ld_out, address, nbytes)
     return out
 
 
 @functools.lru_cache(maxsize=4096)      # a function of the sizes alone
 def _linear_need(rows, Cin, Cout, code, ld_in, aligned):
+    if max(rows, Cin, Cout, ld_in) > _MAX_INT or min(rows, Cin, Cout, ld_in) <= 0:
+        return 0
     return int(lib.sq_linear_workspace_bytes(rows, Cin, Cout, code, ld_in, aligned))
 
 
@@ -899,7 +919,7 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
     workspace, address, nbytes = _scratch(workspace, need, x, index)
     _run(index, "sq_linear_forward", lib.sq_linear_forward, x_at, w_at,
          _dense(b, "b", index, torch.float32), res, out.data_ptr(), code, _dtype_code(out, "out"), rows, Cin, Cout,
-         int(act), ld_in, ld_res, ld_out, address, nbytes)
+         _int(act, -3, "sq_linear_forward"), ld_in, ld_res, ld_out, address, nbytes)
     return out
 
 

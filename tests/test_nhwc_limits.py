@@ -42,3 +42,46 @@ def test_products_that_fit_a_launch_are_not_refused(lib, ti):
             if min(rows, cout) > 0 and max(rows, cout) <= 2 ** 29 and rows * cout <= 2 ** 35:
                 for cin in (1, 3, 8, 16, 32, 33, 40, 64, 65, 257, 1000, 4096):
                     assert linear(lib, rows, cin, cout, ti) == HIP, (rows, cin, cout)
+
+
+class _OnGpu(torch.Tensor):
+    """A tensor without memory that says it lives on GPU 0."""
+    @staticmethod
+    def of(*shape, dtype=torch.float32):
+        return torch.empty(shape, device="meta", dtype=dtype).as_subclass(_OnGpu)
+
+    def get_device(self):
+        return 0
+
+    def data_ptr(self):
+        return 0        # the library itself would say "null"
+
+
+@without_gpu
+def test_numbers_past_32_bits_are_refused_and_not_cut(monkeypatch):
+    import paper_1611_07151_amd as sq
+    monkeypatch.setattr(sq.binding, "_current_gpu", lambda: 0)
+    monkeypatch.setattr(sq.binding, "_raw_stream", lambda index: 0)
+    big = 2 ** 32 + 8
+    m, w = _OnGpu.of(2, 3, 3, 16), _OnGpu.of(4, 16)
+
+    def refused(status, f, *args, **kw):
+        with pytest.raises(sq.SqError) as e:
+            f(*args, **kw)
+        assert e.value.status == status
+
+    refused(-3, sq.sq_nhwc_pack, _OnGpu.of(1, 1, 1, big))
+    refused(-3, sq.sq_nhwc_pack, _OnGpu.of(big, 1, 1, 1))
+    refused(-3, sq.sq_nhwc_pack, _OnGpu.of(1, big, 1, 1))
+    refused(-3, sq.sq_nhwc_unpack, m, out=_OnGpu.of(2, big + 8, 3, 3))
+    refused(-2, sq.sq_nhwc_unpack, m, out=_OnGpu.of(2, 16, 3, 3), c_offset=2 ** 32)
+    for groups in (2 ** 32 + 4, 4 - 2 ** 32):
+        refused(-2, sq.sq_nhwc_group_norm, m, groups)
+        refused(-2, sq.sq_nhwc_group_norm, m, groups, workspace=m)
+    for act in (2 ** 32 + 1, 1 - 2 ** 32):
+        refused(-3, sq.sq_nhwc_group_norm, m, 4, act=act)
+        refused(-3, sq.sq_linear_forward, m, w, act=act)
+    assert sq.sq_nhwc_group_norm_workspace_bytes(big, 64, 80, 80, 4) == 0
+    assert sq.sq_nhwc_group_norm_workspace_bytes(2, 64, 80, 80, 2 ** 32 + 4) == 0
+    assert sq.sq_linear_workspace_bytes(2 ** 32 + 300, 2048, 300) == 0
+    assert sq.sq_linear_workspace_bytes(300, 2048, 300, ld_in=2 ** 32 + 2048) == 0
