@@ -494,9 +494,11 @@ int sq_squeezenet_forward_bf16(const void *in, sq_dtype in_dtype, const void *co
  *   act: one of the codes below; anything else SQ_ERR_UNSUPPORTED.
  *   Every pointer must be aligned to the size of its values (else SQ_ERR_UNSUPPORTED); rows whose
  *     address and ld are multiples of 16 bytes are read and written fastest.
- *   Sizes: offsets are 64-bit.  A call that would need 2^32 threads or more in one launch returns
- *     SQ_ERR_UNSUPPORTED: conversions and group norms of some 2^24 workgroups, each of one image or a
- *     part of one; products from more than 2^29 rows, 2^29 layers or 2^35 results on.
+ *   Sizes: offsets are 64-bit.  A launch takes fewer than 2^32 threads.  Conversions and group norms
+ *     take any N, in several launches where it needs them.  One launch always has room for an image of
+ *     2^29 pixels, 2^29 layers and 2^34 values (conversions) or of 2^21 groups (group norms), and for a
+ *     product of 2^29 rows, 2^29 layers and 2^35 results; what is larger and has no room in one returns
+ *     SQ_ERR_UNSUPPORTED.
  *   The arithmetic mode of sq_set_dtype() does not matter to these calls.
  */
 enum {

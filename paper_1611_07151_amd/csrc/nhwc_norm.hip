@@ -587,7 +587,6 @@ Plan make_plan(int N, int C, long long HW, int G, int size)
 template <typename T, int VB, int KEEP> int launch_fused(const NormArgs &p, const Plan &q)
 {
     const double values = (double)p.N * p.HW * p.C;
-    if (!one_launch((double)p.N * q.blocks, q.threads)) return SQ_ERR_UNSUPPORTED;
     const LaunchScope prof("group_norm", 10.0 * values, 2.0 * sizeof(T) * values, 0.0);
     hipLaunchKernelGGL((group_norm_fused<T, VB, KEEP / VB>), dim3((unsigned)p.N * q.blocks), dim3(q.threads), 0, current_stream(), p);
     return check_launch();
@@ -604,7 +603,6 @@ template <typename T, int VB> int launch(const NormArgs &p, const Plan &q)
             return launch_fused<T, VB, keep_most(VB)>(p, q);
         }
         const double values = (double)p.N * p.HW * p.C;
-        if (!one_launch((double)p.N * q.blocks * q.chunks, 256)) return SQ_ERR_UNSUPPORTED;
         const unsigned grid = (unsigned)p.N * q.blocks * q.chunks;
         {
             const LaunchScope prof("group_norm_moments", 4.0 * values, sizeof(T) * values, 0.0);
@@ -665,7 +663,17 @@ int nhwc_group_norm(const void *in, void *out, int dtype, const float *gamma, co
     NormArgs p{in, out, gamma, beta, N, C, G, HW, ld_in, ld_out, eps, act, q.width, q.groups, q.parts, q.blocks, q.chunks, q.chunk, nullptr, nullptr};
     p.stats = q.combine ? (float *)workspace : nullptr;
     p.partial = (float *)((char *)workspace + align_up((size_t)N * G * 8, 256));
-    return dtype == SQ_F32 ? by_vector<float>(p, q) : by_vector<bf16_t>(p, q);
+    const int threads = q.fused ? q.threads : 256, size = dtype == SQ_F32 ? 4 : 2;
+    const double each = (double)q.blocks * q.chunks;
+    if (!one_launch(each, threads)) return SQ_ERR_UNSUPPORTED;
+    const int most = images_in_one_launch(N, each, threads);
+    for (long long n = 0; n < N; n += most) {       // one after the other, with the same scratch
+        p.N = (int)std::min<long long>(most, N - n);
+        if (const int rc = size == 4 ? by_vector<float>(p, q) : by_vector<bf16_t>(p, q)) return rc;
+        p.in = (const char *)p.in + (long long)p.N * HW * ld_in * size;
+        p.out = (char *)p.out + (long long)p.N * HW * ld_out * size;
+    }
+    return SQ_OK;
 }
 
 }  // namespace sq

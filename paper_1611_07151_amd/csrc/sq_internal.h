@@ -204,6 +204,11 @@ int softmax(const float *in, float *out, int N, int C);
 
 // Whether `blocks` workgroups of `threads` fit one launch (the runtime counts the threads of a grid in 32 bits).
 inline bool one_launch(double blocks, int threads) { return blocks * threads < 4294967296.0; }
+// How many of N images with `blocks` workgroups of `threads` each go into one launch; those of one image have to.
+inline int images_in_one_launch(int N, double blocks, int threads)
+{
+    return one_launch(N * blocks, threads) ? N : (int)(4294967295.0 / (blocks * threads));
+}
 // Channels-last maps: [N][HW] rows of ld values, the first C of them the operator's (nhwc_layout.hip, nhwc_norm.hip).
 int nhwc_pack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld);
 int nhwc_unpack(const void *in, int in_dtype, void *out, int out_dtype, int N, int C, long long HW, long long ld, int out_channels);

@@ -93,6 +93,34 @@ def test_linear_of_many_rows_with_a_short_sum(sq, rows, cin, cout):
         assert ((got[r:r + (1 << 20)].double() - ref).abs() <= bound).all(), r
 
 
+def test_conversions_of_many_small_maps(sq):
+    """More maps than a launch has workgroups."""
+    n, c = 2 ** 24 + 37, 3
+    x = torch.arange(n * c, dtype=torch.int32, device="cuda").remainder(65521).float().reshape(n, c, 1, 1)
+    assert torch.equal(sq.sq_nhwc_pack(x).reshape(n, c), x.reshape(n, c))
+    wide = torch.full((n, 1, 1, 5), float("nan"), device="cuda")
+    m = wide[..., 1:4]
+    sq.sq_nhwc_pack(x, out=m)
+    assert torch.equal(m.reshape(n, c), x.reshape(n, c)) and wide[..., 0].isnan().all() and wide[..., 4].isnan().all()
+    out = torch.full((n, 5, 1, 1), float("nan"), device="cuda")
+    sq.sq_nhwc_unpack(m, out=out, c_offset=2)
+    assert torch.equal(out[:, 2:].reshape(n, c), x.reshape(n, c)) and out[:, :2].isnan().all()
+
+
+@pytest.mark.parametrize("dt", (F32, BF16))
+@pytest.mark.parametrize("n,c,groups", [(2 ** 24 + 37, 8, 1), (2 ** 24 + 37, 8, 8), (2 ** 26 + 37, 4, 1)])
+def test_group_norm_of_many_small_maps(sq, n, c, groups, dt):
+    """More maps than a launch has workgroups; and the same bits as the maps by themselves."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn((n, 1, 1, c), generator=g, device="cuda").to(dt)
+    gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+    got = sq.sq_nhwc_group_norm(x, groups, gamma, beta, act=1)
+    for i in list(range(0, n, n // 7)) + [n - 4096]:
+        part = x[i:i + 4096].cpu().double()
+        ref, bound = norm_ref(part, groups, gamma.cpu().double(), beta.cpu().double(), 1e-5, 1)
+        check(got[i:i + 4096], ref, bound + half_step(ref, dt), i)
+
+
 # ------------------------------------------------------------------------------------------------------------ conversion
 @pytest.mark.parametrize("dst", (F32, BF16))
 def test_unpack_behind_layers_that_nothing_has_written(sq, dst):

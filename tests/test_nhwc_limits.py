@@ -44,6 +44,36 @@ def test_products_that_fit_a_launch_are_not_refused(lib, ti):
                     assert linear(lib, rows, cin, cout, ti) == HIP, (rows, cin, cout)
 
 
+@without_gpu
+def test_maps_that_fit_the_memory_are_not_refused(lib):
+    for ti in (0, 1):
+        for n in (1, 3, 2 ** 16 + 1, 2 ** 24 - 1, 2 ** 24, 2 ** 26, 2 ** 28 + 1, 2 ** 31 - 1):
+            for c in (1, 3, 8, 30, 64, 512):
+                for h, w in ((1, 1), (1, 2), (7, 7), (111, 111), (1024, 1024)):
+                    if n * c * h * w * 4 > 2 ** 37:
+                        continue
+                    assert lib.sq_nhwc_pack(P, ti, P, 0, n, c, h, w, c) == HIP, (n, c, h, w)
+                    assert lib.sq_nhwc_unpack(P, 0, P, ti, n, c, h, w, c, c + 2, 1) == HIP, (n, c, h, w)
+                    for g in {1, 2 - c % 2, c}:
+                        need = lib.sq_nhwc_group_norm_workspace_bytes(n, c, h, w, g)
+                        assert lib.sq_nhwc_group_norm(P, P, ti, NULL, NULL, n, c, h, w, g, 1e-5, 0, c, c, P, need) == HIP, (n, c, h, w, g)
+
+
+@without_gpu
+@pytest.mark.parametrize("ti", (0, 1))
+def test_images_that_fit_a_launch_are_not_refused(lib, ti):
+    """Up to 2^29 pixels, 2^29 layers and 2^34 values of an image in the conversions, and 2^21 groups in the group norm."""
+    sizes = sorted({2 ** e + d for e in range(30) for d in (-1, 0, 1)})
+    for c in sizes:
+        for w in sizes:
+            if 0 < min(c, w) and max(c, w) <= 2 ** 29 and c * w <= 2 ** 34:
+                assert lib.sq_nhwc_pack(P, ti, P, 0, 2, c, 1, w, c) == HIP, (c, w)
+                assert lib.sq_nhwc_unpack(P, ti, P, 1, 2, c, 1, w, c, c, 0) == HIP, (c, w)
+                for g in {g for g in (1, 2, 3, c, c // 2, c // 3, c // 64) if 0 < g <= 2 ** 21 and c % g == 0}:
+                    need = lib.sq_nhwc_group_norm_workspace_bytes(2, c, 1, w, g)
+                    assert lib.sq_nhwc_group_norm(P, P, ti, NULL, NULL, 2, c, 1, w, g, 1e-5, 0, c, c, P, need) == HIP, (c, w, g)
+
+
 class _OnGpu(torch.Tensor):
     """A tensor without memory that says it lives on GPU 0."""
     @staticmethod
