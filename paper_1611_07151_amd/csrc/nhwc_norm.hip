@@ -322,8 +322,10 @@ template <typename T, int VB, int K> __global__ __launch_bounds__(256) void grou
     const T *in = (const T *)p.in + ((long long)at.image * p.HW + at.begin + at.row) * p.ld_in + c;
     float mean[n] = {}, m2[n] = {}, count = 0.f;
     const long long step = (long long)at.rows * K;
-    auto take = [&](auto full, const Turn<K> &turn) {      // full: all K rows, with no test between the loads and their use
-        constexpr bool kFull = decltype(full)::value;
+    // full: all K rows, with no test between the loads and their use; first: nothing to combine them with (as an empty count it would be
+    // mean^2 * 0, and the square may overflow)
+    auto take = [&](auto full, auto first, const Turn<K> &turn) {
+        constexpr bool kFull = decltype(full)::value, kFirst = decltype(first)::value;
         Vector<T, VB> x[K];
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -344,15 +346,25 @@ template <typename T, int VB, int K> __global__ __launch_bounds__(256) void grou
                     const float d = x[k].get(i) - s;
                     q = __builtin_fmaf(d, d, q);
                 }
-            const float d = s - mean[i];
-            mean[i] = __builtin_fmaf(d, part, mean[i]);
-            m2[i] += q + (count > 0.f ? d * d * cross : 0.f);      // of the first rows d is the mean itself, whose square may overflow
+            if constexpr (kFirst) {
+                mean[i] = s;
+                m2[i] = q;
+            } else {
+                const float d = s - mean[i];
+                mean[i] = __builtin_fmaf(d, part, mean[i]);
+                m2[i] += q + d * d * cross;
+            }
         }
         count = both;
     };
     long long left = at.end - at.begin;
-    for (; left >= step; left -= step, in += step * p.ld_in) take(std::true_type{}, Turn<K>(at, left));
-    if (left > 0) take(std::false_type{}, Turn<K>(at, left));
+    if (left < step) {
+        take(std::false_type{}, std::true_type{}, Turn<K>(at, left));
+    } else {
+        take(std::true_type{}, std::true_type{}, Turn<K>(at, left));
+        for (left -= step, in += step * p.ld_in; left >= step; left -= step, in += step * p.ld_in) take(std::true_type{}, std::false_type{}, Turn<K>(at, left));
+        if (left > 0) take(std::false_type{}, std::false_type{}, Turn<K>(at, left));
+    }
     const int cg = p.parts > 1 ? at.width : p.C / p.G;
     const float values = (float)(at.end - at.begin) * (float)cg;
     float middle[n];
@@ -360,7 +372,10 @@ template <typename T, int VB, int K> __global__ __launch_bounds__(256) void grou
     for (int i = 0; i < n; ++i) middle[i] = mean[i] * (count / values);
     group_sums(p, at, middle, lds, sums);
 #pragma unroll
-    for (int i = 0; i < n; ++i) m2[i] += count > 0.f ? (mean[i] - middle[i]) * (mean[i] - middle[i]) * count : 0.f;     // as above
+    for (int i = 0; i < n; ++i) {
+        const float dd = count > 0.f ? (mean[i] - middle[i]) * (mean[i] - middle[i]) : 0.f;     // a thread without rows has no mean
+        m2[i] += dd * count;
+    }
     group_sums(p, at, m2, lds, sums);
     // each group's by the thread of the first row that holds its first layer
     if (at.live && at.row == 0) {
