@@ -1,11 +1,13 @@
-"""Channels-last operators at the ends of the number format and of the sizes.
+"""Channels-last operators at the ends of the number format and of the sizes, and the accuracy that the fp32 products promise.
 
 u = 2^-24 is half a unit of fp32's last place.
 """
+import math
+
 import pytest
 import torch
 
-from test_nhwc_gpu import BF16, F32, U, check, gen, half_step, norm_ref
+from test_nhwc_gpu import BF16, F32, U, check, gen, half_step, linear_case, norm_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -75,6 +77,56 @@ def test_few_and_many_rows_agree_on_what_is_not_finite(sq, rows, cin, cout):
     within = (x[:64, 7].double()[:, None] * w[:, 7].double()).abs() <= MAX
     assert within.sum() > within.numel() // 2
     assert torch.equal(few.isnan()[within], many.isnan()[within]) and torch.equal(few.isinf()[within], many.isinf()[within])
+
+
+# --------------------------------------------------------------------------------------- every bit of an fp32 operand
+@pytest.mark.parametrize("rows,cin,cout", FP32_FORMS)
+def test_fp32_products_are_exact_where_fp32_is(sq, rows, cin, cout):
+    """One operand a row that is not zero, so that a result is one product, of as many bits as fp32 holds: any 24 bits times a
+    power of two from either side, and (1 + i 2^-11)(1 + j 2^-11) with i, j < 16, which has 23.  Every value is found at every
+    step of k; a lost or rounded part of an operand, or a product of two parts left out, shows."""
+    g = gen(cin)
+    k = torch.linspace(0, cin - 1, rows).round().long()
+    at = torch.arange(rows)
+    bits = lambda *s: (torch.randint(0, 2 ** 23, s, generator=g).double() / 2 ** 23 + 1) * (torch.randint(0, 2, s, generator=g) * 2 - 1)
+    powers = lambda *s: torch.exp2(torch.randint(-20, 21, s, generator=g).double()) * (torch.randint(0, 2, s, generator=g) * 2 - 1)
+    short = lambda *s: 1 + torch.randint(1, 16, s, generator=g).double() / 2 ** 11
+    for left, right in ((bits, powers), (powers, bits), (short, short)):
+        x = torch.zeros((rows, cin), dtype=torch.float64)
+        x[at, k] = left(rows)
+        w = right(cout, cin)
+        want = x[at, k][:, None] * w[:, k].t()
+        assert torch.equal(want.float().double(), want)
+        got = sq.sq_linear_forward(x.float().cuda(), w.float().cuda()).cpu()
+        assert torch.equal(got, want.float())
+
+
+@pytest.mark.parametrize("rows,cin,cout", FP32_FORMS + [(200, 4096, 520), (1000, 8200, 64)])
+def test_fp32_products_lose_no_more_than_fp32_sums(sq, rows, cin, cout):
+    """Normally distributed operands: partial sums grow like a random walk, so n additions that are each off by at most 2u of
+    the partial sum, independently, leave 2u sqrt(n / 2) of the result (root mean square), and n <= 6/16 of Cin instructions
+    add to a sum; the terms' own products, and what a product leaves out, are below 4u.  1.5 sqrt(Cin) u + 4u covers these
+    (operands of 16 bits would give 200 u, of 8 bits 40000 u)."""
+    x, w = torch.randn((rows, cin), generator=gen(3)).cuda(), torch.randn((cout, cin), generator=gen(4)).cuda()
+    got = sq.sq_linear_forward(x, w).double()
+    ref = x.double() @ w.double().t()
+    off = float(((got - ref).norm() / ref.norm()).cpu())
+    assert off <= (1.5 * math.sqrt(cin) + 4) * U, off / U
+
+
+# ----------------------------------------------------------------------- tilings and shares that other shapes do not reach
+@pytest.mark.parametrize("ti,to,rows,cin,cout", [
+    # bf16 rows of whole 16-byte pieces: 128 x 128 tiles with two images in LDS, and k in shares with each large tile
+    (BF16, BF16, 3099, 1664, 2400), (BF16, F32, 9481, 32, 395), (BF16, BF16, 2500, 624, 1500), (BF16, BF16, 322, 8128, 5807),
+    (BF16, BF16, 3418, 3808, 69), (BF16, F32, 599, 5208, 1336), (BF16, BF16, 3973, 7408, 1033), (BF16, F32, 8268, 7384, 199),
+    (BF16, BF16, 889, 5816, 399), (BF16, F32, 5581, 5664, 19),
+    # bf16 rows at any address, 128 x 128 in shares
+    (BF16, BF16, 68, 2365, 3480), (BF16, F32, 243, 2971, 4634),
+    # fp32: one team of 64 x 64, and 128 x 128 and 256 x 128, in shares; 32 x 128 without
+    (F32, F32, 17, 5391, 45), (F32, F32, 2806, 1343, 71), (F32, F32, 5518, 1169, 129), (F32, F32, 8223, 1562, 68), (F32, F32, 2043, 85, 429)])
+def test_linear_in_every_tiling(sq, ti, to, rows, cin, cout):
+    linear_case(sq, rows, cin, cout, 0, ti, to, rows, bias=False, residual=False)
+    linear_case(sq, rows, cin, cout, 3, ti, to, rows + 1, pads=(8 if cin % 8 == 0 else 3, 3, 5))
 
 
 # --------------------------------------------------------------------------------------------------------- large sizes
