@@ -1,6 +1,6 @@
 // NCHW maps to channels-last rows and back: a transposition of each image's [layers][pixels] matrix with a conversion on the
-// way.  Bound by memory: 64 x 55 x 55 x 128 fp32 to bf16 in 24 us (6.1 TB/s), fp32 back to NCHW in 32 us (6.2 TB/s); one map of
-// 13 x 13 x 512 in 3.8 us, which is the launch.
+// way.  Bound by memory: 64 x 55 x 55 x 128 fp32 to bf16 in 34 us (4.4 TB/s), fp32 back to NCHW in 48 us (4.1 TB/s); in 24 and 32 us
+// with the same maps again, part of which then lies in the memory-side cache; one map of 13 x 13 x 512 in 3.8 us, which is the launch.
 #include "nhwc_common.h"
 
 #include <algorithm>

@@ -9,8 +9,9 @@
 //   mean = sum n_i mean_i / m,  M2 = sum M2_i + n_i (mean_i - mean)^2,
 // and one for the result, which reads x again (from the last-level cache where it fits its 256 MB).
 // Measured: 13 x 13 x 512 fp32 5.2 us, 16 x 27 x 27 x 384 bf16 10.2 us (launch and two sums across a workgroup), 64 x 55 x 55 x 256
-// fp32 105 us (3.8 TB/s) in one launch; 64 x 111 x 111 x 96 bf16 with SiLU 80 us in two (5.7 TB/s for what they move, 3.7 for x and
-// the result once; in one launch 126 us: one workgroup a compute unit, whose loads, arithmetic and stores follow each other).
+// fp32 105 us (3.8 TB/s) in one launch; 64 x 111 x 111 x 96 bf16 with SiLU 106 us in two (4.3 TB/s for what they move, 2.9 for x and
+// the result once; 81 with the same map again, part of which then lies in the memory-side cache, in one launch 126: one workgroup a
+// compute unit, whose loads, arithmetic and stores follow each other).
 #include "nhwc_common.h"
 
 #include <algorithm>
