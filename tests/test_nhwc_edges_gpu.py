@@ -196,3 +196,20 @@ def test_group_norm_of_means_whose_squares_overflow(sq, n, h, w, c, groups, far)
     got = sq.sq_nhwc_group_norm(x.cuda(), groups)
     assert not got.isnan().any()
     check(got, ref, bound + half_step(ref, F32), (n, h, w, c, groups, far))
+
+
+@pytest.mark.parametrize("n,h,w,c,groups", [(1, 13, 13, 512, 32), (4, 27, 27, 96, 8), (2, 80, 80, 64, 4), (1, 40, 40, 4096, 1), (1, 20, 20, 9999, 1),
+                                            (5, 53, 57, 150, 6), (2, 111, 111, 96, 8), (1, 130, 130, 320, 32), (300, 7, 7, 64, 64)])
+@pytest.mark.parametrize("mean", (0.5, 30.0))
+def test_group_norm_errs_by_few_roundings(sq, n, h, w, c, groups, mean):
+    """The mean error (root mean square) instead of the largest possible: a chain of at most 256 additions, each off by u of a
+    partial sum, independently, leaves 16 u of a sum, hence 16 u (1 + |mean| / spread) of a normalised value through the mean and
+    8 u through the variance; sqrt, quotient and product of the scale 4 u; difference, product and sum 3 u: 15 u + 16 u (1 + |mean|)
+    for a spread of one."""
+    x = (torch.randn((n, h, w, c), generator=gen(12)) + mean).cuda()
+    got = sq.sq_nhwc_group_norm(x, groups).double()
+    v = x.double().reshape(n, h * w, groups, c // groups)
+    var, mu = torch.var_mean(v, (1, 3), unbiased=False, keepdim=True)
+    ref = ((v - mu) / torch.sqrt(var + 1e-5)).reshape(n, h, w, c)
+    off = float(((got - ref).norm() / ref.norm()).cpu())
+    assert off <= (15 + 16 * (1 + mean)) * U, off / U
