@@ -74,7 +74,8 @@ typedef enum sq_status {
 
 typedef enum sq_dtype {
     SQ_F32 = 0,  /* IEEE binary32 inputs and kernels                               */
-    SQ_BF16 = 1  /* bfloat16 inputs and kernels, fp32 accumulate, fp32 bias/output */
+    SQ_BF16 = 1, /* bfloat16 inputs and kernels, fp32 accumulate, fp32 bias/output */
+    SQ_MXFP4 = 2 /* packed rows of 4-bit values: sq_mxfp4_linear_forward alone     */
 } sq_dtype;
 
 /* Algorithm selector of sq_conv2d_forward_ex.  Values >= SQ_ALGO_VARIANT0 pick
@@ -106,7 +107,7 @@ int sq_set_stream(void *hip_stream);
  *   sq_fire_forward, sq_fire_forward_packed, sq_squeezenet_forward: SQ_F32 only, otherwise
  *     SQ_ERR_UNSUPPORTED (reduced precision works on packed kernels and blocked maps:
  *     sq_blocked_fire_forward, sq_squeezenet_forward_packed).
- * Errors: SQ_ERR_UNSUPPORTED for a value that is not an sq_dtype. */
+ * Errors: SQ_ERR_UNSUPPORTED for any other value. */
 int sq_set_dtype(int dtype);
 
 /* Optional one-time set-up for the current device: raises the LDS limit of every kernel of the
@@ -576,6 +577,76 @@ size_t sq_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype,
 int sq_linear_forward(const void *in, const void *w, const float *b, const void *residual, void *out,
                       sq_dtype in_dtype, sq_dtype out_dtype, int rows, int Cin, int Cout, int act,
                       int ld_in, int ld_res, int ld_out, void *workspace, size_t workspace_bytes);
+
+/*
+ * Rows in microscaled 4-bit floating point: a matrix [rows][Cin] in blocks of 32 values of a row, each block with a
+ * power of two in common and its values in 4 bits (sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6).
+ * A block whose largest magnitude is m, 2^(e+2) <= m < 2^(e+3), has the power 2^e (at least 2^-127, also for zeros), and a value
+ * x becomes the element nearest to x / 2^e, halves to the one with the even mantissa, magnitudes above 6 to 6.  A block with an
+ * infinity or NaN is NaN as a whole.  The last block of a row may have fewer values.
+ *   packed buffer: sq_mxfp4_packed_bytes(rows, Cin) bytes, 256-byte aligned (else SQ_ERR_WORKSPACE).  With
+ *     Q = ceil(Cin / 256):
+ *       scales  [ceil(rows / 32)][Q][2][32][4] bytes: the power of block 2 s + h of values 256 c to 256 c + 255 of row r is byte
+ *               [r / 32][c][h][r % 32][s], e + 127 (255 = NaN)
+ *       values  [rows][128 Q] bytes, two values a byte, the earlier one in the lower half; zeros behind the Cin-th
+ *   sq_mxfp4_packed_bytes(): 0 for sizes <= 0 or past 64 bits.
+ *   sq_mxfp4_pack():   in: rows of ld_in values of in_dtype (SQ_F32 or SQ_BF16); writes the whole packed buffer.
+ *   sq_mxfp4_unpack(): out: rows of ld_out values of out_dtype.  Every value a block can stand for is exact in both types
+ *     (bfloat16: down to 2^-133; sq_mxfp4_pack makes none below 2^-128).
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP.
+ */
+size_t sq_mxfp4_packed_bytes(int rows, int Cin);
+int sq_mxfp4_pack(const void *in, sq_dtype in_dtype, void *packed, size_t packed_bytes, int rows, int Cin, int ld_in);
+int sq_mxfp4_unpack(const void *packed, size_t packed_bytes, void *out, sq_dtype out_dtype, int rows, int Cin, int ld_out);
+
+/*
+ * sq_linear_forward on such rows, on the 4-bit matrix instructions:
+ *   out[r][j] = act( b[j] + sum_k X[r][k] * W[j][k] ) + residual[r][j]
+ *   w: the kernels [Cout][Cin], packed ahead of time.  in: rows of ld_in values of in_dtype SQ_F32 or SQ_BF16, which the call
+ *     brings to 4 bits itself as sq_mxfp4_pack does, or SQ_MXFP4 = rows packed already (ld_in is then not looked at; for an input of
+ *     several products).  Both packed buffers 256-byte aligned (else SQ_ERR_WORKSPACE) and of their full size.
+ *   b, residual, out, act, ld_res, ld_out as in sq_linear_forward; out_dtype SQ_F32 or SQ_BF16 with any in_dtype.
+ *   Products and sums are fp32.  A block that is NaN makes the results of its row, or of its kernel, NaN and no others.
+ *   workspace: sq_mxfp4_linear_workspace_bytes(rows, Cin, Cout, in_dtype) bytes of device scratch, 256-byte aligned (else
+ *     SQ_ERR_WORKSPACE; 0 = none is needed, workspace may be NULL).  Contents on return are unspecified; two calls in flight at
+ *     once need two.
+ *   The same call gives the same bits every time, packed rows the same as rows that the call packs.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP.
+ */
+size_t sq_mxfp4_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype);
+int sq_mxfp4_linear_forward(const void *in, const void *packed_w, const float *b, const void *residual, void *out,
+                            sq_dtype in_dtype, sq_dtype out_dtype, int rows, int Cin, int Cout, int act, int ld_in,
+                            int ld_res, int ld_out, void *workspace, size_t workspace_bytes);
+
+/*
+ * Attention of the pixels of a channels-last map (queries) to an encoder's states, a sequence of another length:
+ *   out[n][i][h] = sum_j p[j] v[n][j][h'] / sum_j p[j],   p[j] = exp( scale * q[n][i][h] . k[n][j][h'] ),
+ * over the states j that query i sees, with [h] the D values of head h of a row and h' = h / (heads / kv_heads) the head of the
+ * states that it shares with its neighbours.  A query that sees no state gets zeros.
+ *   q, out: N*Lq rows of ld_q / ld_out values, heads*D of them the operator's; k, v: N*Lk rows of ld_k / ld_v values,
+ *     kv_heads*D the operator's (both may be slices of the rows of one projection).  All of dtype SQ_F32 or SQ_BF16.
+ *     out may be q itself with the same ld; apart from that it must not overlap any input.
+ *   heads a multiple of kv_heads (else SQ_ERR_SHAPE); D from 1 to 256 (more: SQ_ERR_UNSUPPORTED); Lk may be 0, with k and v
+ *     NULL or not, and every result is then zero.
+ *   scale: any number of at most 2^126 in magnitude (else SQ_ERR_SHAPE).
+ *   lengths [N] int32 or NULL: image n has only its first lengths[n] states (less than 0: none; more than Lk: all).
+ *   mask or NULL: bytes; state j is hidden from query i of image n where mask[n * mask_image + i * mask_row + j] is 0.
+ *     A step of 0 shares a mask between images or queries; steps must not be negative (SQ_ERR_SHAPE).
+ *   Scores, their maxima and sums are fp32, and so are the products for SQ_F32; for SQ_BF16 each p is rounded to bfloat16 before it
+ *   multiplies v.  Hidden states have no influence on a result, whatever they hold; states behind a length are not read.  An
+ *   infinity or NaN in a state that a query sees may make the results of that query and the heads that share the
+ *   state's head NaN, and no others.
+ *   workspace: sq_cross_attention_workspace_bytes() bytes of device scratch, 256-byte aligned (else SQ_ERR_WORKSPACE; 0 = none is
+ *     needed, workspace may be NULL).  Contents on return are unspecified; two calls in flight at once need two.
+ *   The same call gives the same bits every time.  Lk and Lq * heads / kv_heads may be 2^30 at most; what is more, or has no
+ *   room in one launch of 2^32 threads, returns SQ_ERR_UNSUPPORTED.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP.
+ */
+size_t sq_cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, sq_dtype dtype);
+int sq_cross_attention_forward(const void *q, const void *k, const void *v, void *out, sq_dtype dtype, int N, int Lq, int Lk,
+                               int heads, int kv_heads, int D, float scale, int ld_q, int ld_k, int ld_v, int ld_out,
+                               const int *lengths, const unsigned char *mask, long long mask_image, long long mask_row,
+                               void *workspace, size_t workspace_bytes);
 
 /*
  * Per-launch timing, off by default.  Between sq_profile_begin() and sq_profile_end()

@@ -7,7 +7,7 @@ supplies device memory and the current stream, nothing else.  There is no CPU
 fallback: if the library is missing the import fails.
 """
 from .binding import (  # noqa: F401
-    SQ_ALGO_AUTO, SQ_ALGO_DIRECT, SQ_ALGO_VARIANT0, SQ_BF16, SQ_F32, SQ_SQUEEZENET_MAX_BATCH, SQ_SQUEEZENET_BF16_MAX_BATCH,
+    SQ_ALGO_AUTO, SQ_ALGO_DIRECT, SQ_ALGO_VARIANT0, SQ_BF16, SQ_F32, SQ_MXFP4, SQ_SQUEEZENET_MAX_BATCH, SQ_SQUEEZENET_BF16_MAX_BATCH,
     SqError, lib,
     sq_avgpool_global, sq_conv2d_forward, sq_conv2d_forward_ex, sq_conv2d_forward_ws,
     sq_conv2d_workspace_bytes, sq_conv2d_strided_workspace_bytes, sq_conv2d_bf16_workspace_bytes, sq_conv_variant_count,
@@ -20,4 +20,6 @@ from .binding import (  # noqa: F401
     sq_squeezenet_bf16_pack_params, sq_squeezenet_bf16_workspace_bytes, sq_squeezenet_forward_bf16, sq_squeezenet_workspace_bytes, sq_strerror, TAP_NAMES, TAP_SHAPES,
     SQ_ACT_NONE, SQ_ACT_RELU, SQ_ACT_SILU, SQ_ACT_GELU, sq_nhwc_pack, sq_nhwc_unpack, sq_nhwc_group_norm,
     sq_nhwc_group_norm_workspace_bytes, sq_linear_forward, sq_linear_workspace_bytes,
+    sq_mxfp4_packed_bytes, sq_mxfp4_pack, sq_mxfp4_unpack, sq_mxfp4_linear_forward, sq_mxfp4_linear_workspace_bytes,
+    sq_cross_attention_forward, sq_cross_attention_workspace_bytes,
     sq_tune_conv2d_forward_poolcols, sq_tune_fire_forward_poolcols, sq_tune_poolrows_conv2d_forward)

@@ -17,7 +17,7 @@ if not os.path.exists(_LIB_PATH):
 
 lib = ctypes.CDLL(_LIB_PATH)
 
-SQ_F32, SQ_BF16 = 0, 1
+SQ_F32, SQ_BF16, SQ_MXFP4 = 0, 1, 2
 SQ_ALGO_AUTO, SQ_ALGO_DIRECT, SQ_ALGO_VARIANT0 = 0, 1, 2
 SQ_ACT_NONE, SQ_ACT_RELU, SQ_ACT_SILU, SQ_ACT_GELU = 0, 1, 2, 3
 SQ_SQUEEZENET_MAX_BATCH, SQ_SQUEEZENET_BF16_MAX_BATCH = 453, 907   # as in include/sq.h
@@ -98,6 +98,16 @@ lib.sq_nhwc_group_norm.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 5 + [ctypes.
 lib.sq_linear_workspace_bytes.restype = _sz
 lib.sq_linear_workspace_bytes.argtypes = [_i] * 6
 lib.sq_linear_forward.argtypes = [_vp] * 5 + [_i] * 9 + [_vp, _sz]
+lib.sq_mxfp4_packed_bytes.restype = _sz
+lib.sq_mxfp4_packed_bytes.argtypes = [_i] * 2
+lib.sq_mxfp4_pack.argtypes = [_vp, _i, _vp, _sz] + [_i] * 3
+lib.sq_mxfp4_unpack.argtypes = [_vp, _sz, _vp] + [_i] * 4
+lib.sq_mxfp4_linear_workspace_bytes.restype = _sz
+lib.sq_mxfp4_linear_workspace_bytes.argtypes = [_i] * 4
+lib.sq_mxfp4_linear_forward.argtypes = [_vp] * 5 + [_i] * 9 + [_vp, _sz]
+lib.sq_cross_attention_workspace_bytes.restype = _sz
+lib.sq_cross_attention_workspace_bytes.argtypes = [_i] * 7
+lib.sq_cross_attention_forward.argtypes = [_vp] * 4 + [_i] * 7 + [ctypes.c_float] + [_i] * 4 + [_vp, _vp, ctypes.c_longlong, ctypes.c_longlong, _vp, _sz]
 
 lib.sq_profile_begin.argtypes = [_i]
 lib.sq_profile_get_mfma_flops.argtypes = [_i, ctypes.POINTER(ctypes.c_double)]
@@ -920,6 +930,177 @@ def sq_linear_forward(x, w, b=None, act=SQ_ACT_NONE, residual=None, out=None, ou
     _run(index, "sq_linear_forward", lib.sq_linear_forward, x_at, w_at,
          _dense(b, "b", index, torch.float32), res, out.data_ptr(), code, _dtype_code(out, "out"), rows, Cin, Cout,
          _int(act, -3, "sq_linear_forward"), ld_in, ld_res, ld_out, address, nbytes)
+    return out
+
+
+@functools.lru_cache(maxsize=4096)      # a function of the sizes alone
+def sq_mxfp4_packed_bytes(rows, Cin) -> int:
+    """Bytes of a matrix [rows][Cin] in microscaled 4-bit floating point."""
+    if max(rows, Cin) > _MAX_INT or min(rows, Cin) <= 0:
+        return 0
+    return int(lib.sq_mxfp4_packed_bytes(rows, Cin))
+
+
+def _packed(t, name, index, rows, Cin):
+    """Address and size of the packed rows in a uint8 tensor."""
+    need = sq_mxfp4_packed_bytes(rows, Cin)
+    address = _dense(t, name, index, torch.uint8)
+    if not need or t.numel() != need:
+        raise ValueError(f"{name} must have the sq_mxfp4_packed_bytes() of {rows} rows of {Cin} values")
+    return address, need
+
+
+def _matrix(x, name):
+    """GPU, rows, values of a row and values from one to the next."""
+    index = _gpu_of(x, name)
+    ld, Cin = _rows_of(x, name, index), x.shape[-1]
+    rows = x.numel() // Cin if Cin else 0
+    if rows > _MAX_INT:
+        _check(-3, name)
+    return index, rows, Cin, ld
+
+
+def sq_mxfp4_pack(x, out=None):
+    """Rows x [..., Cin] (float32 or bfloat16) -> packed uint8 tensor of sq_mxfp4_packed_bytes(rows, Cin) bytes: blocks of 32 values
+    with a power of two in common and 4 bits a value.  Kernels [Cout][Cin][1][1] are taken as [Cout][Cin]."""
+    if x.dim() == 4 and x.shape[2:] == (1, 1):
+        x = x[:, :, 0, 0]
+    index, rows, Cin, ld = _matrix(x, "x")
+    if not rows:
+        _check(-2, "sq_mxfp4_pack")
+    if out is None:
+        out = x.new_empty(sq_mxfp4_packed_bytes(rows, Cin), dtype=torch.uint8)
+    address, nbytes = _packed(out, "out", index, rows, Cin)
+    _run(index, "sq_mxfp4_pack", lib.sq_mxfp4_pack, x.data_ptr(), _dtype_code(x, "x"), address, nbytes, rows, Cin, ld)
+    return out
+
+
+def sq_mxfp4_unpack(packed, rows, Cin, dtype=torch.float32, out=None):
+    """Packed rows -> the values they stand for, [rows][Cin] of `dtype` or of out, whose last dimension is Cin and others count rows."""
+    index = _gpu_of(packed, "packed")
+    address, nbytes = _packed(packed, "packed", index, rows, Cin)
+    if out is None:
+        out, ld = packed.new_empty((rows, Cin), dtype=dtype), Cin
+    else:
+        ld = _rows_of(out, "out", index)
+        if out.shape[-1] != Cin or out.numel() != rows * Cin:
+            raise ValueError("out has the wrong shape")
+    _run(index, "sq_mxfp4_unpack", lib.sq_mxfp4_unpack, address, nbytes, out.data_ptr(), _dtype_code(out, "out"), rows, Cin, ld)
+    return out
+
+
+@functools.lru_cache(maxsize=4096)      # a function of the sizes alone
+def _mxfp4_linear_need(rows, Cin, Cout, code):
+    if max(rows, Cin, Cout) > _MAX_INT or min(rows, Cin, Cout) <= 0:
+        return 0
+    return int(lib.sq_mxfp4_linear_workspace_bytes(rows, Cin, Cout, code))
+
+
+def sq_mxfp4_linear_workspace_bytes(rows, Cin, Cout, dtype=torch.float32) -> int:
+    """Bytes for rows of `dtype`: float32, bfloat16, or uint8 for packed rows."""
+    if dtype not in _CODES and dtype != torch.uint8:
+        raise ValueError("dtype must be float32, bfloat16 or uint8")
+    return _mxfp4_linear_need(rows, Cin, Cout, SQ_MXFP4 if dtype == torch.uint8 else _CODES[dtype])
+
+
+def sq_mxfp4_linear_forward(x, packed_w, Cout, b=None, act=SQ_ACT_NONE, residual=None, out=None, out_dtype=None, rows=None, Cin=None,
+                            workspace=None):
+    """act(x @ w.T + b) + residual with x and w in microscaled 4-bit floating point.  x [..., Cin] float32 or bfloat16, brought to 4 bits
+    by the call, or a uint8 tensor of `rows` packed rows of `Cin` values; packed_w: sq_mxfp4_pack of the kernels [Cout][Cin]; b [Cout]
+    float32 or None; out and residual [..., Cout] ([rows][Cout] for packed x) of out_dtype (default: that of x, bfloat16 for packed x,
+    or that of residual or out).  `residual` may be `out` itself.  `workspace`: sq_mxfp4_linear_workspace_bytes() bytes on the same
+    GPU, which no other call may use at the time; without it the call takes what it needs from torch."""
+    Cout = _int(Cout, -2, "sq_mxfp4_linear_forward")
+    if x.dtype == torch.uint8:
+        if rows is None or Cin is None:
+            raise ValueError("packed rows need rows and Cin")
+        index, rows, Cin = _gpu_of(x, "x"), _int(rows, -2, "sq_mxfp4_linear_forward"), _int(Cin, -2, "sq_mxfp4_linear_forward")
+        x_at, ld_in, code, shape, kind = _packed(x, "x", index, rows, Cin)[0], 0, SQ_MXFP4, (rows, Cout), torch.bfloat16
+    else:
+        if rows is not None or Cin is not None:
+            raise ValueError("rows and Cin belong to packed rows")
+        index, rows, Cin, ld_in = _matrix(x, "x")
+        x_at, code, shape, kind = x.data_ptr(), _dtype_code(x, "x"), (*x.shape[:-1], Cout), x.dtype
+    if not rows or Cout <= 0:
+        _check(-2, "sq_mxfp4_linear_forward")
+    w_at = _packed(packed_w, "packed_w", index, Cout, Cin)[0]
+    if out is None:
+        out, ld_out = x.new_empty(shape, dtype=out_dtype or (kind if residual is None else residual.dtype)), Cout
+    else:
+        if out.shape != shape or out_dtype not in (None, out.dtype):
+            raise ValueError("out has the wrong shape or type")
+        ld_out = _rows_of(out, "out", index)
+    ld_res, res = 0, None
+    if residual is not None:
+        if residual.shape != shape or residual.dtype != out.dtype:
+            raise ValueError("residual must have the shape and type of the result")
+        ld_res, res = _rows_of(residual, "residual", index), residual.data_ptr()
+    if b is not None and b.numel() != Cout:
+        raise ValueError("b must have one value per output layer")
+    workspace, address, nbytes = _scratch(workspace, _mxfp4_linear_need(rows, Cin, Cout, code), x, index)
+    _run(index, "sq_mxfp4_linear_forward", lib.sq_mxfp4_linear_forward, x_at, w_at, _dense(b, "b", index, torch.float32), res, out.data_ptr(),
+         code, _dtype_code(out, "out"), rows, Cin, Cout, _int(act, -3, "sq_mxfp4_linear_forward"), ld_in, ld_res, ld_out, address, nbytes)
+    return out
+
+
+@functools.lru_cache(maxsize=4096)      # a function of the sizes alone
+def _cross_need(N, Lq, Lk, heads, kv_heads, D, code):
+    if max(N, Lq, Lk, heads, kv_heads, D) > _MAX_INT or min(N, Lq, Lk, heads, kv_heads, D) <= 0:
+        return 0
+    return int(lib.sq_cross_attention_workspace_bytes(N, Lq, Lk, heads, kv_heads, D, code))
+
+
+def sq_cross_attention_workspace_bytes(N, Lq, Lk, heads, kv_heads, D, dtype=torch.float32) -> int:
+    if dtype not in _CODES:
+        raise ValueError("dtype must be float32 or bfloat16")
+    return _cross_need(N, Lq, Lk, heads, kv_heads, D, _CODES[dtype])
+
+
+def sq_cross_attention_forward(q, k, v, heads, kv_heads=None, scale=None, lengths=None, mask=None, out=None, workspace=None):
+    """Attention of the rows of a map to an encoder's states.  q [N, ..., heads * D] (a channels-last map, or [N][Lq][heads * D]), k and v
+    [N, ..., kv_heads * D], float32 or all bfloat16; kv_heads divides heads (default: heads).  `scale` of the scores (default
+    1 / sqrt(D)).  `lengths` [N] int32: how many states each image has.  `mask`, bool or uint8: which states are seen, [N][Lk] for all
+    queries of an image or [N][Lq][Lk]; expanded dimensions stay as they are.  A query that sees no state gets zeros.  `out` may be q
+    itself.  `workspace`: sq_cross_attention_workspace_bytes() bytes on the same GPU, which no other call may use at the time; without it
+    the call takes what it needs from torch."""
+    what = "sq_cross_attention_forward"
+    heads = _int(heads, -2, what)
+    kv_heads = heads if kv_heads is None else _int(kv_heads, -2, what)
+    index = _gpu_of(q, "q")
+    N, C = q.shape[0], q.shape[-1]
+    if k.shape[0] != N or k.shape != v.shape or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("k and v must be alike, with the images and the type of q")
+    if heads <= 0 or kv_heads <= 0 or heads % kv_heads:
+        _check(-2, what)
+    D = C // heads
+    if D * heads != C or k.shape[-1] != D * kv_heads:
+        raise ValueError("q must have heads * D values a row, k and v kv_heads * D")
+    ld_q, ld_k, ld_v = _rows_of(q, "q", index), _rows_of(k, "k", index), _rows_of(v, "v", index)
+    if not N or not C or not q.numel():
+        _check(-2, what)
+    Lq, Lk = q.numel() // (N * C), k.numel() // (N * D * kv_heads)
+    if Lq > _MAX_INT or Lk > _MAX_INT:
+        _check(-3, what)
+    if out is None:
+        out, ld_out = torch.empty_like(q, memory_format=torch.contiguous_format), C
+    else:
+        if out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out has the wrong shape or type")
+        ld_out = _rows_of(out, "out", index)
+    if lengths is not None and lengths.numel() != N:
+        raise ValueError("lengths must have one value per image")
+    mask_at, mask_image, mask_row = None, 0, 0
+    if mask is not None:
+        if mask.get_device() != index or mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError(f"mask must be bool or uint8 and live on GPU {index}")
+        if mask.shape != (N, Lk) and mask.shape != (N, Lq, Lk) or Lk > 1 and mask.stride(-1) != 1:
+            raise ValueError("mask must be [N][Lk] or [N][Lq][Lk] with a dense last dimension")
+        mask_at, mask_image, mask_row = mask.data_ptr(), mask.stride(0), mask.stride(1) if mask.dim() == 3 else 0
+    code = _dtype_code(q, "q")
+    workspace, address, nbytes = _scratch(workspace, _cross_need(N, Lq, Lk, heads, kv_heads, D, code), q, index)
+    _run(index, what, lib.sq_cross_attention_forward, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), code, N, Lq, Lk, heads, kv_heads, D,
+         D ** -0.5 if scale is None else scale, ld_q, ld_k, ld_v, ld_out, _dense(lengths, "lengths", index, torch.int32), mask_at, mask_image, mask_row,
+         address, nbytes)
     return out
 
 

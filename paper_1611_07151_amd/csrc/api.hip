@@ -2,6 +2,8 @@
 // fire-layer and whole-network drivers that sequence the kernels.
 #include "sq_internal.h"
 
+#include <cmath>
+
 #include <stdio.h>
 #include <string.h>
 
@@ -304,7 +306,7 @@ int sq_init(void)
     const int rs = static_scratch(&unused);
     if (rs) return rs;
     const bool ok = conv_mfma_register_kernels() & blocked_register_kernels() & split_register_kernels() & stem_register_kernels() & fire_bf16_register_kernels() &
-                    nhwc_layout_register_kernels() & nhwc_norm_register_kernels() & linear_register_kernels();
+                    nhwc_layout_register_kernels() & nhwc_norm_register_kernels() & linear_register_kernels() & mxfp4_register_kernels() & cross_attention_register_kernels();
     if (!ok) {
         const int rc = check_launch();
         return rc ? rc : SQ_ERR_HIP;
@@ -1423,6 +1425,87 @@ int sq_linear_forward(const void *in, const void *w, const float *b, const void 
     a.ld_in = ld_in; a.ld_res = ld_res; a.ld_out = ld_out;
     a.workspace = workspace;
     return linear(a);
+}
+
+size_t sq_mxfp4_packed_bytes(int rows, int Cin)
+{
+    if (rows <= 0 || Cin <= 0) return 0;
+    return mxfp4_packed_bytes(rows, Cin);
+}
+
+int sq_mxfp4_pack(const void *in, sq_dtype in_dtype, void *packed, size_t packed_bytes, int rows, int Cin, int ld_in)
+{
+    if (!in || !packed) return SQ_ERR_NULL;
+    if (rows <= 0 || Cin <= 0 || ld_in < Cin) return SQ_ERR_SHAPE;
+    if (!known_dtype(in_dtype) || !aligned_to(in, in_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (((uintptr_t)packed & 255) || packed_bytes < mxfp4_packed_bytes(rows, Cin)) return SQ_ERR_WORKSPACE;
+    return mxfp4_pack(in, in_dtype, packed, rows, Cin, ld_in);
+}
+
+int sq_mxfp4_unpack(const void *packed, size_t packed_bytes, void *out, sq_dtype out_dtype, int rows, int Cin, int ld_out)
+{
+    if (!packed || !out) return SQ_ERR_NULL;
+    if (rows <= 0 || Cin <= 0 || ld_out < Cin) return SQ_ERR_SHAPE;
+    if (!known_dtype(out_dtype) || !aligned_to(out, out_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (((uintptr_t)packed & 255) || packed_bytes < mxfp4_packed_bytes(rows, Cin)) return SQ_ERR_WORKSPACE;
+    return mxfp4_unpack(packed, out, out_dtype, rows, Cin, ld_out);
+}
+
+size_t sq_mxfp4_linear_workspace_bytes(int rows, int Cin, int Cout, sq_dtype in_dtype)
+{
+    if (rows <= 0 || Cin <= 0 || Cout <= 0 || !(known_dtype(in_dtype) || in_dtype == SQ_MXFP4)) return 0;
+    return mxfp4_linear_workspace_bytes(rows, Cin, Cout, in_dtype);
+}
+
+int sq_mxfp4_linear_forward(const void *in, const void *packed_w, const float *b, const void *residual, void *out, sq_dtype in_dtype,
+                            sq_dtype out_dtype, int rows, int Cin, int Cout, int act, int ld_in, int ld_res, int ld_out, void *workspace,
+                            size_t workspace_bytes)
+{
+    if (!in || !packed_w || !out) return SQ_ERR_NULL;
+    const bool packed = in_dtype == SQ_MXFP4;
+    if (rows <= 0 || Cin <= 0 || Cout <= 0 || (!packed && ld_in < Cin) || ld_out < Cout || (residual && ld_res < Cout)) return SQ_ERR_SHAPE;
+    if (!(packed || known_dtype(in_dtype)) || !known_dtype(out_dtype) || !known_act(act)) return SQ_ERR_UNSUPPORTED;
+    if ((!packed && !aligned_to(in, in_dtype)) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype) || !aligned_to(b, SQ_F32))
+        return SQ_ERR_UNSUPPORTED;
+    if (((uintptr_t)packed_w & 255) || (packed && ((uintptr_t)in & 255))) return SQ_ERR_WORKSPACE;
+    const size_t need = mxfp4_linear_workspace_bytes(rows, Cin, Cout, in_dtype);
+    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+    LinearArgs a{};
+    a.in = in; a.w = packed_w; a.b = b; a.residual = residual; a.out = out;
+    a.in_dtype = in_dtype; a.out_dtype = out_dtype;
+    a.rows = rows; a.Cin = Cin; a.Cout = Cout; a.act = act;
+    a.ld_in = ld_in; a.ld_res = ld_res; a.ld_out = ld_out;
+    a.workspace = workspace;
+    return mxfp4_linear(a);
+}
+
+size_t sq_cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, sq_dtype dtype)
+{
+    if (N <= 0 || Lq <= 0 || Lk <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || D <= 0 || D > 256 || !known_dtype(dtype)) return 0;
+    return cross_attention_workspace_bytes(N, Lq, Lk, heads, kv_heads, D, dtype);
+}
+
+int sq_cross_attention_forward(const void *q, const void *k, const void *v, void *out, sq_dtype dtype, int N, int Lq, int Lk, int heads,
+                               int kv_heads, int D, float scale, int ld_q, int ld_k, int ld_v, int ld_out, const int *lengths,
+                               const unsigned char *mask, long long mask_image, long long mask_row, void *workspace, size_t workspace_bytes)
+{
+    if (!q || !out || (Lk > 0 && (!k || !v))) return SQ_ERR_NULL;
+    if (N <= 0 || Lq <= 0 || Lk < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || D <= 0 || !(std::fabs(scale) <= 8.5070592e37f)) return SQ_ERR_SHAPE;
+    const long long wide = (long long)heads * D, wide_kv = (long long)kv_heads * D;
+    if (ld_q < wide || ld_out < wide || (Lk > 0 && (ld_k < wide_kv || ld_v < wide_kv))) return SQ_ERR_SHAPE;
+    if (mask && (mask_image < 0 || mask_row < 0)) return SQ_ERR_SHAPE;
+    if (!known_dtype(dtype) || D > 256) return SQ_ERR_UNSUPPORTED;
+    if (!aligned_to(q, dtype) || !aligned_to(out, dtype) || (Lk > 0 && (!aligned_to(k, dtype) || !aligned_to(v, dtype))) || ((uintptr_t)lengths & 3))
+        return SQ_ERR_UNSUPPORTED;
+    const size_t need = sq_cross_attention_workspace_bytes(N, Lq, Lk, heads, kv_heads, D, dtype);
+    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+    CrossArgs a{};
+    a.q = q; a.k = k; a.v = v; a.out = out;
+    a.dtype = dtype; a.N = N; a.Lq = Lq; a.Lk = Lk; a.heads = heads; a.kv_heads = kv_heads; a.D = D; a.scale = scale;
+    a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out;
+    a.lengths = lengths; a.mask = mask; a.mask_image = mask_image; a.mask_row = mask_row;
+    a.workspace = workspace;
+    return cross_attention(a);
 }
 
 }  // extern "C"

@@ -236,10 +236,42 @@ inline double linear_bytes(const LinearArgs &a)
     return si * ((double)a.rows * a.Cin + (double)a.Cout * a.Cin) + so * (double)a.rows * a.Cout * (a.residual ? 2 : 1) + 4.0 * a.Cout;
 }
 int linear(const LinearArgs &a);
+// Adds up the shares' sums, a.shares of them in `in` as rows of ld_in = linear_share_row(Cout) values of fp32 each, and finishes them.
+int linear_join(const LinearArgs &a);
+inline long long linear_share_row(int Cout) { return ((long long)Cout + 31) / 32 * 32; }    // rows begin at whole lines
+constexpr int kLinearMostShares = 16;
+// Rows in microscaled 4-bit floating point (mxfp4.hip), after validation.  mxfp4_linear: in_dtype SQ_F32, SQ_BF16 (workspace holds the packed
+// rows) or SQ_MXFP4; w packed.
+size_t mxfp4_packed_bytes(int rows, int Cin);
+int mxfp4_pack(const void *in, int in_dtype, void *out, int rows, int Cin, long long ld);
+int mxfp4_unpack(const void *in, void *out, int out_dtype, int rows, int Cin, long long ld);
+size_t mxfp4_linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype);
+int mxfp4_linear(const LinearArgs &a);
+// Attention to an encoder's states (cross_attention.hip), after validation.
+struct CrossArgs {
+    const void *q, *k, *v;
+    void *out;
+    int dtype, N, Lq, Lk, heads, kv_heads, D;
+    float scale;
+    long long ld_q, ld_k, ld_v, ld_out;
+    const int *lengths;
+    const unsigned char *mask;
+    long long mask_image, mask_row;
+    void *workspace;
+};
+size_t cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype);
+inline double cross_flops(const CrossArgs &a) { return 4.0 * a.N * a.heads * a.Lq * (double)a.Lk * a.D; }
+inline double cross_bytes(const CrossArgs &a)
+{
+    return (a.dtype == SQ_F32 ? 4.0 : 2.0) * 2.0 * a.N * a.D * ((double)a.Lq * a.heads + (double)a.Lk * a.kv_heads);
+}
+int cross_attention(const CrossArgs &a);
 // Loads the code of these kernels onto the current device (sq_init).
 bool nhwc_layout_register_kernels();
 bool nhwc_norm_register_kernels();
 bool linear_register_kernels();
+bool mxfp4_register_kernels();
+bool cross_attention_register_kernels();
 
 // Optional per-launch timing (sq_profile_begin/end).  A LaunchScope brackets one kernel
 // launch with a pair of HIP events on the library's stream when profiling is on and

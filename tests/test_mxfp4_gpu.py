@@ -1,0 +1,296 @@
+"""Rows in microscaled 4-bit floating point and their product against their definitions in 64 bits.
+
+Packing is exact arithmetic with one rounding whose ties are defined, so its values are compared bit by bit.  The product: terms of two
+4-bit elements and powers of two are exact in fp32, and the matrix unit's additions are off by at most a whole unit of the last place (2u,
+u = 2^-24), so (Cin + 16) * 2u * (sum |x||w| + |b|); activation (slope at most 1.13, its own value good to 8u), residual, and half a step
+of the result's type.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24
+ELEMENTS = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
+
+
+@pytest.fixture(scope="module")
+def sq():
+    import paper_1611_07151_amd as m
+    m.sq_init()
+    return m
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def blocks64(x):
+    """Scale exponents [rows][blocks] and element codes [rows][blocks][32] of float64 rows, by the definition, on the CPU."""
+    rows, cin = x.shape
+    nb = (cin + 31) // 32
+    v = torch.zeros(rows, nb * 32, dtype=torch.float64)
+    v[:, :cin] = x
+    v = v.reshape(rows, nb, 32)
+    most = v.abs().amax(2)
+    e = torch.frexp(most)[1].long() - 3
+    e = torch.where(most == 0, torch.full_like(e, -127), e).clamp(min=-127)
+    ratio = v.abs() / torch.pow(torch.tensor(2.0, dtype=torch.float64), e.double())[..., None]
+    # the nearest element, the lower one first, then the upper one where it is nearer or as near and even
+    low = (torch.searchsorted(ELEMENTS, ratio.contiguous(), right=True) - 1).clamp(max=6)
+    below, above = ratio - ELEMENTS[low], ELEMENTS[low + 1] - ratio
+    code = torch.where((above < below) | ((above == below) & (low % 2 == 1)), low + 1, low)
+    return e, code, v < 0
+
+
+def values64(x):
+    rows, cin = x.shape
+    x = x.double()
+    odd = ~x.isfinite()
+    e, code, neg = blocks64(torch.where(odd, torch.zeros_like(x), x))
+    v = ELEMENTS[code] * torch.pow(torch.tensor(2.0, dtype=torch.float64), e.double())[..., None]
+    v = torch.where(neg, -v, v).reshape(rows, -1)[:, :cin].clone()
+    for r, k in odd.nonzero().tolist():
+        v[r, k // 32 * 32:k // 32 * 32 + 32] = math.nan
+    return v
+
+
+def same(got, want):
+    got = got.cpu().double()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got[~want.isnan()], want[~want.isnan()])
+
+
+def spread(rows, cin, seed):
+    """Blocks of different magnitude, some of zeros."""
+    g = gen(seed)
+    x = torch.randn((rows, cin), generator=g) * torch.exp2(torch.randint(-6, 7, (rows, (cin + 31) // 32), generator=g).float()).repeat_interleave(32, 1)[:, :cin]
+    x[torch.rand((rows, cin), generator=g) < 0.05] = 0
+    return x
+
+
+@pytest.mark.parametrize("dt", (F32, BF16))
+@pytest.mark.parametrize("rows,cin", [(1, 1), (1, 31), (1, 32), (2, 33), (3, 255), (31, 256), (32, 257), (33, 512), (65, 99), (7, 1000), (100, 4096), (2187, 99)])
+def test_pack_and_unpack(sq, dt, rows, cin):
+    print(dt, rows, cin, flush=True)
+    x = spread(rows, cin, rows + cin).to(dt)
+    p = sq.sq_mxfp4_pack(x.cuda())
+    assert p.dtype == torch.uint8 and p.numel() == sq.sq_mxfp4_packed_bytes(rows, cin)
+    want = values64(x)
+    same(sq.sq_mxfp4_unpack(p, rows, cin), want)
+    same(sq.sq_mxfp4_unpack(p, rows, cin, dtype=BF16), want)
+
+
+def test_layout_is_as_documented(sq):
+    rows, cin = 37, 600
+    x = spread(rows, cin, 5)
+    p = sq.sq_mxfp4_pack(x.cuda()).cpu()
+    q = 3
+    e, code, neg = blocks64(x.double())
+    scales = p[:2 * q * 256].reshape(2, q, 2, 32, 4).long()
+    values = p[2 * q * 256:].reshape(rows, 128 * q).long()
+    for r in range(rows):
+        for b in range(8 * q):
+            have = int(scales[r // 32, b // 8, b % 2, r % 32, b % 8 // 2])
+            assert have == (int(e[r, b]) + 127 if b < e.shape[1] else 0), (r, b)
+    nibbles = torch.stack((values & 15, values >> 4), 2).reshape(rows, -1)
+    want = torch.zeros_like(nibbles)
+    flat = code.reshape(rows, -1)
+    want[:, :flat.shape[1]] = flat
+    assert torch.equal(nibbles & 7, want)
+    nonzero = want != 0
+    sign = torch.zeros_like(nonzero)
+    sign[:, :flat.shape[1]] = neg.reshape(rows, -1)
+    assert torch.equal((nibbles >> 3 == 1)[nonzero], sign[nonzero])
+
+
+@pytest.mark.parametrize("dt", (F32, BF16))
+def test_borders_and_the_ends_of_the_format(sq, dt):
+    """Every border between elements, the values next to it, in blocks of every power of two that the type has."""
+    grid = torch.arange(0, 8, 0.25, dtype=torch.float64)
+    near = torch.cat((grid, grid * (1 + 2.0 ** -7), grid * (1 - 2.0 ** -8)))[:93]
+    rows = []
+    for power in range(-149, 126):
+        for part in near.split(31):
+            # the block's largest value sets its power: just below 8, so that it goes to 6
+            rows.append(torch.cat((torch.tensor([7.75]), part.clamp(max=7.75))) * 2.0 ** power)
+    x = torch.stack(rows)
+    x[::2] *= -1
+    x = x.float().to(dt)       # what falls below the type's numbers is rounded here, outside the call
+    same(sq.sq_mxfp4_unpack(sq.sq_mxfp4_pack(x.cuda()), *x.shape), values64(x))
+
+
+def test_infinities_and_nan_make_their_block_nan(sq):
+    x = spread(40, 200, 9)
+    x[3, 40], x[3, 70], x[17, 199], x[39, 0] = math.inf, math.nan, -math.inf, math.nan
+    for dt in (F32, BF16):
+        same(sq.sq_mxfp4_unpack(sq.sq_mxfp4_pack(x.to(dt).cuda()), *x.shape), values64(x.to(dt)))
+
+
+def test_slices_and_the_rest_of_the_rows(sq):
+    rows, cin = 33, 70
+    for dt in (F32, BF16):
+        x = spread(rows, cin, 3).to(dt)
+        for left, right in ((0, 5), (3, 0), (8, 8), (1, 1)):
+            wide = torch.full((rows, left + cin + right), math.nan, dtype=dt, device="cuda")
+            wide[:, left:left + cin] = x.cuda()
+            p = sq.sq_mxfp4_pack(wide[:, left:left + cin])
+            assert torch.equal(p, sq.sq_mxfp4_pack(x.cuda()))
+            out = torch.full((rows, left + cin + right), math.nan, dtype=dt, device="cuda")
+            sq.sq_mxfp4_unpack(p, rows, cin, out=out[:, left:left + cin])
+            same(out[:, left:left + cin], values64(x))
+            assert out[:, :left].isnan().all() and out[:, left + cin:].isnan().all()
+
+
+def test_rows_past_32_bits(sq):
+    """Rows whose offsets pass 2^32 bytes."""
+    rows, ld, cin = 70, 2 ** 25 + 8, 300
+    wide = torch.empty((rows, ld), dtype=BF16, device="cuda")
+    x = spread(rows, cin, 11).to(BF16)
+    wide[:, -cin:] = x.cuda()
+    same(sq.sq_mxfp4_unpack(sq.sq_mxfp4_pack(wide[:, -cin:]), rows, cin), values64(x))
+
+
+def act64(y, act):
+    if act == 1:
+        return torch.where(y < 0, torch.zeros_like(y), y)
+    if act == 2:
+        return y / (1 + torch.exp(-y))
+    if act == 3:
+        return 0.5 * y * torch.special.erfc(-y / math.sqrt(2))
+    return y
+
+
+def product(x, w, b, act, res, dt):
+    """Result in 64 bits and its bound."""
+    X, W = values64(x), values64(w)
+    y = X @ W.t()
+    size = X.abs() @ W.abs().t()
+    if b is not None:
+        y, size = y + b.double(), size + b.double().abs()
+    bound = (x.shape[1] + 16) * 2 * U * size
+    a = act64(y, act)
+    if act:
+        bound = 1.13 * bound + 8 * U * y.abs()
+    if res is not None:
+        a = a + res.double()
+        bound = bound + U * a.abs()
+    eps = torch.finfo(dt)
+    return a, bound * (1 + eps.eps) + eps.eps / 2 * a.abs() * (1 + 1e-6) + eps.smallest_normal
+
+
+def check(got, ref, bound, what):
+    got = got.cpu().double()
+    assert torch.equal(got.isnan(), ref.isnan()), what
+    err = torch.where(ref.isnan(), torch.zeros_like(ref), (got - ref).abs())
+    bad = ~(err <= torch.where(ref.isnan(), torch.ones_like(ref), bound))
+    assert not bad.any(), (what, int(bad.sum()), float(err.max()), float((err / bound).nan_to_num(0).max()))
+
+
+SIZES = [(1, 1, 1), (1, 32, 16), (1, 512, 1000), (2, 33, 17), (5, 256, 64), (8, 4096, 300), (15, 99, 333), (16, 2048, 96), (17, 700, 65), (31, 257, 31),
+         (32, 1024, 512), (63, 63, 63), (64, 64, 64), (65, 1000, 129), (100, 8200, 40), (128, 4096, 256), (129, 320, 127), (200, 96, 777), (255, 512, 257),
+         (300, 2049, 300), (515, 768, 515), (729, 1536, 384), (1000, 40, 1024), (1100, 512, 1300)]
+
+
+@pytest.mark.parametrize("rows,cin,cout", SIZES)
+@pytest.mark.parametrize("dt,odt", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+def test_product(sq, rows, cin, cout, dt, odt):
+    print(rows, cin, cout, dt, odt, flush=True)
+    seed = rows * 7 + cin + cout
+    act = seed % 4
+    x, w = spread(rows, cin, seed).to(dt), (torch.randn((cout, cin), generator=gen(seed + 1)) * math.sqrt(2 / cin)).to(dt)
+    b = torch.randn(cout, generator=gen(seed + 2)) if seed % 3 else None
+    res = torch.randn((rows, cout), generator=gen(seed + 3)).to(odt) if seed % 2 else None
+    ref, bound = product(x, w, b, act, res, odt)
+    pw = sq.sq_mxfp4_pack(w.cuda())
+    kw = dict(b=None if b is None else b.cuda(), act=act, residual=None if res is None else res.cuda(), out_dtype=odt)
+    got = sq.sq_mxfp4_linear_forward(x.cuda(), pw, cout, **kw)
+    assert got.shape == (rows, cout) and got.dtype == odt
+    check(got, ref, bound, (rows, cin, cout, act))
+    # the same bits every time, and from rows packed before
+    assert torch.equal(got, sq.sq_mxfp4_linear_forward(x.cuda(), pw, cout, **kw))
+    packed = sq.sq_mxfp4_linear_forward(sq.sq_mxfp4_pack(x.cuda()), pw, cout, rows=rows, Cin=cin, **kw)
+    assert torch.equal(got, packed)
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(3, 300, 50), (20, 64, 40), (200, 600, 200), (600, 512, 600)])
+def test_product_of_slices_in_place(sq, rows, cin, cout):
+    """Input, residual and result as slices of wider rows, the result over the residual; the rest of the rows stays."""
+    dt = BF16
+    x, w, res = spread(rows, cin, 1).to(dt), torch.randn((cout, cin), generator=gen(2)).to(dt), torch.randn((rows, cout), generator=gen(3)).to(dt)
+    ref, bound = product(x, w, None, 0, res, dt)
+    wide = torch.full((rows, cin + 12), math.nan, dtype=dt, device="cuda")
+    wide[:, 5:5 + cin] = x.cuda()
+    out = torch.full((rows, cout + 9), math.nan, dtype=dt, device="cuda")
+    out[:, 3:3 + cout] = res.cuda()
+    view = out[:, 3:3 + cout]
+    sq.sq_mxfp4_linear_forward(wide[:, 5:5 + cin], sq.sq_mxfp4_pack(w.cuda()), cout, residual=view, out=view)
+    check(view, ref, bound, (rows, cin, cout))
+    assert out[:, :3].isnan().all() and out[:, 3 + cout:].isnan().all()
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(2, 96, 33), (40, 512, 48), (300, 700, 300), (600, 512, 600)])
+def test_nan_blocks_reach_their_row_and_kernel_alone(sq, rows, cin, cout):
+    x, w = spread(rows, cin, 4), torch.randn((cout, cin), generator=gen(5))
+    x[rows // 2, cin - 1], w[cout // 3, 0] = math.nan, math.inf
+    ref, bound = product(x, w, None, 0, None, F32)
+    assert int(ref.isnan().sum()) == rows + cout - 1
+    check(sq.sq_mxfp4_linear_forward(x.cuda(), sq.sq_mxfp4_pack(w.cuda()), cout), ref, bound, (rows, cin, cout))
+
+
+def test_far_magnitudes(sq):
+    """Blocks near the ends of the powers of two: products that fp32 holds come out, larger ones are infinite."""
+    x = torch.full((20, 64), 3.0) * torch.exp2(torch.tensor([-120.0] * 10 + [100.0] * 10))[:, None]
+    w = torch.full((18, 64), 2.0) * torch.exp2(torch.tensor([100.0] * 9 + [-100.0] * 9))[:, None]
+    got = sq.sq_mxfp4_linear_forward(x.cuda(), sq.sq_mxfp4_pack(w.cuda()), 18).cpu().double()
+    want = values64(x) @ values64(w).t()
+    assert torch.equal(got[:10, :9], want[:10, :9]) and torch.equal(got[10:, 9:], want[10:, 9:])
+    assert got[10:, :9].isinf().all() and (got[:10, 9:].abs() <= 2.0 ** -126).all()
+
+
+def test_graph_streams_and_workspaces(sq):
+    """Captured with a workspace of its own and replayed between eager calls; two streams at once."""
+    cases = []
+    for rows, cin, cout in ((4, 4096, 512), (300, 512, 300)):
+        x, w = spread(rows, cin, 6).to(BF16).cuda(), sq.sq_mxfp4_pack(torch.randn((cout, cin), generator=gen(7)).cuda())
+        ws = torch.empty(max(1, sq.sq_mxfp4_linear_workspace_bytes(rows, cin, cout, BF16)), dtype=torch.uint8, device="cuda")
+        out = torch.empty((rows, cout), dtype=BF16, device="cuda")
+        cases.append((x, w, cout, ws, out, sq.sq_mxfp4_linear_forward(x, w, cout, act=1)))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for x, w, cout, ws, out, _ in cases:
+            sq.sq_mxfp4_linear_forward(x, w, cout, act=1, out=out, workspace=ws)
+    for turn in range(3):
+        for x, w, cout, ws, out, want in cases:
+            out.zero_()
+        graph.replay()
+        eager = [sq.sq_mxfp4_linear_forward(x, w, cout, act=1) for x, w, cout, *_ in cases]
+        torch.cuda.synchronize()
+        for (x, w, cout, ws, out, want), e in zip(cases, eager):
+            assert torch.equal(out, want) and torch.equal(e, want)
+    streams, results = [torch.cuda.Stream() for _ in range(2)], []
+    for turn in range(4):
+        for s, (x, w, cout, ws, out, want) in zip(streams, cases):
+            with torch.cuda.stream(s):
+                results.append((sq.sq_mxfp4_linear_forward(x, w, cout, act=1), want))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in results)
+
+
+def test_refusals_of_the_binding(sq):
+    x = torch.zeros(4, 64, device="cuda")
+    w = sq.sq_mxfp4_pack(torch.zeros(8, 64, device="cuda"))
+    for call in (lambda: sq.sq_mxfp4_linear_forward(x, w, 7), lambda: sq.sq_mxfp4_linear_forward(x, w.cpu(), 8), lambda: sq.sq_mxfp4_linear_forward(x.half(), w, 8),
+                 lambda: sq.sq_mxfp4_linear_forward(x, w, 8, b=torch.zeros(7, device="cuda")), lambda: sq.sq_mxfp4_linear_forward(x, w, 8, rows=4, Cin=64),
+                 lambda: sq.sq_mxfp4_linear_forward(w, w, 8), lambda: sq.sq_mxfp4_linear_forward(x.t(), w, 8), lambda: sq.sq_mxfp4_pack(x[0]),
+                 lambda: sq.sq_mxfp4_unpack(w, 9, 64), lambda: sq.sq_mxfp4_unpack(w, 8, 64, dtype=torch.float16),
+                 lambda: sq.sq_mxfp4_linear_forward(x, w, 8, residual=torch.zeros(4, 8, device="cuda", dtype=BF16), out_dtype=F32)):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    for call in (lambda: sq.sq_mxfp4_linear_forward(x, w, 8, act=4), lambda: sq.sq_mxfp4_pack(x[:0])):
+        with pytest.raises(sq.SqError):
+            call()
