@@ -33,40 +33,61 @@ template <int n, typename T> __device__ __forceinline__ Vec<T, n> load_n(const T
     return r;
 }
 
-// Bias, activation and residual of n neighbouring results of one row, of which the first `have` exist.
-template <typename TO, int n> __device__ __forceinline__ void finish(const LinearArgs &p, long long r, int j, int have, float (&v)[n])
+// The first `have` of n neighbouring values, more than none; the others are the last of them again.  (All loads are on their way
+// together: one behind the other, each under its own condition, they cost a memory latency apiece.)
+template <int n, typename T> __device__ __forceinline__ Vec<T, n> load_some(const T *p, int have)
 {
-    if (have <= 0) return;
-    TO *out = (TO *)p.out + r * p.ld_out + j;
-    const TO *res = (const TO *)p.residual + r * p.ld_res + j;
+    if (have >= n) return load_n<n>(p);
+    Vec<T, n> r;
+#pragma unroll
+    for (int i = 0; i < n; ++i) r.v[i] = p[min(i, have - 1)];
+    return r;
+}
+template <int n, typename T> __device__ __forceinline__ void store_some(T *p, const Vec<T, n> &v, int have)
+{
     if (have >= n) {
-        if (p.b) {
-            const Vec<float, n> b = load_n<n>(p.b + j);
-#pragma unroll
-            for (int i = 0; i < n; ++i) v[i] += b.v[i];
-        }
-        if (p.act != SQ_ACT_NONE) {
-#pragma unroll
-            for (int i = 0; i < n; ++i) v[i] = activate_by(v[i], p.act);
-        }
-        if (p.residual) {
-            const Vec<TO, n> q = load_n<n>(res);
-#pragma unroll
-            for (int i = 0; i < n; ++i) v[i] += to_f32(q.v[i]);
-        }
-        Vec<TO, n> o;
-#pragma unroll
-        for (int i = 0; i < n; ++i) o.v[i] = from_f32<TO>(v[i]);
-        __builtin_memcpy(out, &o, sizeof(o));
+        __builtin_memcpy(p, &v, sizeof(v));
         return;
     }
 #pragma unroll
     for (int i = 0; i < n; ++i)
-        if (i < have) {
-            float s = activate_by(p.b ? v[i] + p.b[j + i] : v[i], p.act);
-            if (p.residual) s += to_f32(res[i]);
-            out[i] = from_f32<TO>(s);
-        }
+        if (i < have) p[i] = v.v[i];
+}
+template <int n> __device__ __forceinline__ void activate_all(float (&v)[n], int act)
+{
+    auto each = [&](auto a) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = activate<decltype(a)::value>(v[i]);
+    };
+    switch (act) {      // the same for the whole launch
+        case SQ_ACT_RELU: return each(std::integral_constant<int, SQ_ACT_RELU>{});
+        case SQ_ACT_SILU: return each(std::integral_constant<int, SQ_ACT_SILU>{});
+        case SQ_ACT_GELU: return each(std::integral_constant<int, SQ_ACT_GELU>{});
+        default: return;
+    }
+}
+// Results from sums, bias and residual, out to the first `have` places.
+template <typename TO, int n> __device__ __forceinline__ void put(const LinearArgs &p, TO *out, int have, float (&v)[n], const Vec<float, n> &b, const Vec<TO, n> &res)
+{
+    if (p.b)
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] += b.v[i];
+    activate_all(v, p.act);
+    Vec<TO, n> o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) o.v[i] = from_f32<TO>(p.residual ? v[i] + to_f32(res.v[i]) : v[i]);
+    store_some<n>(out, o, have);
+}
+
+// Bias, activation and residual of n neighbouring results of one row, of which the first `have` exist.
+template <typename TO, int n> __device__ __forceinline__ void finish(const LinearArgs &p, long long r, int j, int have, float (&v)[n])
+{
+    if (have <= 0) return;
+    Vec<float, n> b = {};
+    Vec<TO, n> res = {};
+    if (p.b) b = load_some<n>(p.b + j, have);
+    if (p.residual) res = load_some<n>((const TO *)p.residual + r * p.ld_res + j, have);
+    put<TO, n>(p, (TO *)p.out + r * p.ld_out + j, have, v, b, res);
 }
 
 // Rows and layers of the b-th tile: neighbouring workgroups of one XCD take a band of eight row tiles, row tile fastest,
@@ -105,15 +126,22 @@ template <typename TO, int XB, int JB> __device__ __forceinline__ void write_row
         for (int e = 0; e < n; e += 4) *(f32x4_t *)&v[e] = *(const f32x4_t *)&buf[(row + t * kPer) * kRow + j + e];
     };
     if (!row_in(r0, 32 * XB - 1, p.rows) || !row_in(j0, 32 * JB - 1, p.Cout)) {     // the edge of the output
+        const int have = p.Cout - j0 - j;
+        Vec<float, n> b = {};
+        if (p.b && have > 0) b = load_some<n>(p.b + j0 + j, have);
 #pragma unroll
         for (int x = 0; x < XB; ++x) {
+            Vec<TO, n> res[kTurns] = {};
+            if (p.residual && have > 0)
+#pragma unroll
+                for (int t = 0; t < kTurns; ++t) res[t] = load_some<n>((const TO *)p.residual + row_at(r0, 32 * x + row + t * kPer, p.rows) * p.ld_res + j0 + j, have);
             stage(x);
-#pragma unroll 1
+#pragma unroll
             for (int t = 0; t < kTurns; ++t) {
+                const int i = 32 * x + row + t * kPer;
                 float v[n];
                 staged(t, v);
-                const int i = 32 * x + row + t * kPer;
-                if (row_in(r0, i, p.rows)) finish<TO>(p, (long long)r0 + i, j0 + j, p.Cout - j0 - j, v);
+                if (have > 0 && row_in(r0, i, p.rows)) put<TO, n>(p, (TO *)p.out + ((long long)r0 + i) * p.ld_out + j0 + j, have, v, b, res[t]);
             }
         }
         return;
