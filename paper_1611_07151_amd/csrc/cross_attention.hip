@@ -19,7 +19,7 @@ struct CrossParams {
     CrossArgs a;
     int group, rows;        // rows of an image and head of the states
     int tiles;              // of rows
-    int share, shares;      // of the states, in tiles of them
+    int share, shares;      // of the states: one workgroup's, and how many
     float c;                // |scale| log2 e, or 1 where the scale is 0
     uint32_t keep, flip;    // bits of q that stay (none where the scale is 0), sign bits that turn q into -q where it is below 0
     float *part_o;          // [share][image, head, row][part_ld] and
@@ -27,15 +27,35 @@ struct CrossParams {
     int part_ld;
 };
 
-template <typename T> __device__ __forceinline__ u32x4_t piece_of(const T *row, int d, int D, bool there)
+// 16 bytes of a head's D values from value d on, zeros behind the last.  EVEN: heads of whole pieces.  Others are loaded from where all 16
+// bytes are the head's own and moved into place by `placed`, so that no load waits for another, and heads of less than 16 bytes one
+// value at a time.
+template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t loaded(const T *head, int d, int D)
 {
     constexpr int n = 16 / (int)sizeof(T);
-    if (!there || d >= D) return u32x4_t{};
-    if (d + n <= D) return __builtin_bit_cast(u32x4_t, load_n<n>(row + d));
-    Vec<T, n> v;
+    if (EVEN || D >= n) return __builtin_bit_cast(u32x4_t, load_n<n>(head + min(d, D - n)));
+    return __builtin_bit_cast(u32x4_t, load_some<n>(head, D));
+}
+template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t placed(u32x4_t v, int d, int D)
+{
+    constexpr int n = 16 / (int)sizeof(T);
+    if (EVEN) {
+        if (d >= D) v = u32x4_t{};
+        return v;
+    }
+    if (D < n) {
+        Vec<T, n> r = __builtin_bit_cast(Vec<T, n>, v);
 #pragma unroll
-    for (int i = 0; i < n; ++i) v.v[i] = d + i < D ? row[d + i] : T(0);
-    return __builtin_bit_cast(u32x4_t, v);
+        for (int i = 0; i < n; ++i) r.v[i] = d + i < D ? r.v[i] : T(0);
+        return __builtin_bit_cast(u32x4_t, r);
+    }
+    const int away = max(d - (D - n), 0) * (int)sizeof(T);      // bytes
+    if (away >= 16) v = u32x4_t{};
+    if (away & 8) v = u32x4_t{v[2], v[3], 0, 0};
+    if (away & 4) v = u32x4_t{v[1], v[2], v[3], 0};
+    if (sizeof(T) == 2 && (away & 2))
+        v = u32x4_t{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16), v[3] >> 16};
+    return v;
 }
 
 __device__ __forceinline__ float other_half(float v)
@@ -43,11 +63,35 @@ __device__ __forceinline__ float other_half(float v)
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
     return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
+// maximum over the lanes that are 16 and 32 apart
+__device__ __forceinline__ float over_quarters(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t a = r[0], b = r[1];          // (a bit cast of a vector's element itself would take element 0)
+    v = fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    return fmaxf(v, other_half(v));
+}
+// maximum of three, NaN counting for nothing (written out: fmaxf first passes each operand through an instruction of its own)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    __asm__("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// Results of matrix instructions are read by instructions the compiler does not look into: until the last of them has been written.
+template <typename V> __device__ __forceinline__ void settled(V &v) { __asm__ volatile("s_nop 15\n\ts_nop 3" : "+v"(v)); }
 __device__ __forceinline__ uint32_t bf16_two(float a, float b)
 {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const bf16x2 v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, v);
+}
+
+// the sum of two bfloat16 values and c in fp32
+__device__ __forceinline__ float add_two(uint32_t two, float c)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), bf16x2{(__bf16)1.f, (__bf16)1.f}, c, false);
 }
 
 template <typename T> __device__ __forceinline__ void row_of(const CrossParams &p, int image, int head, int r, const T *&q, const uint8_t *&mask, T *&out)
@@ -58,6 +102,56 @@ template <typename T> __device__ __forceinline__ void row_of(const CrossParams &
     q = (const T *)p.a.q + at * p.a.ld_q + h;
     out = (T *)p.a.out + at * p.a.ld_out + h;
     mask = p.a.mask ? p.a.mask + image * p.a.mask_image + i * p.a.mask_row : nullptr;
+}
+
+// A masked value that is not finite has gone into a row's sums as 0 * it: a wavefront makes such a row again from the states it sees, lane by
+// lane of the head's values, its sums into `area`.
+template <typename T, int DP> __device__ __forceinline__ void row_again(const CrossParams &p, int image, int head, int r, int first, int end, float *area, float &base, float &total)
+{
+    constexpr int E = (DP + 63) / 64;
+    const int lane = threadIdx.x & 63, D = p.a.D;
+    const T *q;
+    const uint8_t *mask;
+    T *unused;
+    row_of<T>(p, image, head, r, q, mask, unused);
+    const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
+    float qv[E], sum[E] = {}, m = -HUGE_VALF, l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) qv[e] = lane + 64 * e < D ? (p.keep ? to_f32(q[lane + 64 * e]) : 0.f) * (p.flip ? -1.f : 1.f) : 0.f;
+    for (int j = first; j < end; ++j) {
+        if (mask && !mask[j]) continue;
+        float dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < D) dot = __builtin_fmaf(qv[e], to_f32(k0[j * p.a.ld_k + lane + 64 * e]), dot);
+        for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
+        const float up = fmaxf(m, dot * p.c), upc = up == -HUGE_VALF ? 0.f : up;
+        const float shrink = m == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(m - up), w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, p.c, -upc));
+        m = up;
+        l = l * shrink + w;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < D) sum[e] = sum[e] * shrink + w * to_f32(v0[j * p.a.ld_v + lane + 64 * e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (lane + 64 * e < DP) area[lane + 64 * e] = sum[e];
+    __builtin_amdgcn_wave_barrier();
+    base = m, total = l;
+}
+
+// Four neighbouring sums of a row from d on, out as results or as a share's sums.
+template <typename T> __device__ __forceinline__ void put4(const CrossParams &p, T *out, long long part, int d, const float (&v)[4], float total, float inverse)
+{
+    if (p.shares > 1) {
+        if (total != 0.f && d < p.part_ld) *(f32x4_t *)(p.part_o + part * p.part_ld + d) = f32x4_t{v[0], v[1], v[2], v[3]};
+        return;
+    }
+    if (d >= p.a.D) return;
+    Vec<T, 4> o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o.v[e] = from_f32<T>(total == 0.f ? 0.f : v[e] * inverse);
+    store_some<4>(out + d, o, p.a.D - d);
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------
@@ -79,11 +173,14 @@ template <> struct Tile<float> {
     static constexpr int value_step(int DP) { return DP / 4; }
 };
 
-template <typename T, int DP> __global__ __launch_bounds__(256) void cross_tile_kernel(CrossParams p)
+// How far scores may pass what the exponents are taken against: in base two, and a lane's sum over a tile.
+constexpr float kHeadroom = 8.f, kFar = 8192.f;
+
+template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(256, RB == 2 ? (DP <= 64 ? 2 : 1) : DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void cross_tile_kernel(CrossParams p)
 {
     constexpr bool kF32 = sizeof(T) == 4;
     constexpr int KT = Tile<T>::KT, n = 16 / (int)sizeof(T), P = DP / n, SK = Tile<T>::key_step(DP), SV = Tile<T>::value_step(DP);
-    constexpr int kImage = KT * (SK + SV), NP = KT * P / 256 ? KT * P / 256 : 1, KB = KT / 32, DB = DP / 32;
+    constexpr int kImage = KT * (SK + SV), NP = KT * P / 256, KB = KT / 32, DB = DP / 32;
     static_assert(KT * P % 256 == 0, "whole pieces per thread");
     __shared__ u32x4_t lds[2 * kImage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -94,31 +191,58 @@ template <typename T, int DP> __global__ __launch_bounds__(256) void cross_tile_
     const int tile = (int)(bt % (unsigned)p.tiles), ih = (int)(bt / (unsigned)p.tiles), image = ih / p.a.kv_heads, head = ih - image * p.a.kv_heads;
     const int D = p.a.D;
     const int len = p.a.lengths ? min(max(p.a.lengths[image], 0), p.a.Lk) : p.a.Lk;
-    const int first = min((long long)share * p.share * KT, (long long)len), end = min(((long long)share + 1) * p.share * KT, (long long)len);
+    const int first = min((long long)share * p.share, (long long)len), end = min(((long long)share + 1) * p.share, (long long)len);
 
-    const int row = tile * 128 + wave * 32 + (lane & 31);
-    const T *qrow;
-    const uint8_t *mask;
-    T *out;
-    row_of<T>(p, image, head, min(row, p.rows - 1), qrow, mask, out);
-    u32x4_t q[P / 2];
+    const int row0 = tile * (128 * RB) + wave * (32 * RB) + (lane & 31);
+    const uint8_t *mask[RB];
+    u32x4_t q[RB][P / 2];
 #pragma unroll
-    for (int t = 0; t < P / 2; ++t) {
-        q[t] = piece_of(qrow, (2 * t + half) * n, D, true);
+    for (int r = 0; r < RB; ++r) {
+        const T *qrow;
+        T *out;
+        row_of<T>(p, image, head, min(row0 + 32 * r, p.rows - 1), qrow, mask[r], out);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[t][e] = (q[t][e] & p.keep) ^ p.flip;
+        for (int t = 0; t < P / 2; ++t) q[r][t] = loaded<EVEN>(qrow, (2 * t + half) * n, D);
+#pragma unroll
+        for (int t = 0; t < P / 2; ++t) {
+            q[r][t] = placed<EVEN, T>(q[r][t], (2 * t + half) * n, D);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[r][t][e] = (q[r][t][e] & p.keep) ^ p.flip;
+        }
     }
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
+    // A thread's pieces are those at e % P of the states e / P of a tile, e = threadIdx.x + 256 i, the same in every tile.
     u32x4_t nk[NP], nv[NP];
-    auto fetch = [&](int at) {
+    long long step_k[NP], step_v[NP];
+    const bool whole = EVEN && D == DP;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int e = threadIdx.x + i * 256, j = at + e / P, d = e % P * n;
-            nk[i] = piece_of(k0 + j * p.a.ld_k, d, D, j < end);
-            nv[i] = piece_of(v0 + j * p.a.ld_v, d, D, j < end);
+    for (int i = 0; i < NP; ++i) {
+        const int e = threadIdx.x + i * 256, d = whole ? e % P * n : 0;
+        step_k[i] = e / P * p.a.ld_k + d, step_v[i] = e / P * p.a.ld_v + d;
+    }
+    auto fetch = [&](int at) {
+        const T *const kt = k0 + at * p.a.ld_k, *const vt = v0 + at * p.a.ld_v;
+        if (whole && at + KT <= end) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) nk[i] = __builtin_bit_cast(u32x4_t, load_n<n>(kt + step_k[i])), nv[i] = __builtin_bit_cast(u32x4_t, load_n<n>(vt + step_v[i]));
+        } else {        // states behind the last are the last one again
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int e = threadIdx.x + i * 256, j = min(e / P, end - 1 - at), d = e % P * n;
+                nk[i] = loaded<EVEN>(kt + j * p.a.ld_k, d, D);
+                nv[i] = loaded<EVEN>(vt + j * p.a.ld_v, d, D);
+            }
         }
     };
-    auto store = [&](u32x4_t *to) {
+    auto store = [&](u32x4_t *to, int at) {
+        if (!(whole && at + KT <= end)) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int e = threadIdx.x + i * 256, d = e % P * n;
+                nk[i] = placed<EVEN, T>(nk[i], d, D);
+                nv[i] = placed<EVEN, T>(nv[i], at + e / P < end ? d : D + n, D);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int e = threadIdx.x + i * 256, j = e / P, d = e % P;
@@ -126,11 +250,13 @@ template <typename T, int DP> __global__ __launch_bounds__(256) void cross_tile_
             to[KT * SK + j * SV + d] = nv[i];
         }
     };
-    f32x16_t o[DB] = {};
-    float base = -HUGE_VALF, total = 0.f;      // what the exponents were taken against, in base two
+    f32x16_t o[RB][DB] = {};
+    float base[RB], total[RB];      // what the exponents are taken against, in base two, and their sum
+#pragma unroll
+    for (int r = 0; r < RB; ++r) base[r] = -HUGE_VALF, total[r] = 0.f;
     if (first < end) {
         fetch(first);
-        store(lds);
+        store(lds, first);
     }
     __syncthreads();
     int img = 0;
@@ -138,253 +264,546 @@ template <typename T, int DP> __global__ __launch_bounds__(256) void cross_tile_
         const bool more = at + KT < end;
         if (more) fetch(at + KT);
         const u32x4_t *const keys = lds + img * kImage, *const values = keys + KT * SK;
-        f32x16_t s[KB];
+        f32x16_t s[RB][KB];
+        u32x4_t pt[RB][kF32 ? 1 : KT / 16];         // their exponentials: bfloat16 pairs, or as they are
+        f32x16_t pf[kF32 ? RB : 1];
+        float part[RB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            s[kb] = f32x16_t{};
+#pragma unroll
+            for (int r = 0; r < RB; ++r) s[r][kb] = f32x16_t{};
 #pragma unroll
             for (int t = 0; t < P / 2; ++t) {
                 const u32x4_t k = keys[(kb * 32 + (lane & 31)) * SK + 2 * t + half];
-                if constexpr (kF32) {
-                    const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[t]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[e], s[kb], 0, 0, 0);
-                } else {
-                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[t]), s[kb], 0, 0, 0);
-                }
-            }
-        }
-        if (mask || at + KT > end) {
+                for (int r = 0; r < RB; ++r) {
+                    if constexpr (kF32) {
+                        const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[r][t]);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int j = at + kb * 32 + i * 2 + half * 4;
-                    Vec<uint8_t, 4> m = {{1, 1, 1, 1}};
-                    if (mask) {
-                        if (j + 4 <= end) m = load_n<4>(mask + j);
-                        else
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) m.v[e] = j + e < end ? mask[j + e] : 0;
+                        for (int e = 0; e < 4; ++e) s[r][kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[e], s[r][kb], 0, 0, 0);
+                    } else {
+                        s[r][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[r][t]), s[r][kb], 0, 0, 0);
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[kb][i + e] = j + e < end && m.v[e] ? s[kb][i + e] : -HUGE_VALF;
                 }
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-        top = fmaxf(top, other_half(top));
-        top *= p.c;
-        if (__any(top > base)) {
-            const float raised = fmaxf(base, top), shrink = base == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base - raised);
-            total *= shrink;
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
-            base = raised;
-        }
-        const float mc = base == -HUGE_VALF ? 0.f : base;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], p.c, -mc));
-                total += s[kb][i];
             }
+        }
+        if (p.a.mask || at + KT > end) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int j = at + kb * 32 + i * 2 + half * 4;
+                        Vec<uint8_t, 4> m = {{1, 1, 1, 1}};
+                        if (p.a.mask && j < end) m = load_some<4>(mask[r] + j, end - j);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[r][kb][i + e] = j + e < end && m.v[e] ? s[r][kb][i + e] : -HUGE_VALF;
+                    }
+        }
+        // The exponents are taken against the base as it stands.  Only where there is none yet, or where a sum shows that scores have passed
+        // it by far, is the tile's maximum looked for and are they taken again.
+        auto exponents = [&](int r) {
+            const float off = base[r] == -HUGE_VALF ? 0.f : base[r];
+            part[r] = 0.f;
+            if constexpr (kF32) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    pf[r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][0][i], p.c, -off));
+                    part[r] += pf[r][i];
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = t % 2 * 8 + 2 * e;
+                        pt[r][t][e] = bf16_two(__builtin_amdgcn_exp2f(__builtin_fmaf(s[r][t / 2][i], p.c, -off)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][t / 2][i + 1], p.c, -off)));
+                        part[r] = add_two(pt[r][t][e], part[r]);
+                    }
+            }
+        };
+        bool far = false;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            exponents(r);
+            far |= part[r] > kFar || base[r] == -HUGE_VALF;
+        }
+        if (__any(far)) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float top = s[r][0][0];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[r][kb][i]);
+                top *= p.c;
+                const float raised = fmaxf(base[r], fmaxf(top, other_half(top))), shrink = base[r] == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base[r] - raised);
+                total[r] *= shrink;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[r][d][i] *= shrink;
+                base[r] = raised;
+                exponents(r);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) total[r] += part[r];
         if constexpr (kF32) {
             const float *const vf = (const float *)values;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[(i / 4 * 8 + half * 4 + i % 4) * SV * 4 + d * 32 + (lane & 31)], s[0][i], o[d], 0, 0, 0);
+                for (int d = 0; d < DB; ++d) {
+                    const float v = vf[(i / 4 * 8 + half * 4 + i % 4) * SV * 4 + d * 32 + (lane & 31)];
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, pf[r][i], o[r][d], 0, 0, 0);
+                }
         } else {
             typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
 #pragma unroll
             for (int t = 0; t < KT / 16; ++t) {
-                u32x4_t pt;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pt[e] = bf16_two(s[t / 2][t % 2 * 8 + 2 * e], s[t / 2][t % 2 * 8 + 2 * e + 1]);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     // sixteen lanes read four states of sixteen neighbouring values, a lane four of them, and get a column each
                     const char *const from = (const char *)(values + (t * 16 + half * 4 + (lane & 15) / 4) * SV) + d * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
                     const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(from + 8 * SV * 16));
                     const auto vt = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, pt), o[d], 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, pt[r][t]), o[r][d], 0, 0, 0);
                 }
             }
         }
         img ^= 1;
-        if (more) store(lds + img * kImage);
+        if (more) store(lds + img * kImage, at + KT);
         __syncthreads();
     }
-    total += other_half(total);
-    if (p.a.mask) {
-        // A masked value that is not finite has gone into the sums as 0 * it: such rows are made again from the states they see.
-        bool odd = false;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+    for (int r = 0; r < RB; ++r) {
+        total[r] += other_half(total[r]);
+        const int row = row0 + 32 * r;
+        if (p.a.mask) {
+            bool odd = false;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) odd |= !__builtin_isfinite(o[d][i]);
-        const uint64_t lanes = __ballot(odd);
-        uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
-        float *const area = (float *)lds + wave * DP;       // a row's sums, in the wavefront's own part
-        static_assert(4 * DP * 4 <= 2 * kImage * 16, "the areas fit");
-        while (again) {
-            const int which = __builtin_ctz(again);
-            again &= again - 1;
-            const T *qr;
-            const uint8_t *mr;
-            T *unused;
-            row_of<T>(p, image, head, min(tile * 128 + wave * 32 + which, p.rows - 1), qr, mr, unused);
-            constexpr int E = (DP + 63) / 64;
-            float qv[E], sum[E] = {}, m = -HUGE_VALF, l = 0.f;
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < E; ++e) qv[e] = lane + 64 * e < D ? (p.keep ? to_f32(qr[lane + 64 * e]) : 0.f) * (p.flip ? -1.f : 1.f) : 0.f;
-            for (int j = first; j < end; ++j) {
-                if (!mr[j]) continue;
-                float dot = 0.f;
+                for (int i = 0; i < 16; ++i) odd |= !__builtin_isfinite(o[r][d][i]);
+            const uint64_t lanes = __ballot(odd && row < p.rows);
+            uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+            float *const area = (float *)lds + wave * DP;
+            static_assert(4 * DP * 4 <= 2 * kImage * 16, "the areas fit");
+            while (again) {
+                const int which = __builtin_ctz(again);
+                again &= again - 1;
+                float m, l;
+                row_again<T, DP>(p, image, head, row - (lane & 31) + which, first, end, area, m, l);
+                if ((lane & 31) == which) {
+                    base[r] = m, total[r] = l;
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (lane + 64 * e < D) dot = __builtin_fmaf(qv[e], to_f32(k0[j * p.a.ld_k + lane + 64 * e]), dot);
-                for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
-                const float up = fmaxf(m, dot * p.c), upc = up == -HUGE_VALF ? 0.f : up;
-                const float shrink = m == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(m - up), w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, p.c, -upc));
-                m = up;
-                l = l * shrink + w;
+                    for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (lane + 64 * e < D) sum[e] = sum[e] * shrink + w * to_f32(v0[j * p.a.ld_v + lane + 64 * e]);
+                        for (int i = 0; i < 16; ++i) o[r][d][i] = area[d * 32 + i / 4 * 8 + half * 4 + i % 4];
+                }
+                __builtin_amdgcn_wave_barrier();
             }
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (lane + 64 * e < DP) area[lane + 64 * e] = sum[e];
-            __builtin_amdgcn_wave_barrier();
-            if ((lane & 31) == which) {
-                base = m, total = l;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] = area[d * 32 + i / 4 * 8 + half * 4 + i % 4];
-            }
-            __builtin_amdgcn_wave_barrier();
         }
-    }
-    if (row >= p.rows) return;
-    if (p.shares > 1) {
-        const long long at = ((long long)share * p.a.N * p.a.kv_heads + ih) * p.rows + row;
-        if (half == 0) p.part_ml[at] = float2{base, total};
-        if (total == 0.f) return;
+        if (row >= p.rows) continue;
+        const long long part = ((long long)share * p.a.N * p.a.kv_heads + ih) * p.rows + row;
+        if (p.shares > 1 && half == 0) p.part_ml[part] = float2{base[r], total[r]};
+        const T *qrow;
+        const uint8_t *unused;
+        T *out;
+        row_of<T>(p, image, head, row, qrow, unused, out);
+        const float inverse = 1.f / total[r];
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const int at_d = d * 32 + i * 2 + half * 4;
-                if (at_d < p.part_ld) *(f32x4_t *)(p.part_o + at * p.part_ld + at_d) = f32x4_t{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+                const float v[4] = {o[r][d][i], o[r][d][i + 1], o[r][d][i + 2], o[r][d][i + 3]};
+                put4<T>(p, out, part, d * 32 + i * 2 + half * 4, v, total[r], inverse);
             }
-        return;
     }
-    const float inverse = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int at_d = d * 32 + i * 2 + half * 4;
-            Vec<T, 4> v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v.v[e] = from_f32<T>(total == 0.f ? 0.f : o[d][i + e] * inverse);
-            if (at_d + 4 <= D) {
-                __builtin_memcpy(out + at_d, &v, sizeof(v));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (at_d + e < D) out[at_d + e] = v.v[e];
-            }
-        }
 }
 
-// Four neighbouring results of a row from the shares' sums.
-template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(CrossParams p, long long all)
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+// A workgroup takes 16 rows, its wavefronts share out the states in chunks of KC, each with sums of its own for all 16 rows, which are
+// added up through LDS in the end.  Keys go from memory straight into the lanes of the 16 x 16 instructions (lane l takes 16 bytes of key
+// l % 16 at piece l / 16), and the next chunk's are on their way as soon as these are multiplied.  Scores lie transposed as above: lane l
+// has states 4 (l / 16) to 4 (l / 16) + 3 of row l % 16.
+//   bf16: values go through the wavefront's part of LDS, which gives them back transposed
+//   fp32: an instruction takes one state of each four, and value e of each four of a head, so that lanes load 16 bytes of neighbouring values
+template <typename T> struct Chunk;
+template <> struct Chunk<bf16_t> {
+    static constexpr int KC = 32;
+};
+template <> struct Chunk<float> {
+    static constexpr int KC = 16;
+};
+template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64 * NW) void cross_wave_kernel(CrossParams p)
+{
+    constexpr bool kF32 = sizeof(T) == 4;
+    constexpr int KC = Chunk<T>::KC, n = 16 / (int)sizeof(T), P = DP / n, KB = KC / 16;
+    constexpr int SV = Tile<T>::value_step(DP);     // bf16: pieces from one state to the next in LDS
+    constexpr int NV = kF32 ? 4 * ((DP + 63) / 64) : KC * P / 64, DB = kF32 ? (DP + 63) / 64 * 4 : DP / 16;
+    constexpr int kRow = DP + 4;                                    // of a wavefront's sums
+    constexpr int kArea = kF32 ? 0 : KC * SV, kRoom = kArea > 4 * kRow ? NW * kArea : NW * 4 * kRow;        // 16 bytes: of a wavefront's values; in all
+    __shared__ u32x4_t lds[kRoom];
+    __shared__ float bases[NW][16], totals[NW][16];
+    __shared__ int again[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, quarter = lane >> 4;
+    const unsigned share = blockIdx.x % (unsigned)p.shares, bt = blockIdx.x / (unsigned)p.shares;
+    const int tile = (int)(bt % (unsigned)p.tiles), ih = (int)(bt / (unsigned)p.tiles), image = ih / p.a.kv_heads, head = ih - image * p.a.kv_heads;
+    const int D = p.a.D;
+    const int len = p.a.lengths ? min(max(p.a.lengths[image], 0), p.a.Lk) : p.a.Lk;
+    const int first = min((long long)share * p.share, (long long)len), end = min(((long long)share + 1) * p.share, (long long)len);
+    const int row = tile * 16 + l16;
+    const T *qrow;
+    const uint8_t *mask;
+    T *out;
+    row_of<T>(p, image, head, min(row, p.rows - 1), qrow, mask, out);
+    u32x4_t q[P / 4];
+#pragma unroll
+    for (int t = 0; t < P / 4; ++t) q[t] = loaded<EVEN>(qrow, (4 * t + quarter) * n, D);
+    const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
+    u32x4_t nk[KB][P / 4], nv[NV];
+    auto fetch_keys = [&](int at) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int t = 0; t < P / 4; ++t) nk[kb][t] = loaded<EVEN>(k0 + min(at + kb * 16 + l16, end - 1) * p.a.ld_k, (4 * t + quarter) * n, D);
+    };
+    // bf16: piece e % P of state e / P, e = lane + 64 i; fp32: values 64 (i / 4) + 4 (lane % 16) on of state 4 (lane / 16) + i % 4
+    auto value_state = [&](int i) { return kF32 ? 4 * quarter + i % 4 : (lane + 64 * i) / P; };
+    auto value_at = [&](int i) { return kF32 ? i / 4 * 64 + 4 * l16 : (lane + 64 * i) % P * n; };
+    auto fetch_values = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) nv[i] = loaded<EVEN>(v0 + min(at + value_state(i), end - 1) * p.a.ld_v, value_at(i), D);
+    };
+    f32x4_t o[DB] = {};
+    float base = -HUGE_VALF, total = 0.f;
+    int at = first + wave * KC;
+    if (at < end) {
+        fetch_keys(at);
+        fetch_values(at);
+    }
+#pragma unroll
+    for (int t = 0; t < P / 4; ++t) {
+        q[t] = placed<EVEN, T>(q[t], (4 * t + quarter) * n, D);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[t][e] = (q[t][e] & p.keep) ^ p.flip;
+    }
+    u32x4_t *const area = lds + wave * kArea;
+    for (; at < end; at += NW * KC) {
+        const bool more = at + NW * KC < end;
+        f32x4_t s[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            s[kb] = f32x4_t{};
+#pragma unroll
+            for (int t = 0; t < P / 4; ++t) {
+                const u32x4_t k = placed<EVEN, T>(nk[kb][t], (4 * t + quarter) * n, D);
+                if constexpr (kF32) {
+                    const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[t]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], s[kb], 0, 0, 0);
+                } else {
+                    s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[t]), s[kb], 0, 0, 0);
+                }
+            }
+        }
+        if (more) fetch_keys(at + NW * KC);
+        if (mask || at + KC > end) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const int j = at + kb * 16 + quarter * 4;
+                Vec<uint8_t, 4> m = {{1, 1, 1, 1}};
+                if (mask && j < end) m = load_some<4>(mask + j, end - j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[kb][e] = j + e < end && m.v[e] ? s[kb][e] : -HUGE_VALF;
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) settled(s[kb]);
+        float top = max3(s[0][0], s[0][1], s[0][2]);
+        top = max3(top, s[0][3], s[KB - 1][0]);
+        if constexpr (KB > 1) top = max3(max3(top, s[1][1], s[1][2]), s[1][3], top);
+        top *= p.c;
+        if (__any(top > base + kHeadroom)) {
+            const float raised = fmaxf(base, over_quarters(top)), shrink = base == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base - raised);
+            total *= shrink;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] *= shrink;
+            base = raised;
+        }
+        const float off = base == -HUGE_VALF ? 0.f : base;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[kb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], p.c, -off));
+                total += s[kb][e];
+            }
+        u32x4_t v[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = placed<EVEN, T>(nv[i], at + value_state(i) < end ? value_at(i) : D + n, D);
+        if constexpr (kF32) {
+            if (more) fetch_values(at + NW * KC);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4_t, v[i])[e], s[0][i % 4], o[i / 4 * 4 + e], 0, 0, 0);
+        } else {
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) area[(lane + 64 * i) / P * SV + (lane + 64 * i) % P] = v[i];
+            __builtin_amdgcn_wave_barrier();
+            if (more) fetch_values(at + NW * KC);
+            typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+            const u32x4_t pt = {bf16_two(s[0][0], s[0][1]), bf16_two(s[0][2], s[0][3]), bf16_two(s[KB - 1][0], s[KB - 1][1]), bf16_two(s[KB - 1][2], s[KB - 1][3])};
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const char *const from = (const char *)(area + (quarter * 4 + l16 / 4) * SV) + d * 32 + (lane & 3) * 8;
+                const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(from + 16 * SV * 16));
+                const auto vt = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, pt), o[d], 0, 0, 0);
+            }
+        }
+    }
+    // every wavefront's sums against the largest base, added up by all threads, four of a row each, in order of wavefronts
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    if (quarter == 0) bases[wave][l16] = base, totals[wave][l16] = total;
+    __syncthreads();
+    float most = bases[0][l16];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) most = fmaxf(most, bases[w][l16]);
+    // (without a base the sums are zero, or not finite: of a score that is NaN, or of 0 * a masked value)
+    const float by = base == -HUGE_VALF ? 1.f : __builtin_amdgcn_exp2f(base - most);
+    float *const sums = (float *)lds;
+    if (row < p.rows)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            // the d-th four neighbouring sums of a lane
+            f32x4_t v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = by * (kF32 ? o[d / 4 * 4 + e][d % 4] : o[d][e]);
+            const int at_d = kF32 ? d / 4 * 64 + quarter * 16 + d % 4 * 4 : d * 16 + quarter * 4;
+            if (at_d < DP) *(f32x4_t *)&sums[(wave * 16 + l16) * kRow + at_d] = v;
+        }
+    if (threadIdx.x < 16) again[threadIdx.x] = 0;
+    __syncthreads();
+    constexpr int kQuads = DP / 4, kTurns = (16 * kQuads + 64 * NW - 1) / (64 * NW);
+    f32x4_t of[kTurns];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        const int e = threadIdx.x + t * 64 * NW, r = e / kQuads, d = e % kQuads * 4;
+        if (r >= 16 || tile * 16 + r >= p.rows) continue;
+        of[t] = *(const f32x4_t *)&sums[r * kRow + d];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) of[t] += *(const f32x4_t *)&sums[(w * 16 + r) * kRow + d];
+        if (mask && !(__builtin_isfinite(of[t][0]) && __builtin_isfinite(of[t][1]) && __builtin_isfinite(of[t][2]) && __builtin_isfinite(of[t][3]))) again[r] = 1;
+    }
+    if (mask) {
+        __syncthreads();
+        for (int r = wave; r < 16; r += NW)
+            if (again[r]) {
+                float m, l;
+                row_again<T, DP>(p, image, head, tile * 16 + r, first, end, &sums[r * kRow], m, l);
+                if (lane < NW) bases[lane][r] = m, totals[lane][r] = lane ? 0.f : l;
+            }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        const int e = threadIdx.x + t * 64 * NW, r = e / kQuads, d = e % kQuads * 4;
+        if (r >= 16 || tile * 16 + r >= p.rows) continue;
+        if (mask && again[r]) of[t] = *(const f32x4_t *)&sums[r * kRow + d];
+        float top = bases[0][r], sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) top = fmaxf(top, bases[w][r]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += bases[w][r] == -HUGE_VALF ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f(bases[w][r] - top);
+        const long long part = ((long long)share * p.a.N * p.a.kv_heads + ih) * p.rows + tile * 16 + r;
+        if (p.shares > 1 && d == 0) p.part_ml[part] = float2{top, sum};
+        const T *q_of;
+        const uint8_t *mask_of;
+        T *to;
+        row_of<T>(p, image, head, tile * 16 + r, q_of, mask_of, to);
+        const float v[4] = {of[t][0], of[t][1], of[t][2], of[t][3]};
+        put4<T>(p, to, part, d, v, sum, 1.f / sum);
+    }
+}
+
+// Four neighbouring results of a row from few shares' sums.
+constexpr int kFewShares = 8;
+template <typename T> __global__ __launch_bounds__(256) void cross_join_few_kernel(CrossParams p, long long all)
 {
     const int quads = p.part_ld / 4;
     const long long e = blockIdx.x * 256ll + threadIdx.x, at = e / quads;
     if (at >= all) return;
     const int d = (int)(e - at * quads) * 4;
-    float most = -HUGE_VALF;
-    for (int s = 0; s < p.shares; ++s) {
-        const float2 ml = p.part_ml[s * all + at];
-        if (ml.y != 0.f) most = fmaxf(most, ml.x);
-    }
-    float total = 0.f;
-    f32x4_t sum = {};
-    for (int s = 0; s < p.shares; ++s) {
-        const float2 ml = p.part_ml[s * all + at];
-        if (ml.y == 0.f) continue;
-        const float w = ml.x == most ? 1.f : __builtin_amdgcn_exp2f(ml.x - most);
-        total += w * ml.y;
-        sum += w * *(const f32x4_t *)(p.part_o + (s * all + at) * p.part_ld + d);
-    }
+    float2 ml[kFewShares];
+    f32x4_t of[kFewShares];
+#pragma unroll
+    for (int s = 0; s < kFewShares; ++s)
+        if (s < p.shares) {
+            ml[s] = p.part_ml[s * all + at];
+            of[s] = *(const f32x4_t *)(p.part_o + (s * all + at) * p.part_ld + d);      // (not written where a share saw nothing; not used then)
+        }
+    float most = -HUGE_VALF, total = 0.f;
+#pragma unroll
+    for (int s = 0; s < kFewShares; ++s)
+        if (s < p.shares && ml[s].y != 0.f) most = fmaxf(most, ml[s].x);
+    f32x4_t v = {};
+#pragma unroll
+    for (int s = 0; s < kFewShares; ++s)
+        if (s < p.shares && ml[s].y != 0.f) {
+            const float w = ml[s].x == most ? 1.f : __builtin_amdgcn_exp2f(ml[s].x - most);
+            total += w * ml[s].y;
+            v += w * of[s];
+        }
     const int ih = (int)(at / p.rows), image = ih / p.a.kv_heads;
     const T *q;
     const uint8_t *mask;
     T *out;
     row_of<T>(p, image, ih - image * p.a.kv_heads, (int)(at - (long long)ih * p.rows), q, mask, out);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (d + i < p.a.D) out[d + i] = from_f32<T>(total == 0.f ? 0.f : sum[i] / total);
+    const float f[4] = {v[0], v[1], v[2], v[3]};
+    p.shares = 1;
+    put4<T>(p, out, 0, d, f, total, 1.f / total);
 }
 
-// Widths the tiles are made for.
-int padded(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 160 ? 160 : 256; }
-int tile_keys(int dtype) { return dtype == SQ_F32 ? 32 : 64; }
+// The shares' sums of a row, four neighbouring values to a thread, the shares dealt out among as many threads as a workgroup has beside that:
+// one after the other they cost a memory latency each (16 shares of 256 rows 21 us, in parallel 4).
+constexpr int kMostShares = 64;
+template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(CrossParams p, long long all, int lanes)
+{
+    __shared__ float weights[kMostShares], sum_of;
+    __shared__ f32x4_t red[256];
+    const long long at = blockIdx.x;
+    if (threadIdx.x < 64) {
+        const float2 ml = (int)threadIdx.x < p.shares ? p.part_ml[threadIdx.x * all + at] : float2{-HUGE_VALF, 0.f};
+        const bool none = ml.y == 0.f;
+        float most = none ? -HUGE_VALF : ml.x;
+        for (int x = 32; x; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
+        const float w = none ? 0.f : ml.x == most ? 1.f : __builtin_amdgcn_exp2f(ml.x - most);
+        float sum = none ? 0.f : w * ml.y;
+        for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
+        weights[threadIdx.x] = w;
+        if (threadIdx.x == 0) sum_of = sum;
+    }
+    __syncthreads();
+    const int group = threadIdx.x / (unsigned)lanes, groups = 256 / lanes, d = ((int)threadIdx.x - group * lanes) * 4;
+    f32x4_t v = {};
+    if (d < p.part_ld)
+#pragma unroll 4
+        for (int s = group; s < p.shares; s += groups)
+            if (weights[s] != 0.f) v += weights[s] * *(const f32x4_t *)(p.part_o + (s * all + at) * p.part_ld + d);
+    red[threadIdx.x] = v;
+    __syncthreads();
+    if (group || d >= p.a.D) return;
+    for (int g = 1; g < groups; ++g) v += red[g * lanes + threadIdx.x];
+    const int ih = (int)(at / p.rows), image = ih / p.a.kv_heads;
+    const T *q;
+    const uint8_t *mask;
+    T *out;
+    row_of<T>(p, image, ih - image * p.a.kv_heads, (int)(at - (long long)ih * p.rows), q, mask, out);
+    Vec<T, 4> o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.v[i] = from_f32<T>(sum_of == 0.f ? 0.f : v[i] / sum_of);
+    store_some<4>(out + d, o, p.a.D - d);
+}
 
-// How the states are shared out: in as many shares as it takes to fill the chip with workgroups, none shorter than four tiles.
-struct Plan { int rows, tiles, share, shares; };
-bool plan_of(int N, int Lq, int Lk, int heads, int kv_heads, int dtype, Plan &plan)
+// Widths the kernels are made for.
+constexpr int wave_count(int DP) { return DP <= 64 ? 16 : DP <= 160 ? 8 : 4; }
+int padded(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 160 ? 160 : 256; }
+
+// How the rows are shared out, in blocks of `block` (16: the form for few rows), and the states, in shares of `share`.  By estimate: us of a
+// workgroup's pass over a tile of states (bf16 64, fp32 32; in the form for few rows what its wavefronts take at a time) when it has a compute
+// unit to itself and when units are full, from what heads of 64 measured; a second launch that joins shares costs 4 us, and their sums' bytes.
+// (us, blocks of 16 / 128 / 256, bf16, 8 heads of 64: 64 rows x 2000 states 14.4 / 12.4 / 16.2, 512 x 2000 15.9 / 19.9 / 24.6, 2 images of 2000 x
+// 2000 110 / 35 / 72, 4 of 3025 x 4096 with 16 heads 1057 / 250 / 236; 256 rows in heads of 128 435 / 820.)  Of plans within 5 % the one with
+// the most shares: images may have fewer states than the others.
+struct Plan { int rows, tiles, share, shares, block; };
+bool plan_of(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype, Plan &plan)
 {
     const long long rows = (long long)Lq * (heads / kv_heads);
     if (rows > 1 << 30 || Lk > 1 << 30) return false;
-    plan.rows = (int)rows;
-    plan.tiles = (int)((rows - 1) / 128 + 1);
-    const double blocks = (double)N * kv_heads * plan.tiles;
-    const int key_tiles = (Lk - 1) / tile_keys(dtype) + 1;
-    int shares = blocks >= 256 ? 1 : std::min({(int)(512 / blocks), key_tiles / 4, 64});
-    shares = std::max(shares, 1);
-    plan.share = (key_tiles - 1) / shares + 1;
-    plan.shares = (key_tiles - 1) / plan.share + 1;
-    return one_launch(blocks * plan.shares, 256);
+    const bool f32 = dtype == SQ_F32;
+    const int DP = padded(D), waves = wave_count(DP);
+    const double g = std::max(DP / 64.0, 0.6);
+    struct Form { int block, unit, fit; double alone, full; };
+    const Form forms[] = {{16, waves * (f32 ? 16 : 32), 1, f32 ? 3.5 : DP <= 64 ? 2.7 : 2.4, f32 ? 3.5 : DP <= 64 ? 2.7 : 2.4},
+                          {128, f32 ? 32 : 64, DP <= 64 ? 3 : DP <= 128 ? 2 : 1, g * (f32 ? 2.5 : 1.05), g * (f32 ? 2.1 : 0.62)},
+                          {256, 64, 2, g * 2.2, g * 1.17}};
+    double best = HUGE_VAL;
+    for (int i = 0; i < (f32 || DP > 64 ? 2 : 3); ++i) {
+        const Form &w = forms[i];
+        const int tiles = (int)((rows - 1) / w.block + 1), units = std::max((Lk - 1) / w.unit + 1, 1);
+        const double blocks = (double)N * kv_heads * tiles;
+        for (int want = 1; want <= std::min(units, kMostShares); want += want < 4 ? 1 : want < 16 ? 4 : 16) {
+            const int each = (units - 1) / want + 1, shares = (units - 1) / each + 1;
+            if ((shares != want && want > 1) || !one_launch(blocks * shares, 1024)) continue;
+            const double on_one = std::ceil(blocks * shares / 256);
+            const double us = 3.0 + (w.block == 16 ? 0.8 * on_one : 1.5) + each * std::max(w.alone * std::ceil(on_one / w.fit), w.full * on_one) +
+                              (shares > 1 ? 4.0 + 4e-6 * shares * N * kv_heads * rows * D : 0.0);
+            if (us < (shares > plan.shares && best < HUGE_VAL && plan.block == w.block && plan.shares > 1 ? 1.05 : 1.0) * best) {
+                best = std::min(best, us);
+                plan = Plan{(int)rows, tiles, each * w.unit, shares, w.block};
+            }
+        }
+    }
+    return best < HUGE_VAL;
 }
 int part_row(int D) { return (D + 3) / 4 * 4; }
 
-template <typename T, int DP> int launch_tile(const CrossParams &p)
+template <typename T, int DP, bool EVEN> int launch(const CrossParams &p, int block)
 {
-    const LaunchScope prof("cross_tile", cross_flops(p.a), cross_bytes(p.a));
-    hipLaunchKernelGGL((cross_tile_kernel<T, DP>), dim3((unsigned)(p.a.N * p.a.kv_heads) * p.tiles * p.shares), dim3(256), 0, current_stream(), p);
+    const dim3 grid((unsigned)(p.a.N * p.a.kv_heads) * p.tiles * p.shares);
+    const LaunchScope prof(block == 16 ? "cross_wave" : "cross_tile", cross_flops(p.a), cross_bytes(p.a));
+    constexpr int NW = wave_count(DP);
+    if (block == 16) {
+        hipLaunchKernelGGL((cross_wave_kernel<T, DP, NW, EVEN>), grid, dim3(64 * NW), 0, current_stream(), p);
+        return check_launch();
+    }
+    if constexpr (sizeof(T) == 2 && DP <= 64)
+        if (block == 256) {
+            hipLaunchKernelGGL((cross_tile_kernel<T, DP, 2, EVEN>), grid, dim3(256), 0, current_stream(), p);
+            return check_launch();
+        }
+    hipLaunchKernelGGL((cross_tile_kernel<T, DP, 1, EVEN>), grid, dim3(256), 0, current_stream(), p);
     return check_launch();
 }
-template <typename T> int by_width(const CrossParams &p)
+template <typename T, int DP> int launch(const CrossParams &p, int block)
+{
+    return p.a.D % (16 / (int)sizeof(T)) == 0 ? launch<T, DP, true>(p, block) : launch<T, DP, false>(p, block);
+}
+template <typename T> int by_width(const CrossParams &p, int block)
 {
     switch (padded(p.a.D)) {
-        case 32: return launch_tile<T, 32>(p);
-        case 64: return launch_tile<T, 64>(p);
-        case 96: return launch_tile<T, 96>(p);
-        case 128: return launch_tile<T, 128>(p);
-        case 160: return launch_tile<T, 160>(p);
-        default: return launch_tile<T, 256>(p);
+        case 32: return launch<T, 32>(p, block);
+        case 64: return launch<T, 64>(p, block);
+        case 96: return launch<T, 96>(p, block);
+        case 128: return launch<T, 128>(p, block);
+        case 160: return launch<T, 160>(p, block);
+        default: return launch<T, 256>(p, block);
     }
 }
-template <typename T> int run(const CrossParams &p)
+template <typename T> int run(const CrossParams &p, int block)
 {
-    if (const int rc = by_width<T>(p)) return rc;
+    if (const int rc = by_width<T>(p, block)) return rc;
     if (p.shares == 1) return SQ_OK;
     const long long all = (long long)p.a.N * p.a.kv_heads * p.rows;
     const LaunchScope prof("cross_join", 0, 0);
-    hipLaunchKernelGGL((cross_join_kernel<T>), dim3((unsigned)((all * (p.part_ld / 4) - 1) / 256 + 1)), dim3(256), 0, current_stream(), p, all);
+    if (p.shares <= kFewShares) {
+        hipLaunchKernelGGL((cross_join_few_kernel<T>), dim3((unsigned)((all * (p.part_ld / 4) - 1) / 256 + 1)), dim3(256), 0, current_stream(), p, all);
+        return check_launch();
+    }
+    int lanes = 1;
+    while (lanes * 4 < p.part_ld) lanes *= 2;
+    hipLaunchKernelGGL((cross_join_kernel<T>), dim3((unsigned)all), dim3(256), 0, current_stream(), p, all, lanes);
     return check_launch();
 }
 
@@ -392,16 +811,16 @@ template <typename T> int run(const CrossParams &p)
 
 size_t cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype)
 {
-    Plan plan;
-    if (!plan_of(N, Lq, Lk, heads, kv_heads, dtype, plan) || plan.shares == 1) return 0;
+    Plan plan{};
+    if (!plan_of(N, Lq, Lk, heads, kv_heads, D, dtype, plan) || plan.shares == 1) return 0;
     const size_t rows = (size_t)plan.shares * N * kv_heads * plan.rows;
     return align_up(rows * part_row(D) * sizeof(float), 256) + rows * sizeof(float2);
 }
 
 int cross_attention(const CrossArgs &a)
 {
-    Plan plan;
-    if (!plan_of(a.N, a.Lq, a.Lk, a.heads, a.kv_heads, a.dtype, plan)) return SQ_ERR_UNSUPPORTED;
+    Plan plan{};
+    if (!plan_of(a.N, a.Lq, a.Lk, a.heads, a.kv_heads, a.D, a.dtype, plan)) return SQ_ERR_UNSUPPORTED;
     CrossParams p{};
     p.a = a;
     p.group = a.heads / a.kv_heads;
@@ -412,13 +831,13 @@ int cross_attention(const CrossArgs &a)
     p.part_ld = part_row(a.D);
     p.part_o = (float *)a.workspace;
     p.part_ml = (float2 *)((char *)a.workspace + align_up((size_t)p.shares * a.N * a.kv_heads * p.rows * p.part_ld * sizeof(float), 256));
-    return a.dtype == SQ_F32 ? run<float>(p) : run<bf16_t>(p);
+    return a.dtype == SQ_F32 ? run<float>(p, plan.block) : run<bf16_t>(p, plan.block);
 }
 
 bool cross_attention_register_kernels()
 {
     hipFuncAttributes a;
-    return hipFuncGetAttributes(&a, (const void *)cross_tile_kernel<bf16_t, 64>) == hipSuccess;
+    return hipFuncGetAttributes(&a, (const void *)cross_tile_kernel<bf16_t, 64, 1, true>) == hipSuccess;
 }
 
 }  // namespace sq
