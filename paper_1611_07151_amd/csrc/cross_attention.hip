@@ -27,21 +27,50 @@ struct CrossParams {
     int part_ld;
 };
 
-// 16 bytes of a head's D values from value d on, zeros behind the last.  EVEN: heads of whole pieces.  Others are loaded from where all 16
-// bytes are the head's own and moved into place by `placed`, so that no load waits for another, and heads of less than 16 bytes one
-// value at a time.
-template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t loaded(const T *head, int d, int D)
+// 16 bytes of a head's D values from value d on, zeros behind the last.  EVEN: heads of whole pieces, rows of whole pieces.  Others are loaded
+// from where all 16 bytes are the head's own and moved into place by `placed`, so that no load waits for another, and heads of less than
+// 16 bytes one value at a time.  bfloat16 values may begin between words: the words that hold them are loaded, none beyond (16 bytes at
+// such an address take four times as long), and `placed` shifts them too.
+template <bool EVEN, typename T> struct Piece {
+    u32x4_t v;
+};
+template <> struct Piece<false, bf16_t> {
+    u32x4_t v;
+    uint32_t behind;        // the word behind, where the values begin between words
+};
+template <typename T> __device__ __forceinline__ uint32_t between_words(const T *p) { return (uint32_t)(uintptr_t)p >> 1 & 1; }
+template <bool EVEN, typename T> __device__ __forceinline__ Piece<EVEN, T> loaded(const T *head, int d, int D)
 {
     constexpr int n = 16 / (int)sizeof(T);
-    if (EVEN || D >= n) return __builtin_bit_cast(u32x4_t, load_n<n>(head + min(d, D - n)));
-    return __builtin_bit_cast(u32x4_t, load_some<n>(head, D));
+    Piece<EVEN, T> r;
+    if constexpr (!EVEN && sizeof(T) == 2) {
+        r.behind = 0;
+        if (D >= n) {
+            const T *const at = head + min(d, D - n);
+            const bool between = (uintptr_t)at & 2;
+            const uint32_t *const words = (const uint32_t *)((uintptr_t)at & ~(uintptr_t)3);
+            __builtin_memcpy(&r.v, words, 16);
+            r.behind = words[between ? 4 : 3];
+            return r;
+        }
+    }
+    r.v = EVEN || D >= n ? __builtin_bit_cast(u32x4_t, load_n<n>(head + min(d, D - n))) : __builtin_bit_cast(u32x4_t, load_some<n>(head, D));
+    return r;
 }
-template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t placed(u32x4_t v, int d, int D)
+// `there`: whether the state is (zeros otherwise); odd: whether the head begins between words.
+template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t placed(const Piece<EVEN, T> &piece, int d, int D, bool odd, bool there = true)
 {
     constexpr int n = 16 / (int)sizeof(T);
+    u32x4_t v = piece.v;
+    if (!there) d = D + n;
     if (EVEN) {
         if (d >= D) v = u32x4_t{};
         return v;
+    }
+    if constexpr (!EVEN && sizeof(T) == 2) {
+        const uint32_t shift = D >= n && (odd ^ (min(d, D - n) & 1)) ? 16 : 0;
+        v = u32x4_t{__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift), __builtin_amdgcn_alignbit(v[3], v[2], shift),
+                    __builtin_amdgcn_alignbit(piece.behind, v[3], shift)};
     }
     if (D < n) {
         Vec<T, n> r = __builtin_bit_cast(Vec<T, n>, v);
@@ -183,6 +212,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     constexpr int kImage = KT * (SK + SV), NP = KT * P / 256, KB = KT / 32, DB = DP / 32;
     static_assert(KT * P % 256 == 0, "whole pieces per thread");
     __shared__ u32x4_t lds[2 * kImage];
+    __shared__ __attribute__((aligned(16))) float biases[2][KT];         // of the states of an image: 0, or -infinity for what no row sees
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     // neighbouring workgroups of an XCD take the row tiles of one image and head
     const unsigned all = gridDim.x, xcd = blockIdx.x & 7;
@@ -200,19 +230,25 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     for (int r = 0; r < RB; ++r) {
         const T *qrow;
         T *out;
+        Piece<EVEN, T> nq[P / 2];
         row_of<T>(p, image, head, min(row0 + 32 * r, p.rows - 1), qrow, mask[r], out);
 #pragma unroll
-        for (int t = 0; t < P / 2; ++t) q[r][t] = loaded<EVEN>(qrow, (2 * t + half) * n, D);
+        for (int t = 0; t < P / 2; ++t) nq[t] = loaded<EVEN>(qrow, (2 * t + half) * n, D);
 #pragma unroll
         for (int t = 0; t < P / 2; ++t) {
-            q[r][t] = placed<EVEN, T>(q[r][t], (2 * t + half) * n, D);
+            q[r][t] = placed(nq[t], (2 * t + half) * n, D, between_words(qrow));
 #pragma unroll
             for (int e = 0; e < 4; ++e) q[r][t][e] = (q[r][t][e] & p.keep) ^ p.flip;
         }
     }
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
+    // What hides states from every row, a mask by states or the end of them, is what the scores start from.  (A key there that is not finite
+    // makes the row's sums NaN, and the row is made again.)
+    const bool by_state = p.a.mask && p.a.mask_row == 0, by_pair = RB == 1 && p.a.mask && p.a.mask_row != 0;      // (wider blocks are not launched for these)
+    uint32_t seen = 0;
     // A thread's pieces are those at e % P of the states e / P of a tile, e = threadIdx.x + 256 i, the same in every tile.
-    u32x4_t nk[NP], nv[NP];
+    Piece<EVEN, T> nk[NP], nv[NP];
+    uint32_t odd = 0;           // bits 2 i and 2 i + 1: whether their rows begin between words
     long long step_k[NP], step_v[NP];
     const bool whole = EVEN && D == DP;
 #pragma unroll
@@ -221,33 +257,39 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         step_k[i] = e / P * p.a.ld_k + d, step_v[i] = e / P * p.a.ld_v + d;
     }
     auto fetch = [&](int at) {
+        if (threadIdx.x < KT) seen = at + (int)threadIdx.x < end && (!by_state || mask[0][at + threadIdx.x]);
         const T *const kt = k0 + at * p.a.ld_k, *const vt = v0 + at * p.a.ld_v;
         if (whole && at + KT <= end) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) nk[i] = __builtin_bit_cast(u32x4_t, load_n<n>(kt + step_k[i])), nv[i] = __builtin_bit_cast(u32x4_t, load_n<n>(vt + step_v[i]));
+            for (int i = 0; i < NP; ++i) nk[i].v = __builtin_bit_cast(u32x4_t, load_n<n>(kt + step_k[i])), nv[i].v = __builtin_bit_cast(u32x4_t, load_n<n>(vt + step_v[i]));
         } else {        // states behind the last are the last one again
+            odd = 0;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int e = threadIdx.x + i * 256, j = min(e / P, end - 1 - at), d = e % P * n;
-                nk[i] = loaded<EVEN>(kt + j * p.a.ld_k, d, D);
-                nv[i] = loaded<EVEN>(vt + j * p.a.ld_v, d, D);
+                const T *const kj = kt + j * p.a.ld_k, *const vj = vt + j * p.a.ld_v;
+                nk[i] = loaded<EVEN>(kj, d, D);
+                nv[i] = loaded<EVEN>(vj, d, D);
+                odd |= between_words(kj) << 2 * i | between_words(vj) << (2 * i + 1);
             }
         }
     };
-    auto store = [&](u32x4_t *to, int at) {
+    auto store = [&](int image_of, int at) {
+        u32x4_t *const to = lds + image_of * kImage;
+        if (threadIdx.x < KT) biases[image_of][threadIdx.x] = seen ? 0.f : -HUGE_VALF;
         if (!(whole && at + KT <= end)) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int e = threadIdx.x + i * 256, d = e % P * n;
-                nk[i] = placed<EVEN, T>(nk[i], d, D);
-                nv[i] = placed<EVEN, T>(nv[i], at + e / P < end ? d : D + n, D);
+                nk[i].v = placed(nk[i], d, D, odd >> 2 * i & 1);
+                nv[i].v = placed(nv[i], d, D, odd >> (2 * i + 1) & 1, at + e / P < end);
             }
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int e = threadIdx.x + i * 256, j = e / P, d = e % P;
-            to[j * SK + d] = nk[i];
-            to[KT * SK + j * SV + d] = nv[i];
+            to[j * SK + d] = nk[i].v;
+            to[KT * SK + j * SV + d] = nv[i].v;
         }
     };
     f32x16_t o[RB][DB] = {};
@@ -256,13 +298,25 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     for (int r = 0; r < RB; ++r) base[r] = -HUGE_VALF, total[r] = 0.f;
     if (first < end) {
         fetch(first);
-        store(lds, first);
+        store(0, first);
     }
     __syncthreads();
     int img = 0;
     for (int at = first; at < end; at += KT) {
         const bool more = at + KT < end;
         if (more) fetch(at + KT);
+        const bool hidden = by_state || at + KT > end;
+        uint32_t bytes[RB][KB * 4];
+        if (by_pair) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int i = 0; i < KB * 4; ++i) {
+                    const int j = at + i * 8 + half * 4;
+                    if (at + KT <= end) __builtin_memcpy(&bytes[r][i], mask[r] + j, 4);
+                    else bytes[r][i] = __builtin_bit_cast(uint32_t, load_some<4>(mask[r] + min(j, end - 1), end - min(j, end - 1)));
+                }
+        }
         const u32x4_t *const keys = lds + img * kImage, *const values = keys + KT * SK;
         f32x16_t s[RB][KB];
         u32x4_t pt[RB][kF32 ? 1 : KT / 16];         // their exponentials: bfloat16 pairs, or as they are
@@ -270,8 +324,17 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         float part[RB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
+            f32x16_t start = {};
+            if (hidden) {
 #pragma unroll
-            for (int r = 0; r < RB; ++r) s[r][kb] = f32x16_t{};
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4_t of = *(const f32x4_t *)&biases[img][kb * 32 + i * 2 + half * 4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) start[i + e] = of[e];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r) s[r][kb] = start;
 #pragma unroll
             for (int t = 0; t < P / 2; ++t) {
                 const u32x4_t k = keys[(kb * 32 + (lane & 31)) * SK + 2 * t + half];
@@ -287,19 +350,13 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
                 }
             }
         }
-        if (p.a.mask || at + KT > end) {
+        if (by_pair) {
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const int j = at + kb * 32 + i * 2 + half * 4;
-                        Vec<uint8_t, 4> m = {{1, 1, 1, 1}};
-                        if (p.a.mask && j < end) m = load_some<4>(mask[r] + j, end - j);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[r][kb][i + e] = j + e < end && m.v[e] ? s[r][kb][i + e] : -HUGE_VALF;
-                    }
+                    for (int i = 0; i < 16; ++i) s[r][kb][i] = bytes[r][kb * 4 + i / 4] >> i % 4 * 8 & 255 ? s[r][kb][i] : -HUGE_VALF;
         }
         // The exponents are taken against the base as it stands.  Only where there is none yet, or where a sum shows that scores have passed
         // it by far, is the tile's maximum looked for and are they taken again.
@@ -377,7 +434,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             }
         }
         img ^= 1;
-        if (more) store(lds + img * kImage, at + KT);
+        if (more) store(img, at + KT);
         __syncthreads();
     }
 #pragma unroll
@@ -464,22 +521,33 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
     T *out;
     row_of<T>(p, image, head, min(row, p.rows - 1), qrow, mask, out);
     u32x4_t q[P / 4];
+    Piece<EVEN, T> nq[P / 4];
 #pragma unroll
-    for (int t = 0; t < P / 4; ++t) q[t] = loaded<EVEN>(qrow, (4 * t + quarter) * n, D);
+    for (int t = 0; t < P / 4; ++t) nq[t] = loaded<EVEN>(qrow, (4 * t + quarter) * n, D);
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
-    u32x4_t nk[KB][P / 4], nv[NV];
+    Piece<EVEN, T> nk[KB][P / 4], nv[NV];
+    uint32_t odd_k = 0, odd_v = 0;      // bit i: whether the i-th row begins between words
     auto fetch_keys = [&](int at) {
+        odd_k = 0;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int kb = 0; kb < KB; ++kb) {
+            const T *const kj = k0 + min(at + kb * 16 + l16, end - 1) * p.a.ld_k;
 #pragma unroll
-            for (int t = 0; t < P / 4; ++t) nk[kb][t] = loaded<EVEN>(k0 + min(at + kb * 16 + l16, end - 1) * p.a.ld_k, (4 * t + quarter) * n, D);
+            for (int t = 0; t < P / 4; ++t) nk[kb][t] = loaded<EVEN>(kj, (4 * t + quarter) * n, D);
+            odd_k |= between_words(kj) << kb;
+        }
     };
     // bf16: piece e % P of state e / P, e = lane + 64 i; fp32: values 64 (i / 4) + 4 (lane % 16) on of state 4 (lane / 16) + i % 4
     auto value_state = [&](int i) { return kF32 ? 4 * quarter + i % 4 : (lane + 64 * i) / P; };
     auto value_at = [&](int i) { return kF32 ? i / 4 * 64 + 4 * l16 : (lane + 64 * i) % P * n; };
     auto fetch_values = [&](int at) {
+        odd_v = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) nv[i] = loaded<EVEN>(v0 + min(at + value_state(i), end - 1) * p.a.ld_v, value_at(i), D);
+        for (int i = 0; i < NV; ++i) {
+            const T *const vj = v0 + min(at + value_state(i), end - 1) * p.a.ld_v;
+            nv[i] = loaded<EVEN>(vj, value_at(i), D);
+            odd_v |= between_words(vj) << i;
+        }
     };
     f32x4_t o[DB] = {};
     float base = -HUGE_VALF, total = 0.f;
@@ -490,7 +558,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
     }
 #pragma unroll
     for (int t = 0; t < P / 4; ++t) {
-        q[t] = placed<EVEN, T>(q[t], (4 * t + quarter) * n, D);
+        q[t] = placed(nq[t], (4 * t + quarter) * n, D, between_words(qrow));
 #pragma unroll
         for (int e = 0; e < 4; ++e) q[t][e] = (q[t][e] & p.keep) ^ p.flip;
     }
@@ -503,7 +571,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
             s[kb] = f32x4_t{};
 #pragma unroll
             for (int t = 0; t < P / 4; ++t) {
-                const u32x4_t k = placed<EVEN, T>(nk[kb][t], (4 * t + quarter) * n, D);
+                const u32x4_t k = placed(nk[kb][t], (4 * t + quarter) * n, D, odd_k >> kb & 1);
                 if constexpr (kF32) {
                     const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[t]);
 #pragma unroll
@@ -547,7 +615,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
             }
         u32x4_t v[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = placed<EVEN, T>(nv[i], at + value_state(i) < end ? value_at(i) : D + n, D);
+        for (int i = 0; i < NV; ++i) v[i] = placed(nv[i], value_at(i), D, odd_v >> i & 1, at + value_state(i) < end);
         if constexpr (kF32) {
             if (more) fetch_values(at + NW * KC);
 #pragma unroll
@@ -828,6 +896,10 @@ int cross_attention(const CrossArgs &a)
     p.c = a.scale == 0 ? 1.f : std::fabs(a.scale) * kLog2e;
     p.keep = a.scale == 0 ? 0 : 0xffffffffu;
     p.flip = a.scale < 0 ? (a.dtype == SQ_F32 ? 0x80000000u : 0x80008000u) : 0;
+    if (plan.block == 256 && a.mask && a.mask_row) {       // the wider blocks have no registers left for a mask by rows
+        plan.block = 128, p.tiles = (plan.rows - 1) / 128 + 1;
+        if (!one_launch((double)a.N * a.kv_heads * p.tiles * p.shares, 256)) return SQ_ERR_UNSUPPORTED;
+    }
     p.part_ld = part_row(a.D);
     p.part_o = (float *)a.workspace;
     p.part_ml = (float2 *)((char *)a.workspace + align_up((size_t)p.shares * a.N * a.kv_heads * p.rows * p.part_ld * sizeof(float), 256));

@@ -424,26 +424,28 @@ double blocks_of(int rows, int Cout, int R, int C) { return ((rows - 1) / R + 1.
 
 // How a product is made: by wavefronts in blocks of 16 x 16 (rows not packed before as they are, where they are few), or by a tiling.
 // Rows given as they are: packing them in every block of 16 layers again costs 0.17 us for 256 blocks and chunk, a launch that packs them
-// first 2.3 us on the GPU and 5 on the host (us, in the product / before it: 1 x 512 x 1000 fp32 3.6 / 5.4, 8 x 4096 x 4096 bf16 7.2 / 7.4).
+// first 2.3 us on the GPU and 5 on the host, counted as 4 (us, in the product / before it: 1 x 512 x 1000 fp32 3.6 / 5.4, 8 x 4096 x 4096
+// bf16 7.2 / 7.4); up to 16 chunks a block, so that no block packs for longer than that launch takes.  Packed rows take the same form, so that they give the same bits.
 // What has more threads than a launch takes, or rows too long for the tiles' 32-bit offsets, is passed over.
 enum { kWaves = -1, kNone = -2 };
-constexpr double kRawChunks = 4096;
+constexpr double kRawChunks = 16, kPackFirst = 4.0;
 struct Plan { int which; bool raw; };
-Plan plan_of(int rows, int Cin, int Cout, bool packed)
+Plan plan_of(int rows, int Cin, int Cout)
 {
     const int chunks = chunks_of(Cin);
     Plan plan{kNone, false};
     double us = HUGE_VAL;
     const double blocks = blocks_of(rows, Cout, 16, 16);
     if (one_launch(blocks, 64 * std::min(chunks, 16))) {
-        plan.which = kWaves, plan.raw = !packed && std::max(blocks, 256.0) * chunks <= kRawChunks;
-        us = std::max(0.5, 0.22 * chunks * std::max(1.0, blocks / 256)) + 0.3;
+        const double some = chunks * std::max(1.0, blocks / 256);
+        plan.which = kWaves, plan.raw = some <= kRawChunks;
+        us = std::max(0.5, 0.22 * some) + 0.3 + (plan.raw ? 0.17 * some : kPackFirst);
     }
     if (rows <= 16 || chunks >= 1 << 15) return plan;
     for (int i = 0; i < 4; ++i) {
         const Tiling &t = kTilings[i];
         if (!one_launch(blocks_of(rows, Cout, t.BM, t.BN), t.threads)) continue;
-        const double tu = tiling_us(t, rows, Cout, chunks);
+        const double tu = tiling_us(t, rows, Cout, chunks) + kPackFirst;
         if (tu < us) us = tu, plan = Plan{i, false};
     }
     return plan;
@@ -494,7 +496,7 @@ int mxfp4_unpack(const void *in, void *out, int out_dtype, int rows, int Cin, lo
 
 size_t mxfp4_linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype)
 {
-    const Plan plan = plan_of(rows, Cin, Cout, in_dtype == SQ_MXFP4);
+    const Plan plan = plan_of(rows, Cin, Cout);
     return in_dtype == SQ_MXFP4 || plan.raw ? 0 : mxfp4_packed_bytes(rows, Cin);
 }
 
@@ -504,9 +506,9 @@ int mxfp4_linear(const LinearArgs &p)
     a.p = p;
     a.chunks = a.share = chunks_of(p.Cin);
     a.w = packed_at(p.w, p.Cout, p.Cin);
-    const Plan plan = plan_of(p.rows, p.Cin, p.Cout, p.in_dtype == SQ_MXFP4);
+    const Plan plan = plan_of(p.rows, p.Cin, p.Cout);
     if (plan.which == kNone) return SQ_ERR_UNSUPPORTED;
-    if (plan.raw) return p.in_dtype == SQ_F32 ? raw_rows<float>(a) : raw_rows<bf16_t>(a);
+    if (plan.raw && p.in_dtype != SQ_MXFP4) return p.in_dtype == SQ_F32 ? raw_rows<float>(a) : raw_rows<bf16_t>(a);
     const void *x = p.in;
     if (p.in_dtype != SQ_MXFP4) {
         if (const int rc = mxfp4_pack(p.in, p.in_dtype, p.workspace, p.rows, p.Cin, p.ld_in)) return rc;
