@@ -188,28 +188,29 @@ template <typename T> __device__ __forceinline__ void put4(const CrossParams &p,
 // LDS.  Scores are formed transposed, states x rows, so that a lane holds scores of one row alone (lane % 32): its maximum and sum are sums
 // within the lane and over the two halves.  The scores' places in the accumulators are, as they are, the second operand of the
 // product with the transposed values: lane half h has states 8 i + 4 h to 8 i + 4 h + 3, and the values' lanes take the same ones.
-template <typename T> struct Tile;
-template <> struct Tile<bf16_t> {
-    static constexpr int KT = 64;
-    // 16-byte pieces from one state to the next: keys in odd steps (a column of pieces covers all banks), values in steps of 4 modulo 8
-    // (the four states of a transposed read lie apart)
-    static constexpr int key_step(int DP) { return DP / 8 + 1; }
-    static constexpr int value_step(int DP) { return DP / 8 % 8 == 4 ? DP / 8 : DP / 8 + 4; }
-};
-template <> struct Tile<float> {
-    static constexpr int KT = 32;
-    static constexpr int key_step(int DP) { return DP / 4 + 1; }
-    static constexpr int value_step(int DP) { return DP / 4; }
+// fp32 heads of up to 128 run on the bfloat16 instructions, every operand as the sum of three bfloat16 values (x = h + m + l, exact; of the nine
+// products the six down to 2^-16 of the largest, the smallest first), each a plane of its own in LDS or registers; wider ones, whose planes
+// LDS has no room for, on the fp32 instructions.
+template <typename T, int DP> struct Tile {
+    static constexpr bool kF32 = sizeof(T) == 4, kSplit = kF32 && DP <= 128;
+    static constexpr int KT = kF32 ? 32 : 64, PL = kSplit ? 3 : 1, P = kF32 && !kSplit ? DP / 4 : DP / 8;     // states, planes, 16-byte pieces of a row in LDS
+    // Pieces from one state to the next: keys in odd steps (a column of pieces covers all banks), values in steps of 4 modulo 8 (the four
+    // states of a transposed read lie apart; fp32 ones are read as they lie).
+    // Workgroups to a compute unit, with 32 or 64 rows to a wavefront.
+    static constexpr int kFit[2] = {DP <= 32 || (DP <= 64 && !kF32) ? 3 : DP <= 96 || (DP <= 128 && !kF32) ? 2 : 1, 2};
+    static constexpr int SK = P + 1, SV = kF32 && !kSplit ? P : P % 8 == 4 ? P : P + 4;
 };
 
 // How far scores may pass what the exponents are taken against: in base two, and a lane's sum over a tile.
 constexpr float kHeadroom = 8.f, kFar = 8192.f;
 
-template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(256, RB == 2 ? (DP <= 64 ? 2 : 1) : DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void cross_tile_kernel(CrossParams p)
+template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(256, (Tile<T, DP>::kFit[RB - 1])) void cross_tile_kernel(CrossParams p)
 {
-    constexpr bool kF32 = sizeof(T) == 4;
-    constexpr int KT = Tile<T>::KT, n = 16 / (int)sizeof(T), P = DP / n, SK = Tile<T>::key_step(DP), SV = Tile<T>::value_step(DP);
-    constexpr int kImage = KT * (SK + SV), NP = KT * P / 256, KB = KT / 32, DB = DP / 32;
+    using Form = Tile<T, DP>;
+    constexpr bool kSplit = Form::kSplit, kPlain = Form::kF32 && !kSplit;
+    // P: pieces of a row in memory, PT: in LDS
+    constexpr int KT = Form::KT, PL = Form::PL, PT = Form::P, SK = Form::SK, SV = Form::SV, n = 16 / (int)sizeof(T), P = DP / n;
+    constexpr int kValues = PL * KT * SK, kImage = kValues + PL * KT * SV, NP = KT * P / 256, KB = KT / 32, DB = DP / 32;
     static_assert(KT * P % 256 == 0, "whole pieces per thread");
     __shared__ u32x4_t lds[2 * kImage];
     __shared__ __attribute__((aligned(16))) float biases[2][KT];         // of the states of an image: 0, or -infinity for what no row sees
@@ -225,20 +226,33 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
 
     const int row0 = tile * (128 * RB) + wave * (32 * RB) + (lane & 31);
     const uint8_t *mask[RB];
-    u32x4_t q[RB][P / 2];
+    u32x4_t q[RB][PL][PT / 2];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const T *qrow;
         T *out;
-        Piece<EVEN, T> nq[P / 2];
         row_of<T>(p, image, head, min(row0 + 32 * r, p.rows - 1), qrow, mask[r], out);
+        // pieces of a lane: 2 t + half, or for planes the two that make up that one of bfloat16 values
+        auto value = [&](int i) { return kSplit ? (2 * (i / 2) + half) * 8 + i % 2 * 4 : (2 * i + half) * n; };
+        Piece<EVEN, T> nq[P / 2];
 #pragma unroll
-        for (int t = 0; t < P / 2; ++t) nq[t] = loaded<EVEN>(qrow, (2 * t + half) * n, D);
+        for (int i = 0; i < P / 2; ++i) nq[i] = loaded<EVEN>(qrow, value(i), D);
 #pragma unroll
-        for (int t = 0; t < P / 2; ++t) {
-            q[r][t] = placed(nq[t], (2 * t + half) * n, D, between_words(qrow));
+        for (int i = 0; i < P / 2; ++i) {
+            u32x4_t v = placed(nq[i], value(i), D, between_words(qrow));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[r][t][e] = (q[r][t][e] & p.keep) ^ p.flip;
+            for (int e = 0; e < 4; ++e) v[e] = (v[e] & p.keep) ^ p.flip;
+            if constexpr (kSplit) {
+                const f32x4_t f = __builtin_bit_cast(f32x4_t, v);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t h, m, l;
+                    split_pair(f[2 * e], f[2 * e + 1], h, m, l);
+                    q[r][0][i / 2][i % 2 * 2 + e] = h, q[r][1][i / 2][i % 2 * 2 + e] = m, q[r][2][i / 2][i % 2 * 2 + e] = l;
+                }
+            } else {
+                q[r][0][i] = v;
+            }
         }
     }
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
@@ -288,8 +302,20 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int e = threadIdx.x + i * 256, j = e / P, d = e % P;
-            to[j * SK + d] = nk[i].v;
-            to[KT * SK + j * SV + d] = nv[i].v;
+            if constexpr (kSplit) {
+                auto planes = [&](u32x4_t v, uint2 *at, int plane) {
+                    const f32x4_t f = __builtin_bit_cast(f32x4_t, v);
+                    uint2 h, m, l;
+                    split_pair(f[0], f[1], h.x, m.x, l.x);
+                    split_pair(f[2], f[3], h.y, m.y, l.y);
+                    at[0] = h, at[2 * plane] = m, at[4 * plane] = l;
+                };
+                planes(nk[i].v, (uint2 *)(to + j * SK) + d, KT * SK);
+                planes(nv[i].v, (uint2 *)(to + kValues + j * SV) + d, KT * SV);
+            } else {
+                to[j * SK + d] = nk[i].v;
+                to[kValues + j * SV + d] = nv[i].v;
+            }
         }
     };
     f32x16_t o[RB][DB] = {};
@@ -317,10 +343,11 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
                     else bytes[r][i] = __builtin_bit_cast(uint32_t, load_some<4>(mask[r] + min(j, end - 1), end - min(j, end - 1)));
                 }
         }
-        const u32x4_t *const keys = lds + img * kImage, *const values = keys + KT * SK;
+        const u32x4_t *const keys = lds + img * kImage, *const values = keys + kValues;
+        __builtin_amdgcn_s_setprio(1);
         f32x16_t s[RB][KB];
-        u32x4_t pt[RB][kF32 ? 1 : KT / 16];         // their exponentials: bfloat16 pairs, or as they are
-        f32x16_t pf[kF32 ? RB : 1];
+        u32x4_t pt[RB][PL][kPlain ? 1 : KT / 16];         // their exponentials: bfloat16 pairs, or as they are
+        f32x16_t pf[kPlain ? RB : 1];
         float part[RB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
@@ -336,16 +363,22 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
 #pragma unroll
             for (int r = 0; r < RB; ++r) s[r][kb] = start;
 #pragma unroll
-            for (int t = 0; t < P / 2; ++t) {
-                const u32x4_t k = keys[(kb * 32 + (lane & 31)) * SK + 2 * t + half];
+            for (int t = 0; t < PT / 2; ++t) {
+                u32x4_t k[PL];
+#pragma unroll
+                for (int a = 0; a < PL; ++a) k[a] = keys[(a * KT + kb * 32 + (lane & 31)) * SK + 2 * t + half];
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
-                    if constexpr (kF32) {
-                        const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[r][t]);
+                    if constexpr (kPlain) {
+                        const f32x4_t kf = __builtin_bit_cast(f32x4_t, k[0]), qf = __builtin_bit_cast(f32x4_t, q[r][0][t]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[r][kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[e], s[r][kb], 0, 0, 0);
                     } else {
-                        s[r][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[r][t]), s[r][kb], 0, 0, 0);
+#pragma unroll
+                        for (int sum = PL - 1; sum >= 0; --sum)
+#pragma unroll
+                            for (int a = 0; a <= sum; ++a)
+                                s[r][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[a]), __builtin_bit_cast(bf16x8, q[r][sum - a][t]), s[r][kb], 0, 0, 0);
                     }
                 }
             }
@@ -360,13 +393,15 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         }
         // The exponents are taken against the base as it stands.  Only where there is none yet, or where a sum shows that scores have passed
         // it by far, is the tile's maximum looked for and are they taken again.
+        __builtin_amdgcn_s_setprio(0);
         auto exponents = [&](int r) {
             const float off = base[r] == -HUGE_VALF ? 0.f : base[r];
             part[r] = 0.f;
-            if constexpr (kF32) {
+            auto p_of = [&](int i) { return __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i / 16][i % 16], p.c, -off)); };
+            if constexpr (kPlain) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    pf[r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][0][i], p.c, -off));
+                    pf[r][i] = p_of(i);
                     part[r] += pf[r][i];
                 }
             } else {
@@ -374,9 +409,16 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
                 for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int i = t % 2 * 8 + 2 * e;
-                        pt[r][t][e] = bf16_two(__builtin_amdgcn_exp2f(__builtin_fmaf(s[r][t / 2][i], p.c, -off)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][t / 2][i + 1], p.c, -off)));
-                        part[r] = add_two(pt[r][t][e], part[r]);
+                        const float a = p_of(t * 8 + 2 * e), b = p_of(t * 8 + 2 * e + 1);
+                        if constexpr (kSplit) {
+                            uint32_t h, m, l;
+                            split_pair(a, b, h, m, l);
+                            pt[r][0][t][e] = h, pt[r][1][t][e] = m, pt[r][2][t][e] = l;
+                            part[r] += a + b;
+                        } else {
+                            pt[r][0][t][e] = bf16_two(a, b);
+                            part[r] = add_two(pt[r][0][t][e], part[r]);
+                        }
                     }
             }
         };
@@ -407,7 +449,8 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         }
 #pragma unroll
         for (int r = 0; r < RB; ++r) total[r] += part[r];
-        if constexpr (kF32) {
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (kPlain) {
             const float *const vf = (const float *)values;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -423,16 +466,26 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             for (int t = 0; t < KT / 16; ++t) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    // sixteen lanes read four states of sixteen neighbouring values, a lane four of them, and get a column each
-                    const char *const from = (const char *)(values + (t * 16 + half * 4 + (lane & 15) / 4) * SV) + d * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-                    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(from + 8 * SV * 16));
-                    const auto vt = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    bf16x8 vt[PL];
+#pragma unroll
+                    for (int a = 0; a < PL; ++a) {
+                        // sixteen lanes read four states of sixteen neighbouring values, a lane four of them, and get a column each
+                        const char *const from = (const char *)(values + (a * KT + t * 16 + half * 4 + (lane & 15) / 4) * SV) + d * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+                        const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(from + 8 * SV * 16));
+                        const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        vt[a] = __builtin_bit_cast(bf16x8, both);
+                    }
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
-                        o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, pt[r][t]), o[r][d], 0, 0, 0);
+#pragma unroll
+                        for (int sum = PL - 1; sum >= 0; --sum)
+#pragma unroll
+                            for (int a = 0; a <= sum; ++a)
+                                o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[a], __builtin_bit_cast(bf16x8, pt[r][sum - a][t]), o[r][d], 0, 0, 0);
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         img ^= 1;
         if (more) store(img, at + KT);
         __syncthreads();
@@ -502,7 +555,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
 {
     constexpr bool kF32 = sizeof(T) == 4;
     constexpr int KC = Chunk<T>::KC, n = 16 / (int)sizeof(T), P = DP / n, KB = KC / 16;
-    constexpr int SV = Tile<T>::value_step(DP);     // bf16: pieces from one state to the next in LDS
+    constexpr int SV = P % 8 == 4 ? P : P + 4;      // bf16: pieces from one state to the next in LDS
     constexpr int NV = kF32 ? 4 * ((DP + 63) / 64) : KC * P / 64, DB = kF32 ? (DP + 63) / 64 * 4 : DP / 16;
     constexpr int kRow = DP + 4;                                    // of a wavefront's sums
     constexpr int kArea = kF32 ? 0 : KC * SV, kRoom = kArea > 4 * kRow ? NW * kArea : NW * 4 * kRow;        // 16 bytes: of a wavefront's values; in all
@@ -526,9 +579,17 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
     for (int t = 0; t < P / 4; ++t) nq[t] = loaded<EVEN>(qrow, (4 * t + quarter) * n, D);
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
     Piece<EVEN, T> nk[KB][P / 4], nv[NV];
+    uint32_t bytes[KB];                 // of the mask
     uint32_t odd_k = 0, odd_v = 0;      // bit i: whether the i-th row begins between words
     auto fetch_keys = [&](int at) {
         odd_k = 0;
+        if (mask)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const int j = at + kb * 16 + quarter * 4, there = min(j, end - 1);
+                if (at + KC <= end) __builtin_memcpy(&bytes[kb], mask + j, 4);
+                else bytes[kb] = __builtin_bit_cast(uint32_t, load_some<4>(mask + there, end - there));
+            }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             const T *const kj = k0 + min(at + kb * 16 + l16, end - 1) * p.a.ld_k;
@@ -581,17 +642,14 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
                 }
             }
         }
-        if (more) fetch_keys(at + NW * KC);
         if (mask || at + KC > end) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const int j = at + kb * 16 + quarter * 4;
-                Vec<uint8_t, 4> m = {{1, 1, 1, 1}};
-                if (mask && j < end) m = load_some<4>(mask + j, end - j);
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[kb][e] = j + e < end && m.v[e] ? s[kb][e] : -HUGE_VALF;
-            }
+                for (int e = 0; e < 4; ++e)
+                    s[kb][e] = at + kb * 16 + quarter * 4 + e < end && (!mask || (bytes[kb] >> e * 8 & 255)) ? s[kb][e] : -HUGE_VALF;
         }
+        if (more) fetch_keys(at + NW * KC);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) settled(s[kb]);
         float top = max3(s[0][0], s[0][1], s[0][2]);

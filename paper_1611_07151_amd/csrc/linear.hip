@@ -352,22 +352,6 @@ template <> struct Image<float> {
     static __device__ __forceinline__ int at(int r, int q) { return (r >> 1) * 8 + (((r & 1) * 4 + q) ^ ((r >> 2) & 3)); }
 };
 
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
-{
-    uint32_t v;     // written out: the compiler would round `a` a second time where it is wanted as fp32 again
-    __asm__("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(v) : "v"(a), "v"(b));
-    return v;
-}
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l)
-{
-    const uint32_t ua = __builtin_bit_cast(uint32_t, a), ub = __builtin_bit_cast(uint32_t, b);
-    h = __builtin_amdgcn_perm(ub, ua, 0x07060302);
-    a -= __builtin_bit_cast(float, ua & 0xffff0000u);
-    b -= __builtin_bit_cast(float, ub & 0xffff0000u);
-    m = bf16_pair(a, b);
-    l = bf16_pair(a - __builtin_bit_cast(float, m << 16), b - __builtin_bit_cast(float, m & 0xffff0000u));
-}
-
 template <typename TI, typename TO, int BM, int BN, int WR, int WC, int PF, int KS>
 __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs p, int tiles_r, int tiles_j)
 {

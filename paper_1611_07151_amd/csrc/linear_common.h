@@ -90,6 +90,23 @@ template <typename TO, int n> __device__ __forceinline__ void finish(const Linea
     put<TO, n>(p, (TO *)p.out + r * p.ld_out + j, have, v, b, res);
 }
 
+// Two fp32 values as the sums of three pairs of bfloat16 values: h the upper halves, m = round(x - h), l = x - h - m.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
+{
+    uint32_t v;     // written out: the compiler would round `a` a second time where it is wanted as fp32 again
+    __asm__("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(v) : "v"(a), "v"(b));
+    return v;
+}
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l)
+{
+    const uint32_t ua = __builtin_bit_cast(uint32_t, a), ub = __builtin_bit_cast(uint32_t, b);
+    h = __builtin_amdgcn_perm(ub, ua, 0x07060302);
+    a -= __builtin_bit_cast(float, ua & 0xffff0000u);
+    b -= __builtin_bit_cast(float, ub & 0xffff0000u);
+    m = bf16_pair(a, b);
+    l = bf16_pair(a - __builtin_bit_cast(float, m << 16), b - __builtin_bit_cast(float, m & 0xffff0000u));
+}
+
 // Rows and layers of the b-th tile: neighbouring workgroups of one XCD take a band of eight row tiles, row tile fastest,
 // so that what one of its L2 holds is eight row tiles and a few layer tiles.
 __device__ __forceinline__ void tile_at(int b, int tiles, int tiles_r, int tiles_j, int &tr, int &tj)
