@@ -318,7 +318,16 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             }
         }
     };
-    f32x16_t o[RB][DB] = {};
+    // (Zeros that the compiler does not know: a constant would be the one that the scores start from too, and keep that one in registers.)
+    float zero = 0.f;
+    __asm__ volatile("" : "+v"(zero));
+    f32x16_t o[RB][DB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[r][d][i] = zero;
     float base[RB], total[RB];      // what the exponents are taken against, in base two, and their sum
 #pragma unroll
     for (int r = 0; r < RB; ++r) base[r] = -HUGE_VALF, total[r] = 0.f;
@@ -328,12 +337,13 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     }
     __syncthreads();
     int img = 0;
-    for (int at = first; at < end; at += KT) {
+    // some_hidden: whether some states may be; where that is a constant, the others' way has neither the tests nor the registers for it
+    auto tile_of = [&](int at, auto some_hidden) __attribute__((always_inline)) {
+        const bool hidden = some_hidden;
         const bool more = at + KT < end;
         if (more) fetch(at + KT);
-        const bool hidden = by_state || at + KT > end;
         uint32_t bytes[RB][KB * 4];
-        if (by_pair) {
+        if (hidden && by_pair) {
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
@@ -383,7 +393,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
                 }
             }
         }
-        if (by_pair) {
+        if (hidden && by_pair) {
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
@@ -489,6 +499,14 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         img ^= 1;
         if (more) store(img, at + KT);
         __syncthreads();
+    };
+    int at = first;
+    if constexpr (sizeof(T) == 2 && DP <= 128) {
+        if (!p.a.mask)
+            for (; at + KT <= end; at += KT) tile_of(at, std::false_type{});
+        for (; at < end; at += KT) tile_of(at, std::true_type{});
+    } else {        // (in wider heads there are no registers for two ways)
+        for (; at < end; at += KT) tile_of(at, p.a.mask || at + KT > end);
     }
 #pragma unroll
     for (int r = 0; r < RB; ++r) {

@@ -40,11 +40,11 @@ def reference(q, k, v, heads, kv_heads, scale, seen, dt):
     q = q.double().reshape(n, lq, heads, d).permute(0, 2, 1, 3)
     k, v = (t.double().reshape(n, lk, kv_heads, d).permute(0, 2, 1, 3).repeat_interleave(group, 1) for t in (k, v))
     m = seen[:, None]
-    zero = torch.zeros((), dtype=torch.float64)
+    zero = torch.zeros((), dtype=torch.float64, device=q.device)
     s = torch.where(m, scale * (q @ k.transpose(2, 3)), zero - math.inf)
     big = torch.where(m, abs(scale) * (q.abs() @ k.abs().transpose(2, 3)), zero)
-    big = big.amax(3, keepdim=True) if lk else torch.zeros(n, heads, lq, 1, dtype=torch.float64)
-    top = s.amax(3, keepdim=True) if lk else torch.full((n, heads, lq, 1), -math.inf, dtype=torch.float64)
+    big = big.amax(3, keepdim=True) if lk else torch.zeros(n, heads, lq, 1, dtype=torch.float64, device=q.device)
+    top = s.amax(3, keepdim=True) if lk else torch.full((n, heads, lq, 1), -math.inf, dtype=torch.float64, device=q.device)
     p = torch.exp(s - torch.where(top == -math.inf, zero, top))
     total = p.sum(3, keepdim=True)
     safe = torch.where(total == 0, zero + 1, total)
@@ -252,6 +252,65 @@ def test_graph_streams_and_workspaces(sq):
                 results.append((sq.sq_cross_attention_forward(*c[:5]), c[7]))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in results)
+
+
+@pytest.mark.parametrize("n,lq,lk,heads,kv,d,dt,kind", [(8, 1025, 200, 8, 8, 64, BF16, "none"), (8, 1025, 200, 8, 8, 64, BF16, "states"), (8, 1025, 200, 8, 8, 64, BF16, "pairs"),
+                                                       (8, 1030, 130, 8, 4, 30, BF16, "pairs"), (8, 1030, 130, 8, 4, 30, BF16, "none"), (4, 600, 300, 8, 8, 96, F32, "states"),
+                                                       (4, 700, 200, 8, 8, 128, BF16, "lengths")])
+def test_many_rows(sq, n, lq, lk, heads, kv, d, dt, kind):
+    """Enough rows for the widest blocks; the reference in 64 bits on the GPU."""
+    print(n, lq, lk, heads, kv, d, dt, kind, flush=True)
+    q, k, v = inputs(n, lq, lk, heads, kv, d, dt, 21)
+    seen, mask, lengths = everything(n, lq, lk), None, None
+    if kind == "lengths":
+        lengths = torch.tensor([lk, 0, 65, 1], dtype=torch.int32)
+        seen = (torch.arange(lk) < lengths[:, None])[:, None].expand(n, lq, lk)
+    elif kind == "states":
+        mask = torch.rand((n, lk), generator=gen(22)) < 0.5
+        mask[1] = False
+        seen = mask[:, None].expand(n, lq, lk)
+    elif kind == "pairs":
+        mask = torch.rand((n, lq, lk), generator=gen(22)) < 0.5
+        mask[:, ::7] = False
+        seen = mask
+    cuda = lambda t: None if t is None else t.cuda()
+    ref, bound = reference_on_gpu(q, k, v, heads, kv, d ** -0.5, seen, dt)
+    got = sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads, kv, mask=cuda(mask), lengths=cuda(lengths))
+    check(got, ref, bound, kind)
+    assert torch.equal(got, sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads, kv, mask=cuda(mask), lengths=cuda(lengths)))
+
+
+def reference_on_gpu(q, k, v, heads, kv_heads, scale, seen, dt):
+    parts = [reference(*(t[i:i + 1].cuda() for t in (q, k, v)), heads, kv_heads, scale, seen[i:i + 1].cuda(), dt) for i in range(q.shape[0])]
+    return torch.cat([r.cpu() for r, _ in parts]), torch.cat([b.cpu() for _, b in parts])
+
+
+@pytest.mark.parametrize("lq", (1, 300))
+@pytest.mark.parametrize("size", (1e30, 1e18, 1e-15))
+def test_fp32_magnitudes(sq, lq, size):
+    """fp32 values as large and small as they come, with scores that stay ordinary: every value keeps its own accuracy."""
+    n, lk, heads, d = 1, 170, 2, 64
+    q, k, v = inputs(n, lq, lk, heads, heads, d, F32, 23)
+    q, k, v = q * size, k / size, v * size
+    ref, bound = reference(q, k, v, heads, heads, d ** -0.5, everything(n, lq, lk), F32)
+    check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads), ref, bound, size)
+
+
+@pytest.mark.parametrize("dt", (F32, BF16))
+@pytest.mark.parametrize("lq", (1, 200))
+def test_scores_that_jump(sq, lq, dt):
+    """A state far above all before it, in every place of a tile, and one that only some queries see."""
+    n, lk, d = 1, 300, 64
+    for at in (0, 1, 31, 32, 63, 64, 127, 199, 299):
+        q, k, v = inputs(n, lq, lk, 1, 1, d, dt, 24)
+        q[:] = q.abs() + 0.5
+        k[:, at] = 40.0
+        mask = torch.ones((n, lq, lk), dtype=torch.bool)
+        mask[:, 1::2, at] = False
+        ref, bound = reference(q, k, v, 1, 1, 1.0, mask, dt)
+        check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), 1, scale=1.0, mask=mask.cuda()), ref, bound, at)
+        ref, bound = reference(q, k, v, 1, 1, 1.0, everything(n, lq, lk), dt)
+        check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), 1, scale=1.0), ref, bound, at)
 
 
 @pytest.mark.parametrize("lq", (1, 90))
