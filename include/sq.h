@@ -632,10 +632,12 @@ int sq_mxfp4_linear_forward(const void *in, const void *packed_w, const float *b
  *   lengths [N] int32 or NULL: image n has only its first lengths[n] states (less than 0: none; more than Lk: all).
  *   mask or NULL: bytes; state j is hidden from query i of image n where mask[n * mask_image + i * mask_row + j] is 0.
  *     A step of 0 shares a mask between images or queries; steps must not be negative (SQ_ERR_SHAPE).
- *   Scores, their maxima and sums are fp32, and so are the products for SQ_F32; for SQ_BF16 each p is rounded to bfloat16 before it
- *   multiplies v.  Hidden states have no influence on a result, whatever they hold; states behind a length are not read.  An
- *   infinity or NaN in a state that a query sees may make the results of that query and the heads that share the
- *   state's head NaN, and no others.
+ *   Scores, their maxima and sums are fp32, and so are the products for SQ_F32 (heads of up to 128 may run on the bfloat16 matrix
+ *   instructions as in sq_linear_forward, with the same error but for operands below 2^-110 in magnitude); for SQ_BF16 each p is
+ *   rounded to bfloat16 before it multiplies v, and may be before it is added up.
+ *   Hidden states have no influence on a result, whatever they hold, and states behind a length are not read.  (An infinity or NaN in
+ *   a hidden state costs time: the rows that it touches are made again one by one.)  An infinity or NaN in a state that a query sees
+ *   may make the results of that query, in the heads that share the state's head, NaN, and no others.
  *   workspace: sq_cross_attention_workspace_bytes() bytes of device scratch, 256-byte aligned (else SQ_ERR_WORKSPACE; 0 = none is
  *     needed, workspace may be NULL).  Contents on return are unspecified; two calls in flight at once need two.
  *   The same call gives the same bits every time.  Lk and Lq * heads / kv_heads may be 2^30 at most; what is more, or has no

@@ -962,9 +962,7 @@ def _matrix(x, name):
 
 def sq_mxfp4_pack(x, out=None):
     """Rows x [..., Cin] (float32 or bfloat16) -> packed uint8 tensor of sq_mxfp4_packed_bytes(rows, Cin) bytes: blocks of 32 values
-    with a power of two in common and 4 bits a value.  Kernels [Cout][Cin][1][1] are taken as [Cout][Cin]."""
-    if x.dim() == 4 and x.shape[2:] == (1, 1):
-        x = x[:, :, 0, 0]
+    with a power of two in common and 4 bits a value."""
     index, rows, Cin, ld = _matrix(x, "x")
     if not rows:
         _check(-2, "sq_mxfp4_pack")

@@ -1468,15 +1468,13 @@ int sq_mxfp4_linear_forward(const void *in, const void *packed_w, const float *b
     if ((!packed && !aligned_to(in, in_dtype)) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype) || !aligned_to(b, SQ_F32))
         return SQ_ERR_UNSUPPORTED;
     if (((uintptr_t)packed_w & 255) || (packed && ((uintptr_t)in & 255))) return SQ_ERR_WORKSPACE;
-    const size_t need = mxfp4_linear_workspace_bytes(rows, Cin, Cout, in_dtype);
-    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
     LinearArgs a{};
     a.in = in; a.w = packed_w; a.b = b; a.residual = residual; a.out = out;
     a.in_dtype = in_dtype; a.out_dtype = out_dtype;
     a.rows = rows; a.Cin = Cin; a.Cout = Cout; a.act = act;
     a.ld_in = ld_in; a.ld_res = ld_res; a.ld_out = ld_out;
     a.workspace = workspace;
-    return mxfp4_linear(a);
+    return mxfp4_linear(a, workspace_bytes);
 }
 
 size_t sq_cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, sq_dtype dtype)
@@ -1497,15 +1495,13 @@ int sq_cross_attention_forward(const void *q, const void *k, const void *v, void
     if (!known_dtype(dtype) || D > 256) return SQ_ERR_UNSUPPORTED;
     if (!aligned_to(q, dtype) || !aligned_to(out, dtype) || (Lk > 0 && (!aligned_to(k, dtype) || !aligned_to(v, dtype))) || ((uintptr_t)lengths & 3))
         return SQ_ERR_UNSUPPORTED;
-    const size_t need = sq_cross_attention_workspace_bytes(N, Lq, Lk, heads, kv_heads, D, dtype);
-    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
     CrossArgs a{};
     a.q = q; a.k = k; a.v = v; a.out = out;
     a.dtype = dtype; a.N = N; a.Lq = Lq; a.Lk = Lk; a.heads = heads; a.kv_heads = kv_heads; a.D = D; a.scale = scale;
     a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out;
     a.lengths = lengths; a.mask = mask; a.mask_image = mask_image; a.mask_row = mask_row;
     a.workspace = workspace;
-    return cross_attention(a);
+    return cross_attention(a, workspace_bytes);
 }
 
 }  // extern "C"

@@ -194,10 +194,10 @@ template <typename T> __device__ __forceinline__ void put4(const CrossParams &p,
 template <typename T, int DP> struct Tile {
     static constexpr bool kF32 = sizeof(T) == 4, kSplit = kF32 && DP <= 128;
     static constexpr int KT = kF32 ? 32 : 64, PL = kSplit ? 3 : 1, P = kF32 && !kSplit ? DP / 4 : DP / 8;     // states, planes, 16-byte pieces of a row in LDS
-    // Pieces from one state to the next: keys in odd steps (a column of pieces covers all banks), values in steps of 4 modulo 8 (the four
-    // states of a transposed read lie apart; fp32 ones are read as they lie).
     // Workgroups to a compute unit, with 32 or 64 rows to a wavefront.
     static constexpr int kFit[2] = {DP <= 32 || (DP <= 64 && !kF32) ? 3 : DP <= 96 || (DP <= 128 && !kF32) ? 2 : 1, 2};
+    // Pieces from one state to the next: keys in odd steps (a column of pieces covers all banks), values in steps of 4 modulo 8 (the four
+    // states of a transposed read lie apart; fp32 ones are read as they lie).
     static constexpr int SK = P + 1, SV = kF32 && !kSplit ? P : P % 8 == 4 ? P : P + 4;
 };
 
@@ -953,18 +953,24 @@ template <typename T> int run(const CrossParams &p, int block)
 
 }  // namespace
 
-size_t cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype)
+static size_t need_of(const Plan &plan, int N, int kv_heads, int D)
 {
-    Plan plan{};
-    if (!plan_of(N, Lq, Lk, heads, kv_heads, D, dtype, plan) || plan.shares == 1) return 0;
+    if (plan.shares == 1) return 0;
     const size_t rows = (size_t)plan.shares * N * kv_heads * plan.rows;
     return align_up(rows * part_row(D) * sizeof(float), 256) + rows * sizeof(float2);
 }
 
-int cross_attention(const CrossArgs &a)
+size_t cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype)
+{
+    Plan plan{};
+    return plan_of(N, Lq, Lk, heads, kv_heads, D, dtype, plan) ? need_of(plan, N, kv_heads, D) : 0;
+}
+
+int cross_attention(const CrossArgs &a, size_t workspace_bytes)
 {
     Plan plan{};
     if (!plan_of(a.N, a.Lq, a.Lk, a.heads, a.kv_heads, a.D, a.dtype, plan)) return SQ_ERR_UNSUPPORTED;
+    if (!enough_workspace(need_of(plan, a.N, a.kv_heads, a.D), a.workspace, workspace_bytes)) return SQ_ERR_WORKSPACE;
     CrossParams p{};
     p.a = a;
     p.group = a.heads / a.kv_heads;

@@ -561,7 +561,7 @@ __global__ __launch_bounds__(64 * WR *WC *KS) void linear_tile_kernel(LinearArgs
 // ---- the shares' sums ----------------------------------------------------------------------------------------------
 // A thread adds up four neighbouring results of a row, in order of the shares, and finishes them.  In LinearArgs `in` is the
 // shares' sums in rows of ld_in, a multiple of four.  Bound by its launch.
-constexpr int kMostShares = kLinearMostShares;
+constexpr int kMostShares = 16;
 template <typename TO> __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p)
 {
     const unsigned quads = (unsigned)(p.Cout - 1) / 4 + 1, e = blockIdx.x * 256 + threadIdx.x, r = e / quads;
@@ -592,14 +592,6 @@ template <typename TO> __global__ __launch_bounds__(256) void linear_join_kernel
         o.v[i] = from_f32<TO>(p.residual ? y + to_f32(res.v[i]) : y);
     }
     __builtin_memcpy((TO *)p.out + r * p.ld_out + j, &o, sizeof(o));
-}
-
-template <typename TO> int join(const LinearArgs &p)
-{
-    const unsigned threads = (unsigned)p.rows * ((unsigned)(p.Cout - 1) / 4 + 1);       // at most 512 tiles' results
-    const LaunchScope prof("linear_join", 0, 4.0 * p.shares * p.rows * p.Cout + (sizeof(TO) * (p.residual ? 2.0 : 1.0)) * p.rows * p.Cout);
-    hipLaunchKernelGGL((linear_join_kernel<TO>), dim3((threads - 1) / 256 + 1), dim3(256), 0, current_stream(), p);
-    return check_launch();
 }
 
 // ---- which of them ------------------------------------------------------------------------------------------------
@@ -720,6 +712,8 @@ bool direct_loads(int in_dtype, int Cin, long long ld_in, bool aligned)
 }
 // Whether bfloat16 rows may begin between words.
 bool between_words(const LinearArgs &p) { return p.in_dtype == SQ_BF16 && ((p.Cin | p.ld_in) % 2 || (((uintptr_t)p.in | (uintptr_t)p.w) & 3)); }
+// Rows of the shares' sums begin at whole lines.
+long long share_row(int Cout) { return ((long long)Cout + 31) / 32 * 32; }
 
 template <typename TI, typename TO> int launch_tiling(const LinearArgs &p, int which, bool direct)
 {
@@ -761,10 +755,13 @@ template <typename TI, typename TO> int by_size(LinearArgs p)
     if (plan.shares == 1) return launch_tiling<TI, TO>(p, plan.which, direct);
     LinearArgs part = p;
     part.b = nullptr, part.residual = nullptr, part.act = SQ_ACT_NONE;
-    part.out = p.workspace, part.out_dtype = SQ_F32, part.ld_out = linear_share_row(p.Cout);
+    part.out = p.workspace, part.out_dtype = SQ_F32, part.ld_out = share_row(p.Cout);
     if (const int rc = launch_tiling<TI, float>(part, plan.which, direct)) return rc;
     p.in = p.workspace, p.ld_in = part.ld_out;
-    return join<TO>(p);
+    const unsigned threads = (unsigned)p.rows * ((unsigned)(p.Cout - 1) / 4 + 1);       // at most 512 tiles' results
+    const LaunchScope prof("linear_join", 0, 4.0 * plan.shares * p.rows * p.Cout + (sizeof(TO) * (p.residual ? 2.0 : 1.0)) * p.rows * p.Cout);
+    hipLaunchKernelGGL((linear_join_kernel<TO>), dim3((threads - 1) / 256 + 1), dim3(256), 0, current_stream(), p);
+    return check_launch();
 }
 
 }  // namespace
@@ -780,7 +777,7 @@ size_t linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype, long lo
     LinearArgs p{};
     p.rows = rows, p.Cin = Cin, p.Cout = Cout, p.in_dtype = in_dtype;
     const int shares = plan_of(p, direct_loads(in_dtype, Cin, ld_in, aligned)).shares;
-    return shares == 1 ? 0 : (size_t)shares * rows * linear_share_row(Cout) * sizeof(float);
+    return shares == 1 ? 0 : (size_t)shares * rows * share_row(Cout) * sizeof(float);
 }
 
 int linear(const LinearArgs &p)
@@ -788,7 +785,5 @@ int linear(const LinearArgs &p)
     if (p.in_dtype == SQ_F32) return by_size<float, float>(p);
     return p.out_dtype == SQ_F32 ? by_size<bf16_t, float>(p) : by_size<bf16_t, bf16_t>(p);
 }
-
-int linear_join(const LinearArgs &p) { return p.out_dtype == SQ_F32 ? join<float>(p) : join<bf16_t>(p); }
 
 }  // namespace sq

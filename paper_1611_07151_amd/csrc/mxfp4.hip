@@ -165,7 +165,6 @@ struct MxArgs {
     LinearArgs p;           // in, w, Cin and their ld are not looked at
     Packed x, w;
     int chunks;             // of a row
-    int share;              // of the chunks: a workgroup's
 };
 
 __device__ __forceinline__ i32x8_t wide(u32x4_t v)
@@ -269,10 +268,10 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 136 * NS <= 80 * 1024 ? 2 
     int tr, tj;
     tile_at(blockIdx.x, tiles_r * tiles_j, tiles_r, tiles_j, tr, tj);
     const int r0 = tr * BM, j0 = tj * BN;
-    const int c0 = blockIdx.y * a.share, steps = min(a.share, a.chunks - c0);
+    const int steps = a.chunks;
     const uint32_t row_bytes = (uint32_t)a.chunks * 128;
-    const uint8_t *const x0 = a.x.codes + (long long)r0 * row_bytes + c0 * 128ll, *const w0 = a.w.codes + (long long)j0 * row_bytes + c0 * 128ll;
-    const uint32_t *const xs0 = a.x.scales + ((long long)(r0 >> 5) * a.chunks + c0) * 64, *const ws0 = a.w.scales + ((long long)(j0 >> 5) * a.chunks + c0) * 64;
+    const uint8_t *const x0 = a.x.codes + (long long)r0 * row_bytes, *const w0 = a.w.codes + (long long)j0 * row_bytes;
+    const uint32_t *const xs0 = a.x.scales + (long long)(r0 >> 5) * a.chunks * 64, *const ws0 = a.w.scales + (long long)(j0 >> 5) * a.chunks * 64;
     // A buffer's third word is its size: 0 for the steps behind the last one, whose loads then fetch nothing but are waited for like the
     // others, so that the loop has no branches.
     auto resource = [](const void *at, uint32_t size) {
@@ -388,16 +387,20 @@ __global__ __launch_bounds__(64 * WR *WC, (BM + BN) * 136 * NS <= 80 * 1024 ? 2 
     __syncthreads();
     constexpr int kBuf = 32 * (32 * JB + 4);
     static_assert(kBuf * 4 * NW <= NS * kImage * 16, "the wavefronts' exchange areas fit the images");
-    LinearArgs to = p;
-    to.out = (TO *)p.out + (long long)blockIdx.y * p.rows * p.ld_out;
-    write_rows<TO, XB, JB>(to, (float *)lds + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
+    write_rows<TO, XB, JB>(p, (float *)lds + wave * kBuf, acc, r0 + wave / WC * (XB * 32), j0 + wave % WC * (JB * 32), lane);
 }
 
+// Bytes that a product cannot do without: its packed operands (or the rows as they are), results and residual.
+double mx_bytes(const MxArgs &a)
+{
+    const double so = a.p.out_dtype == SQ_F32 ? 4.0 : 2.0, rows = a.x.codes ? (double)mxfp4_packed_bytes(a.p.rows, a.p.Cin) : (a.p.in_dtype == SQ_F32 ? 4.0 : 2.0) * a.p.rows * a.p.Cin;
+    return rows + (double)mxfp4_packed_bytes(a.p.Cout, a.p.Cin) + so * a.p.rows * a.p.Cout * (a.p.residual ? 2 : 1) + 4.0 * a.p.Cout;
+}
 template <typename TX, typename TO> int launch_wave(const MxArgs &a)
 {
     const int tr = (a.p.rows - 1) / 16 + 1, tj = (a.p.Cout - 1) / 16 + 1, waves = std::min(a.chunks, 16);
     if (!one_launch((double)tr * tj, 64 * waves)) return SQ_ERR_UNSUPPORTED;
-    const LaunchScope prof("mx_wave", linear_flops(a.p), 0);
+    const LaunchScope prof("mx_wave", linear_flops(a.p), mx_bytes(a));
     hipLaunchKernelGGL((mx_wave_kernel<TX, TO, 16>), dim3((unsigned)tr * tj), dim3(64 * waves), 0, current_stream(), a, tr, tj);
     return check_launch();
 }
@@ -406,8 +409,8 @@ template <typename TO, int BM, int BN, int WR, int WC, int NS> int launch_tile(c
 {
     const int tr = (a.p.rows - 1) / BM + 1, tj = (a.p.Cout - 1) / BN + 1;
     if (!one_launch((double)tr * tj, 64 * WR * WC)) return SQ_ERR_UNSUPPORTED;
-    const LaunchScope prof("mx_tile", linear_flops(a.p), 0);
-    hipLaunchKernelGGL((mx_tile_kernel<TO, BM, BN, WR, WC, NS>), dim3((unsigned)tr * tj, (a.chunks - 1) / a.share + 1), dim3(64 * WR * WC), 0, current_stream(), a, tr, tj);
+    const LaunchScope prof("mx_tile", linear_flops(a.p), mx_bytes(a));
+    hipLaunchKernelGGL((mx_tile_kernel<TO, BM, BN, WR, WC, NS>), dim3((unsigned)tr * tj), dim3(64 * WR * WC), 0, current_stream(), a, tr, tj);
     return check_launch();
 }
 
@@ -494,19 +497,21 @@ int mxfp4_unpack(const void *in, void *out, int out_dtype, int rows, int Cin, lo
     return check_launch();
 }
 
+static size_t need_of(const Plan &plan, int rows, int Cin, int in_dtype) { return in_dtype == SQ_MXFP4 || plan.raw ? 0 : mxfp4_packed_bytes(rows, Cin); }
+
 size_t mxfp4_linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype)
 {
-    const Plan plan = plan_of(rows, Cin, Cout);
-    return in_dtype == SQ_MXFP4 || plan.raw ? 0 : mxfp4_packed_bytes(rows, Cin);
+    return need_of(plan_of(rows, Cin, Cout), rows, Cin, in_dtype);
 }
 
-int mxfp4_linear(const LinearArgs &p)
+int mxfp4_linear(const LinearArgs &p, size_t workspace_bytes)
 {
     MxArgs a{};
     a.p = p;
-    a.chunks = a.share = chunks_of(p.Cin);
+    a.chunks = chunks_of(p.Cin);
     a.w = packed_at(p.w, p.Cout, p.Cin);
     const Plan plan = plan_of(p.rows, p.Cin, p.Cout);
+    if (!enough_workspace(need_of(plan, p.rows, p.Cin, p.in_dtype), p.workspace, workspace_bytes)) return SQ_ERR_WORKSPACE;
     if (plan.which == kNone) return SQ_ERR_UNSUPPORTED;
     if (plan.raw && p.in_dtype != SQ_MXFP4) return p.in_dtype == SQ_F32 ? raw_rows<float>(a) : raw_rows<bf16_t>(a);
     const void *x = p.in;

@@ -236,18 +236,16 @@ inline double linear_bytes(const LinearArgs &a)
     return si * ((double)a.rows * a.Cin + (double)a.Cout * a.Cin) + so * (double)a.rows * a.Cout * (a.residual ? 2 : 1) + 4.0 * a.Cout;
 }
 int linear(const LinearArgs &a);
-// Adds up the shares' sums, a.shares of them in `in` as rows of ld_in = linear_share_row(Cout) values of fp32 each, and finishes them.
-int linear_join(const LinearArgs &a);
-inline long long linear_share_row(int Cout) { return ((long long)Cout + 31) / 32 * 32; }    // rows begin at whole lines
-constexpr int kLinearMostShares = 16;
-// Rows in microscaled 4-bit floating point (mxfp4.hip), after validation.  mxfp4_linear: in_dtype SQ_F32, SQ_BF16 (workspace holds the packed
-// rows) or SQ_MXFP4; w packed.
+// Whether a workspace will do.
+inline bool enough_workspace(size_t need, const void *workspace, size_t bytes) { return !need || (workspace && !((uintptr_t)workspace & 255) && bytes >= need); }
+// Rows in microscaled 4-bit floating point (mxfp4.hip), after validation but for the workspace's size, which the calls that take one look
+// at themselves (they know the plan by then).  mxfp4_linear: in_dtype SQ_F32, SQ_BF16 (workspace holds the packed rows) or SQ_MXFP4; w packed.
 size_t mxfp4_packed_bytes(int rows, int Cin);
 int mxfp4_pack(const void *in, int in_dtype, void *out, int rows, int Cin, long long ld);
 int mxfp4_unpack(const void *in, void *out, int out_dtype, int rows, int Cin, long long ld);
 size_t mxfp4_linear_workspace_bytes(int rows, int Cin, int Cout, int in_dtype);
-int mxfp4_linear(const LinearArgs &a);
-// Attention to an encoder's states (cross_attention.hip), after validation.
+int mxfp4_linear(const LinearArgs &a, size_t workspace_bytes);
+// Attention to an encoder's states (cross_attention.hip), likewise.
 struct CrossArgs {
     const void *q, *k, *v;
     void *out;
@@ -265,7 +263,7 @@ inline double cross_bytes(const CrossArgs &a)
 {
     return (a.dtype == SQ_F32 ? 4.0 : 2.0) * 2.0 * a.N * a.D * ((double)a.Lq * a.heads + (double)a.Lk * a.kv_heads);
 }
-int cross_attention(const CrossArgs &a);
+int cross_attention(const CrossArgs &a, size_t workspace_bytes);
 // Loads the code of these kernels onto the current device (sq_init).
 bool nhwc_layout_register_kernels();
 bool nhwc_norm_register_kernels();

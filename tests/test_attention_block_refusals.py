@@ -61,9 +61,10 @@ def test_linear(lib):
     assert f(ldi=39) == -2 and f(ldo=6) == -2 and f(res=P, ldr=6) == -2
     assert f(ti=3) == -3 and f(ti=-1) == -3 and f(to=2) == -3 and f(act=4) == -3 and f(act=-1) == -3
     assert f(x=ODD) == -3 and f(out=ODD) == -3 and f(b=ODD) == -3 and f(res=ODD, ldr=7) == -3
-    assert f(w=OFF) == -4 and f(x=OFF, ti=2) == -4 and f(ws=NULL) == -4 and f(ws=OFF) == -4
+    assert f(w=OFF) == -4 and f(x=OFF, ti=2) == -4
     need = lib.sq_mxfp4_linear_workspace_bytes(100, 4096, 4096, 0)
-    assert need > 0 and f(rows=100, cin=4096, cout=4096, ldi=4096, ldo=4096, nb=need - 1) == -4
+    wide = dict(rows=100, cin=4096, cout=4096, ldi=4096, ldo=4096)
+    assert need > 0 and f(**wide, nb=need - 1) == -4 and f(**wide, ws=NULL) == -4 and f(**wide, ws=OFF) == -4
     assert lib.sq_mxfp4_linear_workspace_bytes(0, 40, 7, 0) == 0 and lib.sq_mxfp4_linear_workspace_bytes(5, 40, 7, 3) == 0
     assert f(rows=2**31 - 1, cout=2**31 - 1, ldo=2**31 - 1, nb=2**63) == -3
 

@@ -7,8 +7,10 @@ u = 2^-24.  With S = the largest scale * sum_d |q_d||k_d| over the states that a
   a maximum that is raised, or sums of shares that are joined, cost 8u S + 8u each time, at most once every 32 states and once a share:
   R = (Lk / 32 + 65) (8u S + 8u);
   sums of up to Lk terms: (Lk + 16) 2u;
-  bfloat16: p is rounded before it multiplies v, half a step, 2^-8;
-  so A (2 (E + R + (Lk + 16) 2u) + [2^-8]) + 8u |out| for the numerator, the denominator and their quotient, and half a step of the type.
+  bfloat16: p is rounded before it multiplies v, half a step, 2^-8, and the rounded ones may be what is added up: sum p' v / sum p' - out =
+  sum (p' - p) (v - out) / sum p', at most 2^-8 sum p |v - out| / sum p' <= 2^-8 (1 + 2^-7) (A + |out|);
+  so A 2 (E + R + (Lk + 16) 2u) + [2^-8 (1 + 2^-7) (A + |out|)] + 8u |out| for the numerator, the denominator and their quotient, and half a
+  step of the type.
 """
 import math
 
@@ -52,7 +54,7 @@ def reference(q, k, v, heads, kv_heads, scale, seen, dt):
     e = (2 * d + 24) * U * big + 8 * U
     r = (lk / 32 + 65) * (8 * U * big + 8 * U)
     eps = torch.finfo(dt)
-    bound = a * (2 * (e + r + (lk + 16) * 2 * U) + (2.0 ** -8 if dt == BF16 else 0)) + 8 * U * out.abs()
+    bound = a * 2 * (e + r + (lk + 16) * 2 * U) + (2.0 ** -8 * (1 + 2.0 ** -7) * (a + out.abs()) if dt == BF16 else 0) + 8 * U * out.abs()
     bound = bound * (1 + eps.eps) + eps.eps / 2 * out.abs() * (1 + 1e-6) + eps.smallest_normal
     back = lambda t: t.permute(0, 2, 1, 3).reshape(n, lq, heads * d)
     return back(out), back(bound)
