@@ -763,6 +763,8 @@ def _rows_of(t, name, index):
     length = shape[-1]
     if t.is_contiguous():
         ld = length
+    elif len(shape) == 3 and shape[1] > 1 and (stride := t.stride())[2] == 1 and stride[1] >= length and (shape[0] == 1 or stride[0] == stride[1] * shape[1]):
+        ld = stride[1]          # the usual slice, without the general search
     else:
         stride, ld, span = t.stride(), None, 0
         for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
@@ -1066,12 +1068,13 @@ def sq_cross_attention_forward(q, k, v, heads, kv_heads=None, scale=None, length
     kv_heads = heads if kv_heads is None else _int(kv_heads, -2, what)
     index = _gpu_of(q, "q")
     N, C = q.shape[0], q.shape[-1]
-    if k.shape[0] != N or k.shape != v.shape or k.dtype != q.dtype or v.dtype != q.dtype:
+    shape, dtype = k.shape, q.dtype
+    if shape[0] != N or shape != v.shape or k.dtype != dtype or v.dtype != dtype:
         raise ValueError("k and v must be alike, with the images and the type of q")
     if heads <= 0 or kv_heads <= 0 or heads % kv_heads:
         _check(-2, what)
     D = C // heads
-    if D * heads != C or k.shape[-1] != D * kv_heads:
+    if D * heads != C or shape[-1] != D * kv_heads:
         raise ValueError("q must have heads * D values a row, k and v kv_heads * D")
     ld_q, ld_k, ld_v = _rows_of(q, "q", index), _rows_of(k, "k", index), _rows_of(v, "v", index)
     if not N or not C or not q.numel():
@@ -1080,7 +1083,7 @@ def sq_cross_attention_forward(q, k, v, heads, kv_heads=None, scale=None, length
     if Lq > _MAX_INT or Lk > _MAX_INT:
         _check(-3, what)
     if out is None:
-        out, ld_out = torch.empty_like(q, memory_format=torch.contiguous_format), C
+        out, ld_out = q.new_empty(q.shape), C
     else:
         if out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out has the wrong shape or type")

@@ -27,10 +27,11 @@ struct CrossParams {
     int part_ld;
 };
 
-// 16 bytes of a head's D values from value d on, zeros behind the last.  EVEN: heads of whole pieces, rows of whole pieces.  Others are loaded
-// from where all 16 bytes are the head's own and moved into place by `placed`, so that no load waits for another, and heads of less than
-// 16 bytes one value at a time.  bfloat16 values may begin between words: the words that hold them are loaded, none beyond (16 bytes at
-// such an address take four times as long), and `placed` shifts them too.
+// 16 bytes of a head's D values from value d on; behind the last its last ones again, as rows behind the last state are the last one again:
+// what multiplies them are zeros of the query or of the exponentials, and what they give is not written (they are finite wherever the
+// state itself is).  EVEN: heads of whole pieces.  The others are loaded from where all 16 bytes are the head's own and moved into place
+// by `placed`, so that no load waits for another, and heads of less than 16 bytes one value at a time.  bfloat16 values may begin between
+// words: the words that hold them are loaded, none beyond (16 bytes at such an address take four times as long), and `placed` shifts them too.
 template <bool EVEN, typename T> struct Piece {
     u32x4_t v;
 };
@@ -57,12 +58,11 @@ template <bool EVEN, typename T> __device__ __forceinline__ Piece<EVEN, T> loade
     r.v = EVEN || D >= n ? __builtin_bit_cast(u32x4_t, load_n<n>(head + min(d, D - n))) : __builtin_bit_cast(u32x4_t, load_some<n>(head, D));
     return r;
 }
-// `there`: whether the state is (zeros otherwise); odd: whether the head begins between words.
-template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t placed(const Piece<EVEN, T> &piece, int d, int D, bool odd, bool there = true)
+// With zeros behind the last value.  odd: whether the head begins between words.
+template <bool EVEN, typename T> __device__ __forceinline__ u32x4_t placed(const Piece<EVEN, T> &piece, int d, int D, bool odd)
 {
     constexpr int n = 16 / (int)sizeof(T);
     u32x4_t v = piece.v;
-    if (!there) d = D + n;
     if (EVEN) {
         if (d >= D) v = u32x4_t{};
         return v;
@@ -264,16 +264,16 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     Piece<EVEN, T> nk[NP], nv[NP];
     uint32_t odd = 0;           // bits 2 i and 2 i + 1: whether their rows begin between words
     long long step_k[NP], step_v[NP];
-    const bool whole = EVEN && D == DP;
+    if (EVEN)
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int e = threadIdx.x + i * 256, d = whole ? e % P * n : 0;
-        step_k[i] = e / P * p.a.ld_k + d, step_v[i] = e / P * p.a.ld_v + d;
-    }
+        for (int i = 0; i < NP; ++i) {
+            const int e = threadIdx.x + i * 256, d = min(e % P * n, D - n);
+            step_k[i] = e / P * p.a.ld_k + d, step_v[i] = e / P * p.a.ld_v + d;
+        }
     auto fetch = [&](int at) {
         if (threadIdx.x < KT) seen = at + (int)threadIdx.x < end && (!by_state || mask[0][at + threadIdx.x]);
         const T *const kt = k0 + at * p.a.ld_k, *const vt = v0 + at * p.a.ld_v;
-        if (whole && at + KT <= end) {
+        if (EVEN && at + KT <= end) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) nk[i].v = __builtin_bit_cast(u32x4_t, load_n<n>(kt + step_k[i])), nv[i].v = __builtin_bit_cast(u32x4_t, load_n<n>(vt + step_v[i]));
         } else {        // states behind the last are the last one again
@@ -288,17 +288,16 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             }
         }
     };
-    auto store = [&](int image_of, int at) {
+    auto store = [&](int image_of) {
         u32x4_t *const to = lds + image_of * kImage;
         if (threadIdx.x < KT) biases[image_of][threadIdx.x] = seen ? 0.f : -HUGE_VALF;
-        if (!(whole && at + KT <= end)) {
+        if constexpr (!EVEN)
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int e = threadIdx.x + i * 256, d = e % P * n;
+                const int d = (int)(threadIdx.x + i * 256) % P * n;
                 nk[i].v = placed(nk[i], d, D, odd >> 2 * i & 1);
-                nv[i].v = placed(nv[i], d, D, odd >> (2 * i + 1) & 1, at + e / P < end);
+                nv[i].v = placed(nv[i], d, D, odd >> (2 * i + 1) & 1);
             }
-        }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int e = threadIdx.x + i * 256, j = e / P, d = e % P;
@@ -333,7 +332,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     for (int r = 0; r < RB; ++r) base[r] = -HUGE_VALF, total[r] = 0.f;
     if (first < end) {
         fetch(first);
-        store(0, first);
+        store(0);
     }
     __syncthreads();
     int img = 0;
@@ -497,7 +496,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         }
         __builtin_amdgcn_s_setprio(0);
         img ^= 1;
-        if (more) store(img, at + KT);
+        if (more) store(img);
         __syncthreads();
     };
     int at = first;
@@ -650,7 +649,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
             s[kb] = f32x4_t{};
 #pragma unroll
             for (int t = 0; t < P / 4; ++t) {
-                const u32x4_t k = placed(nk[kb][t], (4 * t + quarter) * n, D, odd_k >> kb & 1);
+                const u32x4_t k = EVEN ? nk[kb][t].v : placed(nk[kb][t], (4 * t + quarter) * n, D, odd_k >> kb & 1);
                 if constexpr (kF32) {
                     const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[t]);
 #pragma unroll
@@ -691,7 +690,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
             }
         u32x4_t v[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = placed(nv[i], value_at(i), D, odd_v >> i & 1, at + value_state(i) < end);
+        for (int i = 0; i < NV; ++i) v[i] = EVEN ? nv[i].v : placed(nv[i], value_at(i), D, odd_v >> i & 1);
         if constexpr (kF32) {
             if (more) fetch_values(at + NW * KC);
 #pragma unroll
