@@ -190,7 +190,10 @@ template <typename T> __device__ __forceinline__ void put4(const CrossParams &p,
 // product with the transposed values: lane half h has states 8 i + 4 h to 8 i + 4 h + 3, and the values' lanes take the same ones.
 // fp32 heads of up to 128 run on the bfloat16 instructions, every operand as the sum of three bfloat16 values (x = h + m + l, exact; of the nine
 // products the six down to 2^-16 of the largest, the smallest first), each a plane of its own in LDS or registers; wider ones, whose planes
-// LDS has no room for, on the fp32 instructions.
+// LDS has no room for, on the fp32 instructions (4 x 3025 x 729 in 8 heads of 64: 160 us on those, 115 so).
+// Bound by the vector instructions of the exponentials beside the matrix unit: bf16, 16 heads of 64, 16 images of 3025 queries to 4096
+// states 880 to 990 us (820 to 920 TFLOP/s, matrix unit 43 % busy), 4 images in heads of 128 440 to 460 (880 to 930).  Sums by additions instead of
+// the two-value instruction need more registers than there are (spills: 1280 us for 960).
 template <typename T, int DP> struct Tile {
     static constexpr bool kF32 = sizeof(T) == 4, kSplit = kF32 && DP <= 128;
     static constexpr int KT = kF32 ? 32 : 64, PL = kSplit ? 3 : 1, P = kF32 && !kSplit ? DP / 4 : DP / 8;     // states, planes, 16-byte pieces of a row in LDS
@@ -561,6 +564,8 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
 // has states 4 (l / 16) to 4 (l / 16) + 3 of row l % 16.
 //   bf16: values go through the wavefront's part of LDS, which gives them back transposed
 //   fp32: an instruction takes one state of each four, and value e of each four of a head, so that lanes load 16 bytes of neighbouring values
+// Bound by memory where states are many (8 queries to 16384 states of 8 heads of 128: 112 us, 4.8 TB/s), else by the latency of a turn of
+// loads and of the joining (1 query to 729 states of 8 heads of 64: 7.9 us).
 template <typename T> struct Chunk;
 template <> struct Chunk<bf16_t> {
     static constexpr int KC = 32;
