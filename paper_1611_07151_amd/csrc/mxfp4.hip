@@ -91,7 +91,7 @@ template <> struct Eight<bf16_t> {
 template <typename TI> __device__ __forceinline__ Eight<TI> eight_at(const TI *row, int k, int Cin, bool whole)
 {
     Eight<TI> e;
-    if (whole || k + 8 <= Cin) {
+    if (whole || k <= Cin - 8) {         // (k + 8 may pass 32 bits)
         __builtin_memcpy(&e, row + k, sizeof(e));
     } else {
         Vec<TI, 8> v = {};
@@ -151,7 +151,7 @@ template <typename TO> __global__ __launch_bounds__(256) void mx_unpack_kernel(P
         v.v[i] = from_f32<TO>(code == 255 ? __builtin_nanf("") : x);
     }
     TO *at = out + (long long)r * ld + part * 8;
-    if (part * 8 + 8 <= Cin) {
+    if (part * 8 <= Cin - 8) {          // (the sum may pass 32 bits)
         __builtin_memcpy(at, &v, sizeof(v));
     } else {
 #pragma unroll

@@ -294,3 +294,24 @@ def test_refusals_of_the_binding(sq):
     for call in (lambda: sq.sq_mxfp4_linear_forward(x, w, 8, act=4), lambda: sq.sq_mxfp4_pack(x[:0])):
         with pytest.raises(sq.SqError):
             call()
+
+
+@pytest.mark.parametrize("behind", [1, 6, 255])
+def test_rows_whose_end_is_where_32_bits_end(sq, behind):
+    """One row of 2^31 - behind values: the last chunk as that of a short row with the same values, nothing read or written behind."""
+    cin, first = 2 ** 31 - behind, 2 ** 31 - 256        # where the last chunk begins
+    buf = torch.zeros(2 ** 31 + 64, device="cuda", dtype=BF16)
+    tail = torch.randn(cin - first, generator=gen(behind)).to(BF16)
+    buf[first:cin] = tail.cuda()
+    buf[cin:] = 1e30                                    # would raise the last block's power
+    x = buf[:cin].view(1, cin)
+    packed = sq.sq_mxfp4_pack(x)
+    short = sq.sq_mxfp4_pack(tail.cuda().view(1, -1))
+    scales = 2 ** 23 * 256
+    lane = packed[scales - 256:scales].view(2, 32, 4)[:, 0]         # row 0 of the group
+    assert torch.equal(lane, short[:256].view(2, 32, 4)[:, 0])
+    assert torch.equal(packed[-128:], short[-128:])
+    buf.fill_(3.0)
+    sq.sq_mxfp4_unpack(packed, 1, cin, out=x)
+    assert torch.equal(x[0, first:].cpu().double(), values64(tail.view(1, -1))[0]) and not x[0, first - 4096:first].any()
+    assert (buf[cin:] == 3).all()
