@@ -14,6 +14,12 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896341f;
 
+// What a row's exponents were taken against, in base two, and their sum.
+struct PartSum {
+    double base;
+    float total;
+};
+
 // The heads of the queries that share a head of the states are further rows to it: row r is query r / group, head r % group of them.
 struct CrossParams {
     CrossArgs a;
@@ -23,7 +29,7 @@ struct CrossParams {
     float c;                // |scale| log2 e, or 1 where the scale is 0
     uint32_t keep, flip;    // bits of q that stay (none where the scale is 0), sign bits that turn q into -q where it is below 0
     float *part_o;          // [share][image, head, row][part_ld] and
-    float2 *part_ml;        // [share][image, head, row] what the exponents were taken against and their sum, where shares > 1
+    PartSum *part_ml;       // [share][image, head, row], where shares > 1
     int part_ld;
 };
 
@@ -133,9 +139,16 @@ template <typename T> __device__ __forceinline__ void row_of(const CrossParams &
     mask = p.a.mask ? p.a.mask + image * p.a.mask_image + i * p.a.mask_row : nullptr;
 }
 
-// A masked value that is not finite has gone into a row's sums as 0 * it: a wavefront makes such a row again from the states it sees, lane by
-// lane of the head's values, its sums into `area`.
-template <typename T, int DP> __device__ __forceinline__ void row_again(const CrossParams &p, int image, int head, int r, int first, int end, float *area, float &base, float &total)
+// What a row's exponents may be taken against: a scaled score of any size, held within fp32's range, or -infinity where no state has been
+// seen.  A score past that range, and one so far out that its product with c is rounded by more than the exponent's range, leaves a
+// sum that is zero or not finite, by which the row is known.
+__device__ __forceinline__ float in_range(float score) { return fminf(fmaxf(score, -__FLT_MAX__), __FLT_MAX__); }
+__device__ __forceinline__ bool beyond(float base, float total) { return base != -HUGE_VALF && !(total > 0.f && total < HUGE_VALF); }
+
+// A row whose sums 32 bits do not hold, or into whose sums a hidden value that is not finite has gone as 0 * it: a wavefront makes it again
+// from the states it sees, lane by lane of the head's values, with scores and sums in 64 bits, which hold every product and sum of fp32
+// values.  area: the sums over the head's values to go with `total`, their mean where they are the result.
+template <typename T, int DP> __device__ __forceinline__ void row_again(const CrossParams &p, int image, int head, int r, int first, int end, float *area, double &base, float &total)
 {
     constexpr int E = (DP + 63) / 64;
     const int lane = threadIdx.x & 63, D = p.a.D;
@@ -144,29 +157,58 @@ template <typename T, int DP> __device__ __forceinline__ void row_again(const Cr
     T *unused;
     row_of<T>(p, image, head, r, q, mask, unused);
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * D;
-    float qv[E], sum[E] = {}, m = -HUGE_VALF, l = 0.f;
+    float qv[E];
+    double sum[E] = {}, m = -HUGE_VAL, l = 0.0;
+    bool odd = false, sees = false;
 #pragma unroll
-    for (int e = 0; e < E; ++e) qv[e] = lane + 64 * e < D ? (p.keep ? to_f32(q[lane + 64 * e]) : 0.f) * (p.flip ? -1.f : 1.f) : 0.f;
+    for (int e = 0; e < E; ++e) {
+        qv[e] = lane + 64 * e < D ? (p.keep ? to_f32(q[lane + 64 * e]) : 0.f) * (p.flip ? -1.f : 1.f) : 0.f;
+        odd |= !__builtin_isfinite(qv[e]);
+    }
+    odd = __any(odd);
     for (int j = first; j < end; ++j) {
         if (mask && !mask[j]) continue;
-        float dot = 0.f;
+        sees = true;
+        if (odd) l = __builtin_nan("");
+        if (l != l) break;          // and so is the result
+        double dot = 0.0;
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < D) dot = __builtin_fmaf(qv[e], to_f32(k0[j * p.a.ld_k + lane + 64 * e]), dot);
+            if (lane + 64 * e < D) dot = __builtin_fma((double)qv[e], (double)to_f32(k0[j * p.a.ld_k + lane + 64 * e]), dot);
         for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
-        const float up = fmaxf(m, dot * p.c), upc = up == -HUGE_VALF ? 0.f : up;
-        const float shrink = m == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(m - up), w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, p.c, -upc));
+        const double up = fmax(m, dot);
+        const float shrink = m == -HUGE_VAL ? 0.f : __builtin_amdgcn_exp2f((float)((m - up) * p.c)), w = dot == -HUGE_VAL ? 0.f : __builtin_amdgcn_exp2f((float)((dot - up) * p.c));
         m = up;
         l = l * shrink + w;
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < D) sum[e] = sum[e] * shrink + w * to_f32(v0[j * p.a.ld_v + lane + 64 * e]);
+            if (lane + 64 * e < D) sum[e] = sum[e] * shrink + (double)w * to_f32(v0[j * p.a.ld_v + lane + 64 * e]);
+    }
+    // a share's sums are brought below the largest value by a power of two
+    double by = 0.0;
+    base = -HUGE_VAL, total = 0.f;
+    if (sees && !(l > 0.0)) {
+        by = __builtin_nan(""), base = 0.0, total = __builtin_nanf("");
+    } else if (sees) {
+        const int power = p.shares > 1 ? (int)__builtin_amdgcn_logf((float)l) + 1 : 0;
+        by = p.shares > 1 ? __builtin_ldexp(1.0, -power) : 1.0 / l;
+        base = m * p.c + power, total = p.shares > 1 ? (float)(l * by) : 1.f;
     }
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < DP) area[lane + 64 * e] = sum[e];
+        if (lane + 64 * e < DP) area[lane + 64 * e] = (float)(sum[e] * by);
     __builtin_amdgcn_wave_barrier();
-    base = m, total = l;
+}
+// Whether everything is finite in a head's states first to end - 1, looked through by a wavefront.  Rows that are not right because a state is not
+// finite, which no mask hides, stay as they are: all rows made again would take a thousand times the call's time.
+template <typename T> __device__ __forceinline__ bool finite_states(const CrossParams &p, int image, int head, int first, int end)
+{
+    const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * p.a.D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * p.a.D;
+    bool odd = false;
+    for (int d = threadIdx.x & 63; d < p.a.D; d += 64)
+#pragma unroll 4
+        for (int j = first; j < end; ++j) odd |= !__builtin_isfinite(to_f32(k0[j * p.a.ld_k + d])) | !__builtin_isfinite(to_f32(v0[j * p.a.ld_v + d]));
+    return !__any(odd);
 }
 
 // Four neighbouring sums of a row from d on, out as results or as a share's sums.
@@ -395,7 +437,12 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
                 }
             }
         }
+        uint32_t seen_of[RB] = {};
         if (hidden && by_pair) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int i = 0; i < KB * 4; ++i) seen_of[r] |= bytes[r][i];
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
@@ -441,15 +488,19 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             far |= part[r] > kFar || base[r] == -HUGE_VALF;
         }
         if (__any(far)) {
+            // whether a row sees any state of this tile, which its scores may not tell where all are -infinity
+            bool some = true;
+            if (by_state) some = __any(biases[img][lane & (KT - 1)] == 0.f);
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
+                if (hidden && by_pair) some = (seen_of[r] | __shfl_xor(seen_of[r], 32)) != 0;
                 float top = s[r][0][0];
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[r][kb][i]);
                 top *= p.c;
-                const float raised = fmaxf(base[r], fmaxf(top, other_half(top))), shrink = base[r] == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base[r] - raised);
+                const float raised = some ? fmaxf(base[r], in_range(fmaxf(top, other_half(top)))) : base[r], shrink = base[r] == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base[r] - raised);
                 total[r] *= shrink;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -514,23 +565,31 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     for (int r = 0; r < RB; ++r) {
         total[r] += other_half(total[r]);
         const int row = row0 + 32 * r;
-        if (p.a.mask) {
-            bool odd = false;
+        double base_of = base[r];
+        const bool lost = beyond(base[r], total[r]);
+        bool odd = lost;
+        if (p.a.mask)
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) odd |= !__builtin_isfinite(o[r][d][i]);
-            const uint64_t lanes = __ballot(odd && row < p.rows);
-            uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+        const uint64_t lanes = __ballot(odd && row < p.rows);
+        uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+        if (__builtin_expect(again != 0, 0)) {
+            if (!p.a.mask && !finite_states<T>(p, image, head, first, end)) {
+                if (lost) total[r] = __builtin_nanf("");
+                again = 0;
+            }
             float *const area = (float *)lds + wave * DP;
             static_assert(4 * DP * 4 <= 2 * kImage * 16, "the areas fit");
             while (again) {
                 const int which = __builtin_ctz(again);
                 again &= again - 1;
-                float m, l;
+                double m;
+                float l;
                 row_again<T, DP>(p, image, head, row - (lane & 31) + which, first, end, area, m, l);
                 if ((lane & 31) == which) {
-                    base[r] = m, total[r] = l;
+                    base_of = m, total[r] = l;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -541,7 +600,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         }
         if (row >= p.rows) continue;
         const long long part = ((long long)share * p.a.N * p.a.kv_heads + ih) * p.rows + row;
-        if (p.shares > 1 && half == 0) p.part_ml[part] = float2{base[r], total[r]};
+        if (p.shares > 1 && half == 0) p.part_ml[part] = PartSum{base_of, total[r]};
         const T *qrow;
         const uint8_t *unused;
         T *out;
@@ -583,7 +642,8 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
     constexpr int kArea = kF32 ? 0 : KC * SV, kRoom = kArea > 4 * kRow ? NW * kArea : NW * 4 * kRow;        // 16 bytes: of a wavefront's values; in all
     __shared__ u32x4_t lds[kRoom];
     __shared__ float bases[NW][16], totals[NW][16];
-    __shared__ int again[16];
+    __shared__ int again[16], some_again;
+    __shared__ PartSum made[16];        // of the rows that are made again
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, quarter = lane >> 4;
     const unsigned share = blockIdx.x % (unsigned)p.shares, bt = blockIdx.x / (unsigned)p.shares;
     const int tile = (int)(bt % (unsigned)p.tiles), ih = (int)(bt / (unsigned)p.tiles), image = ih / p.a.kv_heads, head = ih - image * p.a.kv_heads;
@@ -633,8 +693,10 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
         }
     };
     f32x4_t o[DB] = {};
-    float base = -HUGE_VALF, total = 0.f;
+    // scores above `limit` raise the base
+    float base = -HUGE_VALF, limit = -HUGE_VALF, total = 0.f;
     int at = first + wave * KC;
+    uint32_t sees = !mask && at < end;
     if (at < end) {
         fetch_keys(at);
         fetch_values(at);
@@ -665,6 +727,9 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
             }
         }
         if (mask || at + KC > end) {
+            if (mask)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) sees |= bytes[kb];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -677,13 +742,14 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
         float top = max3(s[0][0], s[0][1], s[0][2]);
         top = max3(top, s[0][3], s[KB - 1][0]);
         if constexpr (KB > 1) top = max3(max3(top, s[1][1], s[1][2]), s[1][3], top);
-        top *= p.c;
-        if (__any(top > base + kHeadroom)) {
-            const float raised = fmaxf(base, over_quarters(top)), shrink = base == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base - raised);
+        if (__any(top > limit)) {
+            const float highest = over_quarters(top);
+            const float raised = highest == -HUGE_VALF ? base : fmaxf(base, in_range(highest * p.c)), shrink = base == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(base - raised);
             total *= shrink;
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] *= shrink;
             base = raised;
+            limit = (base + kHeadroom) / p.c;
         }
         const float off = base == -HUGE_VALF ? 0.f : base;
 #pragma unroll
@@ -723,12 +789,15 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
     // every wavefront's sums against the largest base, added up by all threads, four of a row each, in order of wavefronts
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
+    sees |= __shfl_xor(sees, 16);
+    sees |= __shfl_xor(sees, 32);
+    if (sees && base == -HUGE_VALF) base = -__FLT_MAX__;        // all of its scores are -infinity
     if (quarter == 0) bases[wave][l16] = base, totals[wave][l16] = total;
     __syncthreads();
     float most = bases[0][l16];
 #pragma unroll
     for (int w = 1; w < NW; ++w) most = fmaxf(most, bases[w][l16]);
-    // (without a base the sums are zero, or not finite: of a score that is NaN, or of 0 * a masked value)
+    // (without a base the sums are zero, or not finite: of 0 * a masked value)
     const float by = base == -HUGE_VALF ? 1.f : __builtin_amdgcn_exp2f(base - most);
     float *const sums = (float *)lds;
     if (row < p.rows)
@@ -742,9 +811,11 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
             if (at_d < DP) *(f32x4_t *)&sums[(wave * 16 + l16) * kRow + at_d] = v;
         }
     if (threadIdx.x < 16) again[threadIdx.x] = 0;
+    if (threadIdx.x == 16) some_again = 0;
     __syncthreads();
     constexpr int kQuads = DP / 4, kTurns = (16 * kQuads + 64 * NW - 1) / (64 * NW);
     f32x4_t of[kTurns];
+    float top_of[kTurns], sum_of[kTurns];
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
         const int e = threadIdx.x + t * 64 * NW, r = e / kQuads, d = e % kQuads * 4;
@@ -752,15 +823,25 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
         of[t] = *(const f32x4_t *)&sums[r * kRow + d];
 #pragma unroll
         for (int w = 1; w < NW; ++w) of[t] += *(const f32x4_t *)&sums[(w * 16 + r) * kRow + d];
-        if (mask && !(__builtin_isfinite(of[t][0]) && __builtin_isfinite(of[t][1]) && __builtin_isfinite(of[t][2]) && __builtin_isfinite(of[t][3]))) again[r] = 1;
+        float top = bases[0][r], sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) top = fmaxf(top, bases[w][r]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += bases[w][r] == -HUGE_VALF ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f(bases[w][r] - top);
+        bool odd = beyond(top, sum);
+        if (mask) odd |= !(__builtin_isfinite(of[t][0]) && __builtin_isfinite(of[t][1]) && __builtin_isfinite(of[t][2]) && __builtin_isfinite(of[t][3]));
+        if (odd) again[r] = some_again = 1;
+        top_of[t] = top, sum_of[t] = sum;
     }
-    if (mask) {
-        __syncthreads();
+    __syncthreads();
+    const bool remake = some_again && (mask || finite_states<T>(p, image, head, first, end));
+    if (__builtin_expect(remake, 0)) {
         for (int r = wave; r < 16; r += NW)
             if (again[r]) {
-                float m, l;
+                double m;
+                float l;
                 row_again<T, DP>(p, image, head, tile * 16 + r, first, end, &sums[r * kRow], m, l);
-                if (lane < NW) bases[lane][r] = m, totals[lane][r] = lane ? 0.f : l;
+                if (lane == 0) made[r] = PartSum{m, l};
             }
         __syncthreads();
     }
@@ -768,20 +849,17 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
     for (int t = 0; t < kTurns; ++t) {
         const int e = threadIdx.x + t * 64 * NW, r = e / kQuads, d = e % kQuads * 4;
         if (r >= 16 || tile * 16 + r >= p.rows) continue;
-        if (mask && again[r]) of[t] = *(const f32x4_t *)&sums[r * kRow + d];
-        float top = bases[0][r], sum = 0.f;
-#pragma unroll
-        for (int w = 1; w < NW; ++w) top = fmaxf(top, bases[w][r]);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) sum += bases[w][r] == -HUGE_VALF ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f(bases[w][r] - top);
+        PartSum own{top_of[t], sum_of[t]};
+        if (remake && again[r]) own = made[r], of[t] = *(const f32x4_t *)&sums[r * kRow + d];
+        else if (beyond(top_of[t], sum_of[t])) own.total = __builtin_nanf("");
         const long long part = ((long long)share * p.a.N * p.a.kv_heads + ih) * p.rows + tile * 16 + r;
-        if (p.shares > 1 && d == 0) p.part_ml[part] = float2{top, sum};
+        if (p.shares > 1 && d == 0) p.part_ml[part] = own;
         const T *q_of;
         const uint8_t *mask_of;
         T *to;
         row_of<T>(p, image, head, tile * 16 + r, q_of, mask_of, to);
         const float v[4] = {of[t][0], of[t][1], of[t][2], of[t][3]};
-        put4<T>(p, to, part, d, v, sum, 1.f / sum);
+        put4<T>(p, to, part, d, v, own.total, 1.f / own.total);
     }
 }
 
@@ -793,7 +871,7 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_few_kern
     const long long e = blockIdx.x * 256ll + threadIdx.x, at = e / quads;
     if (at >= all) return;
     const int d = (int)(e - at * quads) * 4;
-    float2 ml[kFewShares];
+    PartSum ml[kFewShares];
     f32x4_t of[kFewShares];
 #pragma unroll
     for (int s = 0; s < kFewShares; ++s)
@@ -801,16 +879,17 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_few_kern
             ml[s] = p.part_ml[s * all + at];
             of[s] = *(const f32x4_t *)(p.part_o + (s * all + at) * p.part_ld + d);      // (not written where a share saw nothing; not used then)
         }
-    float most = -HUGE_VALF, total = 0.f;
+    double most = -HUGE_VAL;
+    float total = 0.f;
 #pragma unroll
     for (int s = 0; s < kFewShares; ++s)
-        if (s < p.shares && ml[s].y != 0.f) most = fmaxf(most, ml[s].x);
+        if (s < p.shares && ml[s].total != 0.f) most = fmax(most, ml[s].base);
     f32x4_t v = {};
 #pragma unroll
     for (int s = 0; s < kFewShares; ++s)
-        if (s < p.shares && ml[s].y != 0.f) {
-            const float w = ml[s].x == most ? 1.f : __builtin_amdgcn_exp2f(ml[s].x - most);
-            total += w * ml[s].y;
+        if (s < p.shares && ml[s].total != 0.f) {
+            const float w = __builtin_amdgcn_exp2f((float)(ml[s].base - most));
+            total += w * ml[s].total;
             v += w * of[s];
         }
     const int ih = (int)(at / p.rows), image = ih / p.a.kv_heads;
@@ -832,12 +911,12 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(C
     __shared__ f32x4_t red[256];
     const long long at = blockIdx.x;
     if (threadIdx.x < 64) {
-        const float2 ml = (int)threadIdx.x < p.shares ? p.part_ml[threadIdx.x * all + at] : float2{-HUGE_VALF, 0.f};
-        const bool none = ml.y == 0.f;
-        float most = none ? -HUGE_VALF : ml.x;
-        for (int x = 32; x; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
-        const float w = none ? 0.f : ml.x == most ? 1.f : __builtin_amdgcn_exp2f(ml.x - most);
-        float sum = none ? 0.f : w * ml.y;
+        const PartSum ml = (int)threadIdx.x < p.shares ? p.part_ml[threadIdx.x * all + at] : PartSum{-HUGE_VAL, 0.f};
+        const bool none = ml.total == 0.f;
+        double most = none ? -HUGE_VAL : ml.base;
+        for (int x = 32; x; x >>= 1) most = fmax(most, __shfl_xor(most, x));
+        const float w = none ? 0.f : __builtin_amdgcn_exp2f((float)(ml.base - most));
+        float sum = none ? 0.f : w * ml.total;
         for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
         weights[threadIdx.x] = w;
         if (threadIdx.x == 0) sum_of = sum;
@@ -961,7 +1040,7 @@ static size_t need_of(const Plan &plan, int N, int kv_heads, int D)
 {
     if (plan.shares == 1) return 0;
     const size_t rows = (size_t)plan.shares * N * kv_heads * plan.rows;
-    return align_up(rows * part_row(D) * sizeof(float), 256) + rows * sizeof(float2);
+    return align_up(rows * part_row(D) * sizeof(float), 256) + rows * sizeof(PartSum);
 }
 
 size_t cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype)
@@ -988,7 +1067,7 @@ int cross_attention(const CrossArgs &a, size_t workspace_bytes)
     }
     p.part_ld = part_row(a.D);
     p.part_o = (float *)a.workspace;
-    p.part_ml = (float2 *)((char *)a.workspace + align_up((size_t)p.shares * a.N * a.kv_heads * p.rows * p.part_ld * sizeof(float), 256));
+    p.part_ml = (PartSum *)((char *)a.workspace + align_up((size_t)p.shares * a.N * a.kv_heads * p.rows * p.part_ld * sizeof(float), 256));
     return a.dtype == SQ_F32 ? run<float>(p, plan.block) : run<bf16_t>(p, plan.block);
 }
 
