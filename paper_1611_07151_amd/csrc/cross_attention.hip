@@ -145,7 +145,7 @@ template <typename T> __device__ __forceinline__ void row_of(const CrossParams &
 __device__ __forceinline__ float in_range(float score) { return fminf(fmaxf(score, -__FLT_MAX__), __FLT_MAX__); }
 __device__ __forceinline__ bool beyond(float base, float total) { return base != -HUGE_VALF && !(total > 0.f && total < HUGE_VALF); }
 
-// A row whose sums 32 bits do not hold, or into whose sums a hidden value that is not finite has gone as 0 * it: a wavefront makes it again
+// A row whose sums 32 bits do not hold (of scores, or of values too large to be added up), or into whose sums a hidden value that is not finite has gone as 0 * it: a wavefront makes it again
 // from the states it sees, lane by lane of the head's values, with scores and sums in 64 bits, which hold every product and sum of fp32
 // values.  area: the sums over the head's values to go with `total`, their mean where they are the result.
 template <typename T, int DP> __device__ __forceinline__ void row_again(const CrossParams &p, int image, int head, int r, int first, int end, float *area, double &base, float &total)
@@ -568,11 +568,10 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         double base_of = base[r];
         const bool lost = beyond(base[r], total[r]);
         bool odd = lost;
-        if (p.a.mask)
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) odd |= !__builtin_isfinite(o[r][d][i]);
+            for (int i = 0; i < 16; ++i) odd |= !__builtin_isfinite(o[r][d][i]);
         const uint64_t lanes = __ballot(odd && row < p.rows);
         uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
         if (__builtin_expect(again != 0, 0)) {
@@ -828,9 +827,7 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
         for (int w = 1; w < NW; ++w) top = fmaxf(top, bases[w][r]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += bases[w][r] == -HUGE_VALF ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f(bases[w][r] - top);
-        bool odd = beyond(top, sum);
-        if (mask) odd |= !(__builtin_isfinite(of[t][0]) && __builtin_isfinite(of[t][1]) && __builtin_isfinite(of[t][2]) && __builtin_isfinite(of[t][3]));
-        if (odd) again[r] = some_again = 1;
+        if (beyond(top, sum) || !(__builtin_isfinite(of[t][0]) && __builtin_isfinite(of[t][1]) && __builtin_isfinite(of[t][2]) && __builtin_isfinite(of[t][3]))) again[r] = some_again = 1;
         top_of[t] = top, sum_of[t] = sum;
     }
     __syncthreads();
@@ -884,14 +881,19 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_few_kern
 #pragma unroll
     for (int s = 0; s < kFewShares; ++s)
         if (s < p.shares && ml[s].total != 0.f) most = fmax(most, ml[s].base);
-    f32x4_t v = {};
+    float w[kFewShares];
 #pragma unroll
     for (int s = 0; s < kFewShares; ++s)
         if (s < p.shares && ml[s].total != 0.f) {
-            const float w = __builtin_amdgcn_exp2f((float)(ml[s].base - most));
-            total += w * ml[s].total;
-            v += w * of[s];
+            w[s] = __builtin_amdgcn_exp2f((float)(ml[s].base - most));
+            total += w[s] * ml[s].total;
         }
+    // each share's part of the mean, as the sum of the shares' sums may pass the range
+    const float inverse = 1.f / total;
+    f32x4_t v = {};
+#pragma unroll
+    for (int s = 0; s < kFewShares; ++s)
+        if (s < p.shares && ml[s].total != 0.f) v += w[s] * inverse * of[s];
     const int ih = (int)(at / p.rows), image = ih / p.a.kv_heads;
     const T *q;
     const uint8_t *mask;
@@ -899,7 +901,7 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_few_kern
     row_of<T>(p, image, ih - image * p.a.kv_heads, (int)(at - (long long)ih * p.rows), q, mask, out);
     const float f[4] = {v[0], v[1], v[2], v[3]};
     p.shares = 1;
-    put4<T>(p, out, 0, d, f, total, 1.f / total);
+    put4<T>(p, out, 0, d, f, total, 1.f);
 }
 
 // The shares' sums of a row, four neighbouring values to a thread, the shares dealt out among as many threads as a workgroup has beside that:
@@ -907,7 +909,7 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_few_kern
 constexpr int kMostShares = 64;
 template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(CrossParams p, long long all, int lanes)
 {
-    __shared__ float weights[kMostShares], sum_of;
+    __shared__ float weights[kMostShares];
     __shared__ f32x4_t red[256];
     const long long at = blockIdx.x;
     if (threadIdx.x < 64) {
@@ -918,8 +920,7 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(C
         const float w = none ? 0.f : __builtin_amdgcn_exp2f((float)(ml.base - most));
         float sum = none ? 0.f : w * ml.total;
         for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
-        weights[threadIdx.x] = w;
-        if (threadIdx.x == 0) sum_of = sum;
+        weights[threadIdx.x] = w == 0.f ? 0.f : w / sum;        // of the mean, as the sum of the shares' sums may pass the range
     }
     __syncthreads();
     const int group = threadIdx.x / (unsigned)lanes, groups = 256 / lanes, d = ((int)threadIdx.x - group * lanes) * 4;
@@ -939,7 +940,7 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(C
     row_of<T>(p, image, ih - image * p.a.kv_heads, (int)(at - (long long)ih * p.rows), q, mask, out);
     Vec<T, 4> o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o.v[i] = from_f32<T>(sum_of == 0.f ? 0.f : v[i] / sum_of);
+    for (int i = 0; i < 4; ++i) o.v[i] = from_f32<T>(v[i]);
     store_some<4>(out + d, o, p.a.D - d);
 }
 

@@ -126,3 +126,39 @@ def test_a_key_that_is_not_finite_beside_scores_past_the_range(sq, dt, n, lq, lk
     assert got[0].isnan().all()
     ref = largest(v, score, everything(n, lq, lk), heads, kv, 1.0)
     check(got[1:], ref[1:], bound_of(ref[1:], dt), "others")
+
+
+@pytest.mark.parametrize("dt,n,lq,lk,heads,kv,d", FORMS)
+@pytest.mark.parametrize("masked", (False, True))
+@pytest.mark.parametrize("jump", (False, True))
+def test_values_whose_sums_pass_the_range(sq, dt, n, lq, lk, heads, kv, d, masked, jump):
+    """Values up to 2^127 of either sign: every weighted mean is finite, sums of them are not.  jump: scores that stand far above those before,
+    which sums are not yet brought down for."""
+    print(dt, n, lq, lk, heads, kv, d, masked, jump, flush=True)
+    q, k, v = inputs(n, lq, lk, heads, kv, d, dt, 41)
+    if jump:
+        q, k = q.abs(), k / 8
+        k[:, lk // 2:] = k[:, lk // 2:].abs() + 0.25 * torch.rand((n, lk - lk // 2, 1), generator=gen(42)).to(dt)
+    v = torch.where(torch.rand(v.shape, generator=gen(43)) < 0.9, 1.0, -1.0) * (v.float().abs() % 1 + 0.5) * 2.0 ** 126
+    v[..., ::3] *= 2.0 ** -20
+    v = v.to(dt)
+    mask = torch.rand((n, lk), generator=gen(44)) < 0.7 if masked else None
+    seen = mask[:, None].expand(n, lq, lk) if masked else everything(n, lq, lk)
+    ref, bound = reference_on_gpu(q, k, v, heads, kv, d ** -0.5, seen, dt)
+    check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads, kv, mask=mask.cuda() if masked else None), ref, bound, (masked, jump))
+
+
+@pytest.mark.parametrize("dt,n,lq,lk,heads,kv,d", FORMS)
+def test_values_that_are_not_finite_stay_in_their_place(sq, dt, n, lq, lk, heads, kv, d):
+    """Without a mask a NaN or infinite value makes those results NaN or infinite that it is part of, and leaves the others."""
+    q, k, v = inputs(n, lq, lk, heads, kv, d, dt, 45)
+    ref, bound = reference_on_gpu(q, k, v, heads, kv, d ** -0.5, everything(n, lq, lk), dt)
+    bad = v.clone()
+    bad[0, lk // 3, 0], bad[0, lk - 1, d // 2], bad[0, 0, d - 1] = math.nan, math.inf, -math.inf
+    got = sq.sq_cross_attention_forward(q.cuda(), k.cuda(), bad.cuda(), heads, kv).cpu()
+    struck = torch.zeros_like(got, dtype=torch.bool).reshape(n, lq, heads, d)
+    for i in (0, d // 2, d - 1):
+        struck[0, :, :heads // kv, i] = True
+    struck = struck.reshape(n, lq, heads * d)
+    assert not got[struck].isfinite().any()
+    check(torch.where(struck, torch.zeros_like(got), got), torch.where(struck, torch.zeros_like(ref), ref), bound, "others")
