@@ -637,9 +637,9 @@ int sq_mxfp4_linear_forward(const void *in, const void *packed_w, const float *b
  *   rounded to bfloat16 before it multiplies v, and may be before it is added up.
  *   Where a query's scaled scores pass what fp32 holds with a useful rest (from about 2^30 in magnitude on), its products with keys
  *   pass 2^128, or its weighted values, whose weights may be up to 2^13 each before they are added up, pass it, the query is made
- *   again with scores and sums in 64 bits: right, but slow (a wavefront takes one state after the other).
+ *   again with scores and sums in 64 bits: right, but some hundred times slower.
  *   Hidden states have no influence on a result, whatever they hold, and states behind a length are not read.  (An infinity or NaN in
- *   a hidden state costs time: the rows that it touches are made again one by one.)  An infinity or NaN in a state that a query sees
+ *   a hidden state costs time: the queries of its image and head are made again likewise; a length in place of a mask avoids it.)  An infinity or NaN in a state that a query sees
  *   may make the results of that query, in the heads that share the state's head, NaN, and no others.
  *   workspace: sq_cross_attention_workspace_bytes() bytes of device scratch, 256-byte aligned (else SQ_ERR_WORKSPACE; 0 = none is
  *     needed, workspace may be NULL).  Contents on return are unspecified; two calls in flight at once need two.

@@ -145,6 +145,8 @@ template <typename T> __device__ __forceinline__ void row_of(const CrossParams &
 __device__ __forceinline__ float in_range(float score) { return fminf(fmaxf(score, -__FLT_MAX__), __FLT_MAX__); }
 __device__ __forceinline__ bool beyond(float base, float total) { return base != -HUGE_VALF && !(total > 0.f && total < HUGE_VALF); }
 
+__device__ __forceinline__ float lane_of(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
 // A row whose sums 32 bits do not hold (of scores, or of values too large to be added up), or into whose sums a hidden value that is not finite has gone as 0 * it: a wavefront makes it again
 // from the states it sees, lane by lane of the head's values, with scores and sums in 64 bits, which hold every product and sum of fp32
 // values.  area: the sums over the head's values to go with `total`, their mean where they are the result.
@@ -166,23 +168,45 @@ template <typename T, int DP> __device__ __forceinline__ void row_again(const Cr
         odd |= !__builtin_isfinite(qv[e]);
     }
     odd = __any(odd);
-    for (int j = first; j < end; ++j) {
-        if (mask && !mask[j]) continue;
+    // 64 states at a time: a lane each for the scores, then the lanes of the head's values
+    for (int j0 = first; j0 < end; j0 += 64) {
+        const int j = min(j0 + lane, end - 1);
+        const bool seen = j0 + lane < end && (!mask || mask[j]);
+        if (!__any(seen)) continue;
         sees = true;
         if (odd) l = __builtin_nan("");
         if (l != l) break;          // and so is the result
         double dot = 0.0;
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < D) dot = __builtin_fma((double)qv[e], (double)to_f32(k0[j * p.a.ld_k + lane + 64 * e]), dot);
-        for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
-        const double up = fmax(m, dot);
-        const float shrink = m == -HUGE_VAL ? 0.f : __builtin_amdgcn_exp2f((float)((m - up) * p.c)), w = dot == -HUGE_VAL ? 0.f : __builtin_amdgcn_exp2f((float)((dot - up) * p.c));
-        m = up;
-        l = l * shrink + w;
+            for (int d = 0; d < 64 && 64 * e + d < D; d += 8) {
+                float k[8];
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < D) sum[e] = sum[e] * shrink + (double)w * to_f32(v0[j * p.a.ld_v + lane + 64 * e]);
+                for (int i = 0; i < 8; ++i) k[i] = to_f32(k0[j * p.a.ld_k + min(64 * e + d + i, D - 1)]);       // behind the head times the zeros of the query
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dot = __builtin_fma((double)lane_of(qv[e], d + i), (double)k[i], dot);
+            }
+        double up = seen ? dot : -HUGE_VAL;
+        for (int x = 32; x; x >>= 1) up = fmax(up, __shfl_xor(up, x));
+        up = fmax(up, m);
+        const float shrink = m == -HUGE_VAL ? 0.f : __builtin_amdgcn_exp2f((float)((m - up) * p.c));
+        const float w = !seen || dot == -HUGE_VAL ? 0.f : __builtin_amdgcn_exp2f((float)((dot - up) * p.c));
+        m = up;
+        double all = w;
+        for (int x = 32; x; x >>= 1) all += __shfl_xor(all, x);
+        l = l * shrink + all;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int d = min(lane + 64 * e, D - 1);
+            sum[e] *= shrink;
+            for (int i = 0; i < 64 && j0 + i < end; i += 8) {
+                float v[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] = to_f32(v0[min(j0 + i + x, end - 1) * p.a.ld_v + d]);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) sum[e] = __builtin_fma((double)lane_of(w, i + x), lane_of(w, i + x) == 0.f ? 0.0 : (double)v[x], sum[e]);
+            }
+        }
     }
     // a share's sums are brought below the largest value by a power of two
     double by = 0.0;
@@ -206,7 +230,6 @@ template <typename T> __device__ __forceinline__ bool finite_states(const CrossP
     const T *const k0 = (const T *)p.a.k + (long long)image * p.a.Lk * p.a.ld_k + head * p.a.D, *const v0 = (const T *)p.a.v + (long long)image * p.a.Lk * p.a.ld_v + head * p.a.D;
     bool odd = false;
     for (int d = threadIdx.x & 63; d < p.a.D; d += 64)
-#pragma unroll 4
         for (int j = first; j < end; ++j) odd |= !__builtin_isfinite(to_f32(k0[j * p.a.ld_k + d])) | !__builtin_isfinite(to_f32(v0[j * p.a.ld_v + d]));
     return !__any(odd);
 }
@@ -490,7 +513,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         if (__any(far)) {
             // whether a row sees any state of this tile, which its scores may not tell where all are -infinity
             bool some = true;
-            if (by_state) some = __any(biases[img][lane & (KT - 1)] == 0.f);
+            if (hidden && by_state) some = __any(biases[img][lane & (KT - 1)] == 0.f);
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 if (hidden && by_pair) some = (seen_of[r] | __shfl_xor(seen_of[r], 32)) != 0;
@@ -567,12 +590,12 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         const int row = row0 + 32 * r;
         double base_of = base[r];
         const bool lost = beyond(base[r], total[r]);
-        bool odd = lost;
+        float zeros[2] = {};        // NaN where a sum is not finite
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) odd |= !__builtin_isfinite(o[r][d][i]);
-        const uint64_t lanes = __ballot(odd && row < p.rows);
+            for (int i = 0; i < 16; ++i) zeros[i & 1] = __builtin_fmaf(o[r][d][i], 0.f, zeros[i & 1]);
+        const uint64_t lanes = __ballot((lost || !(zeros[0] + zeros[1] == 0.f)) && row < p.rows);
         uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
         if (__builtin_expect(again != 0, 0)) {
             if (!p.a.mask && !finite_states<T>(p, image, head, first, end)) {
@@ -827,7 +850,8 @@ template <typename T, int DP, int NW, bool EVEN> __global__ __launch_bounds__(64
         for (int w = 1; w < NW; ++w) top = fmaxf(top, bases[w][r]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += bases[w][r] == -HUGE_VALF ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f(bases[w][r] - top);
-        if (beyond(top, sum) || !(__builtin_isfinite(of[t][0]) && __builtin_isfinite(of[t][1]) && __builtin_isfinite(of[t][2]) && __builtin_isfinite(of[t][3]))) again[r] = some_again = 1;
+        const f32x4_t zeros = 0.f * of[t];      // NaN where a sum is not finite
+        if (beyond(top, sum) || !(zeros[0] + zeros[1] + (zeros[2] + zeros[3]) == 0.f)) again[r] = some_again = 1;
         top_of[t] = top, sum_of[t] = sum;
     }
     __syncthreads();
