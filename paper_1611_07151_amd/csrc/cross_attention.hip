@@ -980,6 +980,10 @@ template <typename T> __global__ __launch_bounds__(256) void cross_join_kernel(C
 constexpr int wave_count(int DP) { return DP <= 64 ? 16 : DP <= 160 ? 8 : 4; }
 int padded(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 160 ? 160 : 256; }
 
+int part_row(int D) { return (D + 3) / 4 * 4; }
+// Workgroups of the launch that joins the shares of `all` rows.
+double join_blocks(long long all, int D, int shares) { return shares <= kFewShares ? (double)((all * (part_row(D) / 4) - 1) / 256 + 1) : (double)all; }
+
 // How the rows are shared out, in blocks of `block` (16: the form for few rows), and the states, in shares of `share`.  By estimate: us of a
 // workgroup's pass over a tile of states (bf16 64, fp32 32; in the form for few rows what its wavefronts take at a time) when it has a compute
 // unit to itself and when units are full, from what heads of 64 measured; a second launch that joins shares costs 4 us, and their sums' bytes.
@@ -1006,6 +1010,7 @@ bool plan_of(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype, P
         for (int want = 1; want <= std::min(units, kMostShares); want += want < 4 ? 1 : want < 16 ? 4 : 16) {
             const int each = (units - 1) / want + 1, shares = (units - 1) / each + 1;
             if ((shares != want && want > 1) || !one_launch(blocks * shares, 1024)) continue;
+            if (shares > 1 && !one_launch(join_blocks(N * kv_heads * rows, D, shares), 256)) continue;
             const double on_one = std::ceil(blocks * shares / 256);
             const double us = 3.0 + (w.block == 16 ? 0.8 * on_one : 1.5) + each * std::max(w.alone * std::ceil(on_one / w.fit), w.full * on_one) +
                               (shares > 1 ? 4.0 + 4e-6 * shares * N * kv_heads * rows * D : 0.0);
@@ -1017,8 +1022,6 @@ bool plan_of(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype, P
     }
     return best < HUGE_VAL;
 }
-int part_row(int D) { return (D + 3) / 4 * 4; }
-
 template <typename T, int DP, bool EVEN> int launch(const CrossParams &p, int block)
 {
     const dim3 grid((unsigned)(p.a.N * p.a.kv_heads) * p.tiles * p.shares);
@@ -1057,13 +1060,14 @@ template <typename T> int run(const CrossParams &p, int block)
     if (p.shares == 1) return SQ_OK;
     const long long all = (long long)p.a.N * p.a.kv_heads * p.rows;
     const LaunchScope prof("cross_join", 0, 0);
+    const dim3 grid((unsigned)join_blocks(all, p.a.D, p.shares));
     if (p.shares <= kFewShares) {
-        hipLaunchKernelGGL((cross_join_few_kernel<T>), dim3((unsigned)((all * (p.part_ld / 4) - 1) / 256 + 1)), dim3(256), 0, current_stream(), p, all);
+        hipLaunchKernelGGL((cross_join_few_kernel<T>), grid, dim3(256), 0, current_stream(), p, all);
         return check_launch();
     }
     int lanes = 1;
     while (lanes * 4 < p.part_ld) lanes *= 2;
-    hipLaunchKernelGGL((cross_join_kernel<T>), dim3((unsigned)all), dim3(256), 0, current_stream(), p, all, lanes);
+    hipLaunchKernelGGL((cross_join_kernel<T>), grid, dim3(256), 0, current_stream(), p, all, lanes);
     return check_launch();
 }
 
