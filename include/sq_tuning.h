@@ -80,6 +80,15 @@ void sq_tune_blocked_force_tile(int layer_blocks, int pixel_blocks);
  * -1 = for maps of 200 MiB and more (default).  Per host thread. */
 void sq_tune_conv7_f32out_rows(int mode);
 
+/* Which form a call of sq_mxfp4_linear_forward or sq_cross_attention_forward takes, for tests that have to reach each.
+ *   sq_tune_mxfp4_linear_plan: plan[0] x plan[1] results to a workgroup, plan[2] = whether rows that are not packed are packed in
+ *     the product.
+ *   sq_tune_cross_attention_plan: plan[0] queries (times heads that share states) to a workgroup, plan[1] workgroups that share
+ *     a query's states, plan[2] states to each; mask_by_queries: with a mask whose mask_row is not 0.
+ * SQ_ERR_SHAPE and SQ_ERR_UNSUPPORTED where the call would return them. */
+int sq_tune_mxfp4_linear_plan(int rows, int Cin, int Cout, int *plan);
+int sq_tune_cross_attention_plan(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype, int mask_by_queries, int *plan);
+
 /* Host-side self check of the division-by-multiplication the kernels use: number of x in
  * [0, x_max] for which it disagrees with x / d. */
 long long sq_tune_fastdiv_mismatches(unsigned d, unsigned x_max);

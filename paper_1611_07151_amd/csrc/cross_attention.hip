@@ -1080,6 +1080,23 @@ static size_t need_of(const Plan &plan, int N, int kv_heads, int D)
     return align_up(rows * part_row(D) * sizeof(float), 256) + rows * sizeof(PartSum);
 }
 
+// The wider blocks have no registers left for a mask by rows: half as wide ones in their place, with the same shares.
+static bool for_mask_by_rows(Plan &plan, int N, int kv_heads)
+{
+    if (plan.block != 256) return true;
+    plan.block = 128, plan.tiles = (plan.rows - 1) / 128 + 1;
+    return one_launch((double)N * kv_heads * plan.tiles * plan.shares, 256);
+}
+
+extern "C" int sq_tune_cross_attention_plan(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype, int mask_by_queries, int *plan)
+{
+    if (!plan || N <= 0 || Lq <= 0 || Lk < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || D <= 0 || D > 256) return SQ_ERR_SHAPE;
+    Plan of{};
+    if (!plan_of(N, Lq, Lk, heads, kv_heads, D, dtype, of) || (mask_by_queries && !for_mask_by_rows(of, N, kv_heads))) return SQ_ERR_UNSUPPORTED;
+    plan[0] = of.block, plan[1] = of.shares, plan[2] = of.share;
+    return SQ_OK;
+}
+
 size_t cross_attention_workspace_bytes(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype)
 {
     Plan plan{};
@@ -1091,6 +1108,7 @@ int cross_attention(const CrossArgs &a, size_t workspace_bytes)
     Plan plan{};
     if (!plan_of(a.N, a.Lq, a.Lk, a.heads, a.kv_heads, a.D, a.dtype, plan)) return SQ_ERR_UNSUPPORTED;
     if (!enough_workspace(need_of(plan, a.N, a.kv_heads, a.D), a.workspace, workspace_bytes)) return SQ_ERR_WORKSPACE;
+    if (a.mask && a.mask_row && !for_mask_by_rows(plan, a.N, a.kv_heads)) return SQ_ERR_UNSUPPORTED;
     CrossParams p{};
     p.a = a;
     p.group = a.heads / a.kv_heads;
@@ -1098,10 +1116,6 @@ int cross_attention(const CrossArgs &a, size_t workspace_bytes)
     p.c = a.scale == 0 ? 1.f : std::fabs(a.scale) * kLog2e;
     p.keep = a.scale == 0 ? 0 : 0xffffffffu;
     p.flip = a.scale < 0 ? (a.dtype == SQ_F32 ? 0x80000000u : 0x80008000u) : 0;
-    if (plan.block == 256 && a.mask && a.mask_row) {       // the wider blocks have no registers left for a mask by rows
-        plan.block = 128, p.tiles = (plan.rows - 1) / 128 + 1;
-        if (!one_launch((double)a.N * a.kv_heads * p.tiles * p.shares, 256)) return SQ_ERR_UNSUPPORTED;
-    }
     p.part_ld = part_row(a.D);
     p.part_o = (float *)a.workspace;
     p.part_ml = (PartSum *)((char *)a.workspace + align_up((size_t)p.shares * a.N * a.kv_heads * p.rows * p.part_ld * sizeof(float), 256));

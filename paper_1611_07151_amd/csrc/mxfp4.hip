@@ -528,6 +528,15 @@ int mxfp4_linear(const LinearArgs &p, size_t workspace_bytes)
     return p.out_dtype == SQ_F32 ? by_size<float>(a, plan.which) : by_size<bf16_t>(a, plan.which);
 }
 
+extern "C" int sq_tune_mxfp4_linear_plan(int rows, int Cin, int Cout, int *plan)
+{
+    if (!plan || rows <= 0 || Cin <= 0 || Cout <= 0) return SQ_ERR_SHAPE;
+    const Plan of = plan_of(rows, Cin, Cout);
+    if (of.which == kNone) return SQ_ERR_UNSUPPORTED;
+    plan[0] = of.which < 0 ? 16 : kTilings[of.which].BM, plan[1] = of.which < 0 ? 16 : kTilings[of.which].BN, plan[2] = of.raw;
+    return SQ_OK;
+}
+
 bool mxfp4_register_kernels()
 {
     hipFuncAttributes a;

@@ -29,6 +29,7 @@ def sq():
 # n, lq, lk, heads, kv_heads, d
 FORMS = [(F32, 1, 5, 200, 2, 1, 64), (F32, 1, 1, 300, 1, 1, 100), (F32, 1, 1030, 130, 8, 8, 64), (F32, 1, 1030, 300, 4, 2, 33), (F32, 1, 1030, 65, 16, 16, 160),
          (F32, 3, 1, 1000, 8, 8, 25), (BF16, 1, 5, 300, 2, 1, 64), (BF16, 1, 1, 1000, 1, 1, 100), (BF16, 1, 700, 300, 8, 8, 64), (BF16, 8, 500, 130, 16, 16, 64),
+         (BF16, 2, 2000, 130, 32, 8, 64), (BF16, 4, 1000, 150, 32, 8, 30),
          (BF16, 1, 1030, 1000, 4, 2, 40), (BF16, 1, 1030, 130, 8, 8, 160), (BF16, 2, 70, 200, 4, 4, 59)]
 
 
