@@ -179,6 +179,7 @@ template <typename T, int DP> __device__ __forceinline__ void row_again(const Cr
         double dot = 0.0;
 #pragma unroll
         for (int e = 0; e < E; ++e)
+#pragma unroll 1
             for (int d = 0; d < 64 && 64 * e + d < D; d += 8) {
                 float k[8];
 #pragma unroll
@@ -199,6 +200,7 @@ template <typename T, int DP> __device__ __forceinline__ void row_again(const Cr
         for (int e = 0; e < E; ++e) {
             const int d = min(lane + 64 * e, D - 1);
             sum[e] *= shrink;
+#pragma unroll 1
             for (int i = 0; i < 64 && j0 + i < end; i += 8) {
                 float v[8];
 #pragma unroll
@@ -254,8 +256,13 @@ template <typename T> __device__ __forceinline__ void put4(const CrossParams &p,
 // within the lane and over the two halves.  The scores' places in the accumulators are, as they are, the second operand of the
 // product with the transposed values: lane half h has states 8 i + 4 h to 8 i + 4 h + 3, and the values' lanes take the same ones.
 // fp32 heads of up to 128 run on the bfloat16 instructions, every operand as the sum of three bfloat16 values (x = h + m + l, exact; of the nine
-// products the six down to 2^-16 of the largest, the smallest first), each a plane of its own in LDS or registers; wider ones, whose planes
-// LDS has no room for, on the fp32 instructions (4 x 3025 x 729 in 8 heads of 64: 160 us on those, 115 so).
+// products the six down to 2^-16 of the largest, the smallest first), each a plane of its own in LDS or registers (4 x 3025 x 729 in 8 heads of
+// 64: 160 us on the fp32 instructions, 115 so).  Wider ones run on the fp32 instructions: two images of the planes take 126 KB of LDS at 160
+// values, which would fit and has not been made, and 212 KB at 256, which does not.
+// bf16: the exponentials are rounded to bfloat16, half a step or 2^-8 each, as the matrix instruction takes them, and it is the rounded ones that
+// are added up, so that a row's weights add up to one.  Against 64 bits results are off by 2.0e-3 to 2.3e-3 of their size so, 1.5e-3 to
+// 1.7e-3 with fp32 exponentials (of that nearly all the rounding of the result itself).  Exponentials in two pieces would take half as
+// many matrix instructions again, and five vector instructions more for two scores, where both bound the kernel.
 // Bound by the vector instructions of the exponentials beside the matrix unit: bf16, 16 heads of 64, 16 images of 3025 queries to 4096
 // states 880 to 990 us (820 to 920 TFLOP/s, matrix unit 43 % busy), 4 images in heads of 128 440 to 460 (880 to 930).  Sums by additions instead of
 // the two-value instruction need more registers than there are (spills: 1280 us for 960).
@@ -987,9 +994,10 @@ double join_blocks(long long all, int D, int shares) { return shares <= kFewShar
 // How the rows are shared out, in blocks of `block` (16: the form for few rows), and the states, in shares of `share`.  By estimate: us of a
 // workgroup's pass over a tile of states (bf16 64, fp32 32; in the form for few rows what its wavefronts take at a time) when it has a compute
 // unit to itself and when units are full, from what heads of 64 measured; a second launch that joins shares costs 4 us, and their sums' bytes.
-// (us, blocks of 16 / 128 / 256, bf16, 8 heads of 64: 64 rows x 2000 states 14.4 / 12.4 / 16.2, 512 x 2000 15.9 / 19.9 / 24.6, 2 images of 2000 x
-// 2000 110 / 35 / 72, 4 of 3025 x 4096 with 16 heads 1057 / 250 / 236; 256 rows in heads of 128 435 / 820.)  Of plans within 5 % the one with
-// the most shares: images may have fewer states than the others.
+// (us, blocks of 16 / 128 / 256, bf16, 8 heads of 64: 64 rows x 2000 states 12.2 / 11.0 / 13.3, 512 x 2000 16.0 / 17.6 / 21.5, 2 images of 2000 x
+// 2000 108 / 35 / 50; 16 heads: 4 images of 1024 x 4096 366 / 94 / 103, of 3025 x 4096 1049 / 252 / 248, 16 images of these 4190 / 969 / 934.  The
+// estimate is short of that where three blocks of 256 come to a unit that holds two, as in the second last, and takes 128.)  Of plans within
+// 5 % the one with the most shares: images may have fewer states than the others.
 struct Plan { int rows, tiles, share, shares, block; };
 bool plan_of(int N, int Lq, int Lk, int heads, int kv_heads, int D, int dtype, Plan &plan)
 {

@@ -163,3 +163,36 @@ def test_values_that_are_not_finite_stay_in_their_place(sq, dt, n, lq, lk, heads
     struck = struck.reshape(n, lq, heads * d)
     assert not got[struck].isfinite().any()
     check(torch.where(struck, torch.zeros_like(got), got), torch.where(struck, torch.zeros_like(ref), ref), bound, "others")
+
+
+@pytest.mark.parametrize("dt,n,lq,lk,heads,kv,d", FORMS)
+@pytest.mark.parametrize("kind", ("none", "states", "pairs"))
+def test_queries_that_are_not_finite(sq, dt, n, lq, lk, heads, kv, d, kind):
+    """A query with a NaN or an infinity gets NaN where it sees anything, zeros where it does not, and leaves the others alone."""
+    q, k, v = inputs(n, lq, lk, heads, kv, d, dt, 51)
+    mask, seen = None, everything(n, lq, lk)
+    if kind == "states":
+        mask = torch.rand((n, lk), generator=gen(52)) < 0.5
+        mask[-1], mask[0, 0] = False, n > 1
+        seen = mask[:, None].expand(n, lq, lk)
+    elif kind == "pairs":
+        mask = torch.rand((n, lq, lk), generator=gen(52)) < 0.5
+        mask[:, ::3] = False
+        seen = mask
+    ref, bound = reference_on_gpu(q, k, v, heads, kv, d ** -0.5, seen, dt)
+    bad = q.clone().reshape(n, lq, heads, d)
+    bad[:, ::2, 0, 0], bad[:, 1::2, heads - 1, d - 1] = math.nan, math.inf
+    struck = ~bad.isfinite().all(3, keepdim=True) & seen.any(2)[..., None, None]
+    struck = struck.expand(n, lq, heads, d).reshape(n, lq, heads * d)
+    got = sq.sq_cross_attention_forward(bad.reshape(n, lq, heads * d).cuda(), k.cuda(), v.cuda(), heads, kv, mask=None if mask is None else mask.cuda()).cpu()
+    assert got[struck].isnan().all()
+    check(torch.where(struck, torch.zeros_like(got), got), torch.where(struck, torch.zeros_like(ref), ref), bound, kind)
+
+
+@pytest.mark.parametrize("scale", (1e-42, -1e-42, 1e-37))
+@pytest.mark.parametrize("dt,n,lq,lk,heads,kv,d", FORMS)
+def test_scales_below_the_normal_numbers(sq, dt, n, lq, lk, heads, kv, d, scale):
+    """All scores are as good as equal."""
+    q, k, v = inputs(n, lq, lk, heads, kv, d, dt, 53)
+    ref, bound = reference_on_gpu(q, k, v, heads, kv, scale, everything(n, lq, lk), dt)
+    check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads, kv, scale=scale), ref, bound, scale)
