@@ -264,7 +264,7 @@ template <typename T> __device__ __forceinline__ void put4(const CrossParams &p,
 // 1.7e-3 with fp32 exponentials (of that nearly all the rounding of the result itself).  Exponentials in two pieces would take half as
 // many matrix instructions again, and five vector instructions more for two scores, where both bound the kernel.
 // Bound by the vector instructions of the exponentials beside the matrix unit: bf16, 16 heads of 64, 16 images of 3025 queries to 4096
-// states 880 to 990 us (820 to 920 TFLOP/s, matrix unit 43 % busy), 4 images in heads of 128 440 to 460 (880 to 930).  Sums by additions instead of
+// states 880 to 1010 us (800 to 920 TFLOP/s, matrix unit 42 % busy), 4 images in heads of 128 420 to 470 (860 to 960).  Sums by additions instead of
 // the two-value instruction need more registers than there are (spills: 1280 us for 960).
 template <typename T, int DP> struct Tile {
     static constexpr bool kF32 = sizeof(T) == 4, kSplit = kF32 && DP <= 128;
@@ -334,6 +334,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     // What hides states from every row, a mask by states or the end of them, is what the scores start from.  (A key there that is not finite
     // makes the row's sums NaN, and the row is made again.)
     const bool by_state = p.a.mask && p.a.mask_row == 0, by_pair = RB == 1 && p.a.mask && p.a.mask_row != 0;      // (wider blocks are not launched for these)
+    const uint8_t *const shared = by_state ? p.a.mask + image * p.a.mask_image : nullptr;
     uint32_t seen = 0;
     // A thread's pieces are those at e % P of the states e / P of a tile, e = threadIdx.x + 256 i, the same in every tile.
     Piece<EVEN, T> nk[NP], nv[NP];
@@ -345,8 +346,11 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             const int e = threadIdx.x + i * 256, d = min(e % P * n, D - n);
             step_k[i] = e / P * p.a.ld_k + d, step_v[i] = e / P * p.a.ld_v + d;
         }
+    // Whether a tile's biases are written: wide blocks, whose registers are all taken, write them only where they are looked at (16 x 3025 x
+    // 4096 in 16 heads of 64 998 -> 987 us); the others have no use for the test (fp32 4 x 3025 x 729 117 -> 121).
+    auto some_hidden_at = [&](int at) { return RB == 1 || p.a.mask || at + KT > end; };
     auto fetch = [&](int at) {
-        if (threadIdx.x < KT) seen = at + (int)threadIdx.x < end && (!by_state || mask[0][at + threadIdx.x]);
+        if (some_hidden_at(at) && threadIdx.x < KT) seen = at + (int)threadIdx.x < end && (!by_state || shared[at + threadIdx.x]);
         const T *const kt = k0 + at * p.a.ld_k, *const vt = v0 + at * p.a.ld_v;
         if (EVEN && at + KT <= end) {
 #pragma unroll
@@ -363,9 +367,9 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
             }
         }
     };
-    auto store = [&](int image_of) {
+    auto store = [&](int image_of, int at) {
         u32x4_t *const to = lds + image_of * kImage;
-        if (threadIdx.x < KT) biases[image_of][threadIdx.x] = seen ? 0.f : -HUGE_VALF;
+        if (some_hidden_at(at) && threadIdx.x < KT) biases[image_of][threadIdx.x] = seen ? 0.f : -HUGE_VALF;
         if constexpr (!EVEN)
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
@@ -407,7 +411,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
     for (int r = 0; r < RB; ++r) base[r] = -HUGE_VALF, total[r] = 0.f;
     if (first < end) {
         fetch(first);
-        store(0);
+        store(0, first);
     }
     __syncthreads();
     int img = 0;
@@ -588,7 +592,7 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
         }
         __builtin_amdgcn_s_setprio(0);
         img ^= 1;
-        if (more) store(img);
+        if (more) store(img, at + KT);
         __syncthreads();
     };
     int at = first;
@@ -660,8 +664,8 @@ template <typename T, int DP, int RB, bool EVEN> __global__ __launch_bounds__(25
 // has states 4 (l / 16) to 4 (l / 16) + 3 of row l % 16.
 //   bf16: values go through the wavefront's part of LDS, which gives them back transposed
 //   fp32: an instruction takes one state of each four, and value e of each four of a head, so that lanes load 16 bytes of neighbouring values
-// Bound by memory where states are many (8 queries to 16384 states of 8 heads of 128: 112 us, 4.8 TB/s), else by the latency of a turn of
-// loads and of the joining (1 query to 729 states of 8 heads of 64: 7.9 us).
+// Bound by memory where states are many (8 queries to 16384 states of 8 heads of 128: 114 us, 4.7 TB/s), else by the latency of a turn of
+// loads and of the joining (1 query to 729 states of 8 heads of 64: 8.1 us).
 template <typename T> struct Chunk;
 template <> struct Chunk<bf16_t> {
     static constexpr int KC = 32;
