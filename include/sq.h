@@ -635,7 +635,7 @@ int sq_mxfp4_linear_forward(const void *in, const void *packed_w, const float *b
  *   Scores, their maxima and sums are fp32, and so are the products for SQ_F32 (heads of up to 128 may run on the bfloat16 matrix
  *   instructions as in sq_linear_forward, with the same error but for operands below 2^-110 in magnitude); for SQ_BF16 each p is
  *   rounded to bfloat16 before it multiplies v, and may be before it is added up.
- *   Where a query's scaled scores pass what fp32 holds with a useful rest (from about 2^30 in magnitude on), its products with keys
+ *   Where a query's scaled scores pass what fp32 holds with a useful rest (from about 2^26 in magnitude on), its products with keys
  *   pass 2^128, or its weighted values, whose weights may be up to 2^13 each before they are added up, pass it, the query is made
  *   again with scores and sums in 64 bits: right, but some hundred times slower.
  *   Hidden states have no influence on a result, whatever they hold, and states behind a length are not read.  (An infinity or NaN in

@@ -140,10 +140,11 @@ template <typename T> __device__ __forceinline__ void row_of(const CrossParams &
 }
 
 // What a row's exponents may be taken against: a scaled score of any size, held within fp32's range, or -infinity where no state has been
-// seen.  A score past that range, and one so far out that its product with c is rounded by more than the exponent's range, leaves a
-// sum that is zero or not finite, by which the row is known.
+// seen.  The exponentials' sum is about one at least and 2^43 at most (2^30 states, 2^13 each).  A score past the range leaves a sum that is
+// zero or infinite, and one so far out, from about 2^26 on, that its product with c is rounded by several powers of two may leave a sum that
+// is too small for the bits of its products with small values, or too large: by that the row is known.
 __device__ __forceinline__ float in_range(float score) { return fminf(fmaxf(score, -__FLT_MAX__), __FLT_MAX__); }
-__device__ __forceinline__ bool beyond(float base, float total) { return base != -HUGE_VALF && !(total > 0.f && total < HUGE_VALF); }
+__device__ __forceinline__ bool beyond(float base, float total) { return base != -HUGE_VALF && !(total > 0x1p-8f && total < 0x1p60f); }
 
 __device__ __forceinline__ float lane_of(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
 

@@ -196,3 +196,14 @@ def test_scales_below_the_normal_numbers(sq, dt, n, lq, lk, heads, kv, d, scale)
     q, k, v = inputs(n, lq, lk, heads, kv, d, dt, 53)
     ref, bound = reference_on_gpu(q, k, v, heads, kv, scale, everything(n, lq, lk), dt)
     check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads, kv, scale=scale), ref, bound, scale)
+
+
+@pytest.mark.parametrize("size", (1e-20, 1e-28, 1e20))
+@pytest.mark.parametrize("dt,n,lq,lk,heads,kv,d", FORMS)
+def test_small_and_large_values_under_large_scales(sq, dt, n, lq, lk, heads, kv, d, size):
+    """Weights that are far from one because a large score's product is rounded lose nothing of small values and do not overflow large ones."""
+    q, k, v, score = levels(n, lq, lk, heads, kv, d, dt, 1.0, 1.0, 0, 61)
+    v = (v.float() * size).to(dt)
+    for scale in (3e7, 1e8, 3.1e8, 1.1e9, 3.7e9, 7.3e9):
+        ref = largest(v, score, everything(n, lq, lk), heads, kv, scale)
+        check(sq.sq_cross_attention_forward(q.cuda(), k.cuda(), v.cuda(), heads, kv, scale=scale), ref, bound_of(ref, dt), (size, scale))
